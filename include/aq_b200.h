@@ -97,7 +97,7 @@ enum {
   AQ_RAW_LIST = 11       /* device pointer to an array of n_batch device pointers, or 0: the raw messages
                             of aq_decode_list, one per sample; a null entry = no raw message for that sample */
 };
-enum { AQ_FP16 = 0, AQ_BF16 = 1 };
+enum { AQ_FP16 = 0, AQ_BF16 = 1, AQ_FP32 = 2 };   /* AQ_FP32: logits of a stage handle only (below) */
 /*
  * AQ_ROUND_INTERVAL: Q of Section 4.1 as described at the top of this file.
  * AQ_ROUND_STOCHASTIC: the unbiased Q that Theorem 3.1 assumes (its footnote sketches a randomised
@@ -370,6 +370,130 @@ int aq_wire_copy_grad(aq_handle* h, int dst_device, void* packed_dst, float* sca
  */
 int aq_export_sample(aq_handle* h, int64_t sample_id, void* m_host, uint8_t* seen_host);
 int aq_import_sample(aq_handle* h, int64_t sample_id, const void* m_host, uint8_t seen);
+
+/* ---------------------------------------------------------------------------------------------
+ * What a pipeline stage computes between its boundaries.
+ *
+ * A stage decodes an activation, runs its layers, and encodes the result; on the way back it quantizes
+ * the gradient of the activation.  Three operators of those layers, each with its gradient, that a stage
+ * of a language model needs next to the codec: the norm and rotation of query and key heads, the gated
+ * feed-forward product, and the last stage's loss.
+ *
+ * They run on a stage handle, which holds an element type, a stream, a status word and workspaces, and
+ * no model state.  Rules as for the codec's handles: calls enqueue on the handle's stream and return;
+ * calls on one handle must not overlap on the GPU; one host thread at a time; pointers are device
+ * pointers that stay valid until the work has finished.  Outputs may not overlap inputs except where a
+ * call says so.  All statistics, sums and products are accumulated in binary32; each 16-bit output is rounded once
+ * from binary32.  Results of a call do not depend on timing: the same inputs give the same bits.
+ * `ld` and `stride` arguments count elements from one row (token) to the next.
+ */
+typedef struct aq_stage aq_stage;
+
+/* On the current device; NULL on failure (aq_stage_last_error(NULL), aq_stage_last_error_code(NULL)). */
+aq_stage* aq_stage_create(void);
+/* Waits for the handle's stream, frees everything the handle owns.  NULL is allowed. */
+void aq_stage_destroy(aq_stage* st);
+/* AQ_DTYPE (AQ_FP16, the default, AQ_BF16 or AQ_FP32; AQ_FP32 serves the token log probabilities only, the
+ * other calls answer AQ_EUNSUPPORTED) or AQ_STREAM. */
+int aq_stage_configure(aq_stage* st, int key, int64_t value);
+/* Synchronises the stream, returns the sticky AQ_ST_* bits in *bits_host (host) and clears them. */
+int aq_stage_status(aq_stage* st, uint32_t* bits_host);
+const char* aq_stage_last_error(aq_stage* st);
+int aq_stage_last_error_code(aq_stage* st);
+
+/*
+ * Log probabilities of given tokens, with the entropy and the top alternatives of every row.
+ *   z = scale * logits[row][0..vocab),  lse = ln sum_j e^z_j,
+ *   logprob = z_target - lse,  entropy = -sum_j p_j ln p_j  with p_j = e^(z_j - lse),
+ *   top_ids / top_logprobs: the top_k largest logits in falling order, equal ones by rising id, and z - lse of each.
+ * logits T[rows][ld] (in; only the first vocab of a row are read; any element alignment), targets int32[rows]
+ * or null (in).  logprob, entropy, lse float[rows], each may be null; top_ids int32[rows][top_k],
+ * top_logprobs float[rows][top_k] (out; either may be null).  0 <= top_k <= min(vocab, 32); scale is finite and
+ * positive; vocab < 2^31.
+ * A negative target means no token: its logprob is 0.  A target >= vocab does the same and sets AQ_ST_BAD_ID.
+ * Masked logits are -infinity or any very low value: they have probability 0 and do not touch the other
+ * outputs.  A row of nothing but -infinity has lse = logprob = top_logprobs = -infinity, entropy 0 and top_ids
+ * 0, 1, 2 ...  (as has one whose scaled values all overflow to -infinity).  A row with a NaN or a +infinity has NaN in lse,
+ * logprob and entropy; NaNs are never among the alternatives, whose missing places hold id -1.
+ */
+int aq_token_logprobs(aq_stage* st, const void* logits, int64_t rows, int64_t vocab, int64_t ld, const int32_t* targets,
+                      float scale, int top_k, float* logprob, float* entropy, float* lse, int32_t* top_ids, float* top_logprobs);
+
+/*
+ * The gradient of sum_row (d_logprob * logprob + d_entropy * entropy) with respect to the logits:
+ *   d_logits_j = scale * ( d_logprob * ([j = target] - p_j) - d_entropy * p_j * (ln p_j + entropy) ).
+ * lse and entropy float[rows] as aq_token_logprobs left them for the same logits and scale (entropy may be null when
+ * d_entropy is); targets as above (a row without a token has no d_logprob term); d_logprob, d_entropy
+ * float[rows], either may be null for none.  d_logits T[rows][ld_d] (out; the first vocab of a row are written); may be the logits
+ * themselves with the same ld.  A row whose lse is -infinity gets zeros.
+ */
+int aq_token_logprobs_grad(aq_stage* st, const void* logits, int64_t rows, int64_t vocab, int64_t ld, const int32_t* targets,
+                           float scale, const float* lse, const float* entropy, const float* d_logprob, const float* d_entropy,
+                           void* d_logits, int64_t ld_d);
+
+enum {
+  AQ_ACT_SILU = 0,        /* g / (1 + e^-g) */
+  AQ_ACT_GELU = 1,        /* g Phi(g), Phi the normal distribution function */
+  AQ_ACT_GELU_TANH = 2    /* g / 2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) */
+};
+
+/*
+ * Gated feed-forward product: both projections, the activation and the product in one kernel.
+ *   g = x wg^T,  u = x wu^T,  h = act(g) * u
+ * x T[rows][ldx], first `hidden` of a row (in); wg, wu T[inner][ldw], first `hidden` of a row (in); h T[rows][ldh], first
+ * `inner` of a row (out); g, u T[rows][ldgu] (out; both or neither may be null): what aq_gated_ffn_grad
+ * needs.  h is formed from the binary32 g and u, not from the rounded ones.  hidden and inner are
+ * multiples of 8 (AQ_EUNSUPPORTED otherwise), every ld a multiple of 8, every pointer 16-byte aligned; rows >= 0.
+ */
+int aq_gated_ffn(aq_stage* st, const void* x, int64_t ldx, const void* wg, const void* wu, int64_t ldw, int64_t rows, int hidden,
+                 int inner, int act, void* h, int64_t ldh, void* g, void* u, int64_t ldgu);
+
+/*
+ * Its gradient, from dh T[rows][lddh], the inputs, and g, u as aq_gated_ffn left them:
+ *   dg = dh * u * act'(g),  du = dh * act(g),
+ *   dx = dg wg + du wu,  dwg = dg^T x,  dwu = du^T x
+ * dx T[rows][lddx] (out; may be null), dwg, dwu T[inner][lddw] (out; both or neither may be null).  dg and du
+ * are rounded to T before the products (the tensor cores' operand type) and kept in the handle's workspace, 4 * rows * inner bytes, which
+ * grows at the first call that needs more (that call synchronises the stream and cannot be captured into a
+ * CUDA graph: AQ_EUNSUPPORTED).
+ */
+int aq_gated_ffn_grad(aq_stage* st, const void* dh, int64_t lddh, const void* x, int64_t ldx, const void* wg, const void* wu,
+                      int64_t ldw, const void* g, const void* u, int64_t ldgu, int64_t rows, int hidden, int inner, int act,
+                      void* dx, int64_t lddx, void* dwg, void* dwu, int64_t lddw);
+
+/* Heads of aq_qk_norm_rope. */
+typedef struct {
+  int32_t heads_q, heads_k;   /* >= 0; at least one of the two > 0 */
+  int32_t head_dim;           /* a multiple of 8, 8..256 */
+  int32_t rot_dim;            /* rotated leading elements of a head: even, 0..head_dim */
+  int32_t interleaved;        /* 0: pairs are (i, i + rot_dim/2); 1: pairs are (2i, 2i + 1) */
+  float eps;                  /* >= 0, finite */
+  int64_t n_positions;        /* rows of cos_sin */
+} aq_qk_shape;
+
+/*
+ * RMS norm of every query and key head and the position rotation, in one pass:
+ *   y = w * x / sqrt(mean(x^2) + eps),   pair i of the rotated elements: (a, b) -> (a cos_i - b sin_i, b cos_i + a sin_i)
+ * q T[rows][q_stride], heads_q * head_dim of a row; k likewise (in; slices of one projection's output are fine);
+ * wq, wk T[head_dim] or null for ones; cos_sin float[n_positions][rot_dim]: a position's rot_dim/2 cosines, then its sines
+ * (null when rot_dim is 0); positions int32[rows] (null when rot_dim is 0).  q_out, k_out (out) with
+ * strides of their own; they may be q and k themselves with the same strides.  A position outside the table zero-fills
+ * that token's outputs and sets AQ_ST_BAD_ID.  Strides are multiples of 8, pointers of q, k, wq, wk, cos_sin and the outputs
+ * 16-byte aligned.
+ */
+int aq_qk_norm_rope(aq_stage* st, const aq_qk_shape* shape, int64_t rows, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                    const void* wq, const void* wk, const float* cos_sin, const int32_t* positions,
+                    void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride);
+
+/*
+ * Its gradient: dq, dk T (out, strides of their own; may be dq_out and dk_out themselves with the same strides) and dwq, dwk
+ * float[head_dim] (out; summed over rows and heads; may be null) from dq_out, dk_out, the forward inputs
+ * and the same tables.  A token with a position outside the table gets zeros and adds nothing to dwq and dwk.
+ */
+int aq_qk_norm_rope_grad(aq_stage* st, const aq_qk_shape* shape, int64_t rows, const void* dq_out, int64_t dq_out_stride,
+                         const void* dk_out, int64_t dk_out_stride, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                         const void* wq, const void* wk, const float* cos_sin, const int32_t* positions,
+                         void* dq, int64_t dq_stride, void* dk, int64_t dk_stride, float* dwq, float* dwk);
 
 #ifdef __cplusplus
 }

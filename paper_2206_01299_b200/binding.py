@@ -16,9 +16,19 @@ AQ_DTYPE, AQ_BATCH, AQ_STREAM, AQ_RAW, AQ_FIRST_FLAGS, AQ_ROWS_PER_CTA = 1, 2, 3
 AQ_L2_PREFETCH = 10
 AQ_RAW_LIST = 11
 AQ_ROUNDING, AQ_SEED, AQ_EPOCH = 7, 8, 9
-AQ_FP16, AQ_BF16 = 0, 1
+AQ_FP16, AQ_BF16, AQ_FP32 = 0, 1, 2
 AQ_ROUND_INTERVAL, AQ_ROUND_STOCHASTIC = 0, 1
+AQ_ACT_SILU, AQ_ACT_GELU, AQ_ACT_GELU_TANH = 0, 1, 2
 AQ_ST_BAD_ID, AQ_ST_DUP_ID, AQ_ST_NO_RAW, AQ_ST_STAGED, AQ_ST_BAD_PTR = 1, 2, 4, 8, 16
+
+
+class QkShape(C.Structure):
+    """aq_qk_shape: the heads of aq_qk_norm_rope."""
+    _fields_ = [("heads_q", C.c_int32), ("heads_k", C.c_int32), ("head_dim", C.c_int32), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("eps", C.c_float), ("n_positions", C.c_int64)]
+
+
+_P, _I, _L, _F = C.c_void_p, C.c_int, C.c_int64, C.c_float
 
 # name -> (restype, argtypes); the load test checks these against the header
 SIGNATURES = {
@@ -51,6 +61,18 @@ SIGNATURES = {
     "aq_prefetch": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int]),
     "aq_export_sample": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
     "aq_import_sample": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_uint8]),
+    "aq_stage_create": (_P, []),
+    "aq_stage_destroy": (None, [_P]),
+    "aq_stage_configure": (_I, [_P, _I, _L]),
+    "aq_stage_status": (_I, [_P, C.POINTER(C.c_uint32)]),
+    "aq_stage_last_error": (C.c_char_p, [_P]),
+    "aq_stage_last_error_code": (_I, [_P]),
+    "aq_token_logprobs": (_I, [_P, _P, _L, _L, _L, _P, _F, _I, _P, _P, _P, _P, _P]),
+    "aq_token_logprobs_grad": (_I, [_P, _P, _L, _L, _L, _P, _F, _P, _P, _P, _P, _P, _L]),
+    "aq_gated_ffn": (_I, [_P, _P, _L, _P, _P, _L, _L, _I, _I, _I, _P, _L, _P, _P, _L]),
+    "aq_gated_ffn_grad": (_I, [_P, _P, _L, _P, _L, _P, _P, _L, _P, _P, _L, _L, _I, _I, _I, _P, _L, _P, _P, _L]),
+    "aq_qk_norm_rope": (_I, [_P, C.POINTER(QkShape), _L, _P, _L, _P, _L, _P, _P, _P, _P, _P, _L, _P, _L]),
+    "aq_qk_norm_rope_grad": (_I, [_P, C.POINTER(QkShape), _L, _P, _L, _P, _L, _P, _L, _P, _L, _P, _P, _P, _P, _P, _L, _P, _L, _P, _P]),
 }
 
 _lib = None
@@ -232,3 +254,81 @@ def aq_export_sample(h, sample_id, m_host):
 
 def aq_import_sample(h, sample_id, m_host, seen):
     return _check(h, lib().aq_import_sample(h, sample_id, _ptr(m_host), int(bool(seen))))
+
+
+# ---- stage operators: buffers are named with their row strides, so a tensor may be a slice whose rows are contiguous
+
+def _row(x):
+    """Address of a tensor whose rows (last dimension) are contiguous, of an int address, or None."""
+    if x is None or isinstance(x, int):
+        return x
+    assert x.numel() < 2 or x.stride(-1) == 1 or x.shape[-1] == 1, "rows must be contiguous"
+    return x.data_ptr()
+
+
+def _check_stage(st, rc):
+    if rc != AQ_OK:
+        raise AqError(rc, aq_stage_last_error(st))
+    return rc
+
+
+def aq_stage_create():
+    st = lib().aq_stage_create()
+    if not st:
+        raise AqError(aq_stage_last_error_code(None), aq_stage_last_error(None))
+    return st
+
+
+def aq_stage_destroy(st):
+    lib().aq_stage_destroy(st)
+
+
+def aq_stage_configure(st, key, value):
+    return _check_stage(st, lib().aq_stage_configure(st, key, value))
+
+
+def aq_stage_status(st):
+    v = C.c_uint32(0)
+    _check_stage(st, lib().aq_stage_status(st, C.byref(v)))
+    return v.value
+
+
+def aq_stage_last_error(st):
+    return lib().aq_stage_last_error(st).decode()
+
+
+def aq_stage_last_error_code(st):
+    return lib().aq_stage_last_error_code(st)
+
+
+def aq_token_logprobs(st, logits, rows, vocab, ld, targets, scale, top_k, logprob, entropy, lse, top_ids, top_logprobs):
+    return _check_stage(st, lib().aq_token_logprobs(st, _row(logits), rows, vocab, ld, _ptr(targets), scale, top_k, _ptr(logprob),
+                                                    _ptr(entropy), _ptr(lse), _ptr(top_ids), _ptr(top_logprobs)))
+
+
+def aq_token_logprobs_grad(st, logits, rows, vocab, ld, targets, scale, lse, entropy, d_logprob, d_entropy, d_logits, ld_d):
+    return _check_stage(st, lib().aq_token_logprobs_grad(st, _row(logits), rows, vocab, ld, _ptr(targets), scale, _ptr(lse),
+                                                         _ptr(entropy), _ptr(d_logprob), _ptr(d_entropy), _row(d_logits), ld_d))
+
+
+def aq_gated_ffn(st, x, ldx, wg, wu, ldw, rows, hidden, inner, act, h, ldh, g, u, ldgu):
+    return _check_stage(st, lib().aq_gated_ffn(st, _row(x), ldx, _row(wg), _row(wu), ldw, rows, hidden, inner, act, _row(h), ldh,
+                                               _row(g), _row(u), ldgu))
+
+
+def aq_gated_ffn_grad(st, dh, lddh, x, ldx, wg, wu, ldw, g, u, ldgu, rows, hidden, inner, act, dx, lddx, dwg, dwu, lddw):
+    return _check_stage(st, lib().aq_gated_ffn_grad(st, _row(dh), lddh, _row(x), ldx, _row(wg), _row(wu), ldw, _row(g), _row(u), ldgu,
+                                                    rows, hidden, inner, act, _row(dx), lddx, _row(dwg), _row(dwu), lddw))
+
+
+def aq_qk_norm_rope(st, shape, rows, q, q_stride, k, k_stride, wq, wk, cos_sin, positions, q_out, q_out_stride, k_out, k_out_stride):
+    """shape: a QkShape."""
+    return _check_stage(st, lib().aq_qk_norm_rope(st, shape, rows, _row(q), q_stride, _row(k), k_stride, _ptr(wq), _ptr(wk),
+                                                  _ptr(cos_sin), _ptr(positions), _row(q_out), q_out_stride, _row(k_out), k_out_stride))
+
+
+def aq_qk_norm_rope_grad(st, shape, rows, dq_out, dq_out_stride, dk_out, dk_out_stride, q, q_stride, k, k_stride, wq, wk, cos_sin,
+                         positions, dq, dq_stride, dk, dk_stride, dwq, dwk):
+    return _check_stage(st, lib().aq_qk_norm_rope_grad(st, shape, rows, _row(dq_out), dq_out_stride, _row(dk_out), dk_out_stride,
+                                                       _row(q), q_stride, _row(k), k_stride, _ptr(wq), _ptr(wk), _ptr(cos_sin),
+                                                       _ptr(positions), _row(dq), dq_stride, _row(dk), dk_stride, _ptr(dwq), _ptr(dwk)))

@@ -5,18 +5,21 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = [os.path.join(CSRC, f) for f in ("aq_api.cu", "aq_kernels.cu", "aq_lowbit.cu", "aq_anygroup.cu", "aq_noalloc.cu")]
-HEADERS = [os.path.join(CSRC, "aq_internal.h"), os.path.join(CSRC, "aq_device.cuh"),
+CODEC_SOURCES = [os.path.join(CSRC, f) for f in ("aq_api.cu", "aq_kernels.cu", "aq_lowbit.cu", "aq_anygroup.cu", "aq_noalloc.cu")]
+STAGE_SOURCES = [os.path.join(CSRC, f) for f in ("aq_stage_api.cu", "aq_logprob.cu", "aq_qknorm.cu", "aq_ffn.cu")]
+SOURCES = CODEC_SOURCES + STAGE_SOURCES
+HEADERS = [os.path.join(CSRC, "aq_internal.h"), os.path.join(CSRC, "aq_device.cuh"), os.path.join(CSRC, "aq_stage.h"),
            os.path.join(os.path.dirname(HERE), "include", "aq_b200.h")]
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libaq_b200.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    # bit-exact fp32: no fused multiply-add, no flush-to-zero, IEEE division
-    "-fmad=false", "-ftz=false", "-prec-div=true", "-prec-sqrt=true",
+    "-ftz=false", "-prec-div=true", "-prec-sqrt=true",
     "-Xcompiler", "-fPIC",
 ]
+# the codec is bit-exact fp32: no fused multiply-add (and no flush-to-zero, IEEE division, above)
+CODEC_FLAGS = ["-fmad=false"]
 LINK_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-cudart", "static"]
 
 
@@ -39,7 +42,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     os.makedirs(OBJ_DIR, exist_ok=True)
     objs = [os.path.join(OBJ_DIR, os.path.basename(src)[:-3] + ".o") for src in SOURCES]
     extra = ["-Xptxas", "-v"] if verbose else []
-    procs = [subprocess.Popen([nvcc()] + NVCC_FLAGS + extra + ["-c", src, "-o", obj]) for src, obj in zip(SOURCES, objs)]
+    procs = [subprocess.Popen([nvcc()] + NVCC_FLAGS + (CODEC_FLAGS if src in CODEC_SOURCES else []) + extra + ["-c", src, "-o", obj])
+             for src, obj in zip(SOURCES, objs)]
     failed = [src for src, p in zip(SOURCES, procs) if p.wait() != 0]
     if failed:
         raise subprocess.CalledProcessError(1, "nvcc -c " + " ".join(failed))
