@@ -120,8 +120,10 @@ enum {
   AQ_ST_NO_RAW = 4,      /* aq_decode met a first-visit sample while AQ_RAW was 0 */
   AQ_ST_STAGED = 8,      /* a call after aq_prefetch brought another id at some position than the one
                             prefetched for it; that sample is skipped */
-  AQ_ST_BAD_PTR = 16     /* a list-form call found a null or misaligned pointer in one of its arrays; nothing
+  AQ_ST_BAD_PTR = 16,    /* a list-form call found a null or misaligned pointer in one of its arrays; nothing
                             is read or written for that sample */
+  AQ_ST_STALLED = 32     /* stage handles: a kernel gave up on a wait that should have ended (every wait in a kernel
+                            is bounded); the outputs of that call are not valid */
 };
 
 /*

@@ -20,6 +20,7 @@ AQ_FP16, AQ_BF16, AQ_FP32 = 0, 1, 2
 AQ_ROUND_INTERVAL, AQ_ROUND_STOCHASTIC = 0, 1
 AQ_ACT_SILU, AQ_ACT_GELU, AQ_ACT_GELU_TANH = 0, 1, 2
 AQ_ST_BAD_ID, AQ_ST_DUP_ID, AQ_ST_NO_RAW, AQ_ST_STAGED, AQ_ST_BAD_PTR = 1, 2, 4, 8, 16
+AQ_ST_STALLED = 32
 
 
 class QkShape(C.Structure):

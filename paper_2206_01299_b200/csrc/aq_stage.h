@@ -61,6 +61,7 @@ struct FfnArgs {
   long long rows; int hidden, inner, act;
   void* h; long long ldh;
   void *g, *u; long long ldgu;            // may be null
+  uint32_t* status;
   int sms;
 };
 
@@ -73,6 +74,7 @@ struct FfnGradArgs {
   void* dx; long long lddx;               // may be null
   void *dwg, *dwu; long long lddw;        // may be null
   void *dg, *du;                          // T[rows][inner], workspace
+  uint32_t* status;
   int sms;
 };
 

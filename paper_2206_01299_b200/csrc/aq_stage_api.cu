@@ -247,7 +247,7 @@ int aq_gated_ffn(aq_stage* st, const void* x, int64_t ldx, const void* wg, const
     AQ_TRY(check_matrix(st, who, "u", u, ldgu, inner));
   }
   DeviceGuard guard(st->device);
-  const aq::FfnArgs a{x, ldx, wg, wu, ldw, rows, hidden, inner, act, h, ldh, g, u, ldgu, st->sms};
+  const aq::FfnArgs a{x, ldx, wg, wu, ldw, rows, hidden, inner, act, h, ldh, g, u, ldgu, st->status, st->sms};
   return launched(st, aq::launch_ffn(st->dtype, a, st->stream), who);
 }
 
@@ -282,7 +282,7 @@ int aq_gated_ffn_grad(aq_stage* st, const void* dh, int64_t lddh, const void* x,
   const size_t half = (size_t)rows * (size_t)inner * 2;
   AQ_TRY(ensure_work(st, 2 * half));
   const aq::FfnGradArgs a{dh, lddh, x, ldx, wg, wu, ldw, g, u, ldgu, rows, hidden, inner, act, dx, lddx, dwg, dwu, lddw,
-                          st->work, static_cast<char*>(st->work) + half, st->sms};
+                          st->work, static_cast<char*>(st->work) + half, st->status, st->sms};
   return launched(st, aq::launch_ffn_grad(st->dtype, a, st->stream), who);
 }
 

@@ -36,7 +36,7 @@ def test_constants_of_the_stage_operators():
     import os
     import re
     text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "aq_b200.h")).read()
-    for name in ("AQ_FP32", "AQ_ACT_SILU", "AQ_ACT_GELU", "AQ_ACT_GELU_TANH"):
+    for name in ("AQ_FP32", "AQ_ACT_SILU", "AQ_ACT_GELU", "AQ_ACT_GELU_TANH", "AQ_ST_STALLED"):
         assert getattr(aq, name) == int(re.search(rf"\b{name}\s*=\s*(\d+)", text).group(1))
     # int32 x 5, float, int64: no padding
     assert ctypes.sizeof(aq.QkShape) == 32 and aq.QkShape.n_positions.offset == 24
