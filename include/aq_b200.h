@@ -455,9 +455,9 @@ int aq_gated_ffn(aq_stage* st, const void* x, int64_t ldx, const void* wg, const
  *   dg = dh * u * act'(g),  du = dh * act(g),
  *   dx = dg wg + du wu,  dwg = dg^T x,  dwu = du^T x
  * dx T[rows][lddx] (out; may be null), dwg, dwu T[inner][lddw] (out; both or neither may be null).  dg and du
- * are rounded to T before the products (the tensor cores' operand type) and kept in the handle's workspace, 4 * rows * inner bytes, which
- * grows at the first call that needs more (that call synchronises the stream and cannot be captured into a
- * CUDA graph: AQ_EUNSUPPORTED).
+ * are rounded to T before the products (the tensor cores' operand type) and kept in the handle's workspace: 4 * rows * inner bytes,
+ * and for few rows up to 256 MB for parts of dx.  It grows at the first call that needs more (that call synchronises the
+ * stream and cannot be captured into a CUDA graph: AQ_EUNSUPPORTED).
  */
 int aq_gated_ffn_grad(aq_stage* st, const void* dh, int64_t lddh, const void* x, int64_t ldx, const void* wg, const void* wu,
                       int64_t ldw, const void* g, const void* u, int64_t ldgu, int64_t rows, int hidden, int inner, int act,

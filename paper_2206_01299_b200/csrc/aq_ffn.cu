@@ -26,20 +26,39 @@ template <typename T> struct Num;
 template <> struct Num<__half> {
   static constexpr CUtensorMapDataType kMap = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   static constexpr uint32_t kFormat = 0;
+  static __device__ __half one(float x) { return __float2half_rn(x); }
   static __device__ float2 open(uint32_t u) { return __half22float2(*reinterpret_cast<__half2*>(&u)); }
   static __device__ uint32_t close(float a, float b) { const __half2 p = __floats2half2_rn(a, b); return *reinterpret_cast<const uint32_t*>(&p); }
 };
 template <> struct Num<__nv_bfloat16> {
   static constexpr CUtensorMapDataType kMap = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   static constexpr uint32_t kFormat = 1;
+  static __device__ __nv_bfloat16 one(float x) { return __float2bfloat16_rn(x); }
   static __device__ float2 open(uint32_t u) { return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)); }
   static __device__ uint32_t close(float a, float b) { const __nv_bfloat162 p = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t*>(&p); }
 };
 
+// Phi(-|g|), the normal distribution's tail: e^(-g^2/2) times a polynomial in t = 1 / (1 + 0.375 |g| / sqrt(2)), fitted to
+// erfc(x) e^(x^2) / 2 over x = 0..12 by reweighted least squares (relative error 2.5e-8; 4e-7 as evaluated here).
+// Against erfcf: the forward kernel's epilogue at 256 x 128 outputs a tile 15000 cycles with erfcf.
+__device__ float normal_tail(float g) {
+  const float x = fabsf(g), t = __fdividef(1.0f, fmaf(x, 0.2651650429f, 1.0f));
+  float p = 0.029775582253932953f;
+  p = fmaf(p, t, -0.13898201286792755f);
+  p = fmaf(p, t, 0.2068338394165039f);
+  p = fmaf(p, t, -0.10435142368078232f);
+  p = fmaf(p, t, 0.12995630502700806f);
+  p = fmaf(p, t, 0.06359007209539413f);
+  p = fmaf(p, t, 0.10195682942867279f);
+  p = fmaf(p, t, 0.10541940480470657f);
+  p = fmaf(p, t, 0.10580138117074966f);
+  return p * t * __expf(-0.5f * g * g);
+}
+
 // act(g) and act'(g)
 template <int ACT> __device__ void activation(float g, float* a, float* da) {
   if (ACT == AQ_ACT_GELU) {
-    const float cdf = 0.5f * erfcf(-0.70710678f * g);
+    const float tail = normal_tail(g), cdf = g < 0.0f ? tail : 1.0f - tail;
     *a = g * cdf;
     *da = fmaf(g * 0.3989422804f, __expf(-0.5f * g * g), cdf);
     return;
@@ -49,8 +68,8 @@ template <int ACT> __device__ void activation(float g, float* a, float* da) {
   const float dy = ACT == AQ_ACT_SILU ? 1.0f : 1.5957691216f * fmaf(3.0f * 0.044715f * g, g, 1.0f);
   const float sig = __fdividef(1.0f, 1.0f + __expf(-y));
   *a = g * sig;
-  // sig (1 - sig) is 0 long before the cubic's derivative could overflow
-  *da = fmaf(g * (sig * (1.0f - sig)), dy, sig);
+  const float bend = g * (sig * (1.0f - sig));                  // 0 long before the cubic's derivative overflows
+  *da = bend == 0.0f ? sig : fmaf(bend, dy, sig);
 }
 
 // ---- instructions ------------------------------------------------------------------------------------------------
@@ -85,6 +104,10 @@ __device__ bool barrier_wait(uint32_t bar, uint32_t parity, uint32_t* status) {
     if (barrier_try(bar, parity)) return true;
   return barrier_wait_long(bar, parity, status);
 }
+__device__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+// programmatic launch: the next kernel of the stream may be placed; the results of the previous one are needed from here
+__device__ void next_may_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // a box of this GPU's memory into this CTA's shared memory, counted by the first CTA's barrier
 __device__ void load_box(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
@@ -143,42 +166,63 @@ constexpr int kColumns = 512;                 // tensor memory: two tiles' sums 
 constexpr int kSharedBytes = 1024 + kStages * 2 * kHalfTile + kEpilogueWarps * kOutBuffers * kOutBytes;
 constexpr int kMaxPairs = 128;
 
+constexpr int kClasses = 4;                   // kinds of tiles of one launch: dx and dW, each with full and last columns
+
+// Tiles that take the same time: `columns` wide from column tile `first`, `count` of them, in each of m_tiles rows of tiles,
+// `parts` times over (forward and dx: parts of the depth; dW: dWg and dWu).
+struct TileClass {
+  int problem, m_tiles, first, count, columns, parts, k_blocks;
+};
+
 struct Products {
-  CUtensorMap a[2], b[2];                     // first problem
+  CUtensorMap a[2], b[2];                     // forward and dx
   CUtensorMap a2[2], b2;                      // dW: dg and du across their rows, x
   CUtensorMap out[3];                         // forward: h, g, u; backward: dx, dWg, dWu
-  int m_tiles[2], n_tiles[2];                 // of the first problem and of dW
-  int k_blocks[2];                            // stages per tile
-  int n[2];                                   // columns of a tile (both halves of the pair)
+  int n;                                      // columns of a tile (both halves of the pair)
+  int k_total;                                // stages of the whole depth of forward and dx
   int rows[2], cols[2];                       // of the outputs
   int save;                                   // forward: write g and u
-  uint32_t first[2][kMaxPairs + 1];           // backward: the tiles of each problem that a pair works on
+  float* partial;                             // dx in parts: float[parts][rows][cols], else null
+  TileClass cls[kClasses];                    // the longest tiles first
+  uint32_t first[kClasses][kMaxPairs + 1];    // the tiles of each class that a pair works on; forward: pair, pair + pairs, ...
   uint32_t format;
   uint32_t* status;
 };
 
 struct Tile {
-  int problem, z, m0, n0;
+  int problem, part, m0, n0, columns, k0, k_blocks;
 };
+
+__device__ void place(const Products& p, const TileClass& c, unsigned at, Tile* t) {
+  const unsigned n = at % (unsigned)c.count, rest = at / (unsigned)c.count;
+  t->problem = c.problem;
+  t->part = (int)(rest / (unsigned)c.m_tiles);
+  t->m0 = (int)(rest % (unsigned)c.m_tiles) * 256;
+  t->n0 = (c.first + (int)n) * p.n;
+  t->columns = c.columns;
+  t->k0 = c.problem == 0 ? t->part * c.k_blocks : 0;
+  t->k_blocks = c.problem == 0 ? min(c.k_blocks, p.k_total - t->k0) : c.k_blocks;
+}
 
 template <bool BACKWARD>
 __device__ bool tile_at(const Products& p, unsigned pair, unsigned pairs, unsigned i, Tile* t) {
   if constexpr (!BACKWARD) {
+    // rows of tiles fastest: the pairs at work share their columns' weights
+    const TileClass& c = p.cls[0];
     const unsigned at = pair + i * pairs;
-    if (at >= (unsigned)p.m_tiles[0] * (unsigned)p.n_tiles[0]) return false;
-    *t = {0, 0, (int)(at % (unsigned)p.m_tiles[0]) * 256, (int)(at / (unsigned)p.m_tiles[0]) * (p.n[0] / 2)};
+    if (at >= (unsigned)c.m_tiles * (unsigned)c.count) return false;
+    *t = {0, 0, (int)(at % (unsigned)c.m_tiles) * 256, (int)(at / (unsigned)c.m_tiles) * (c.columns / 2), c.columns, 0, c.k_blocks};
     return true;
   } else {
-    unsigned at = p.first[0][pair] + i;
-    if (at < p.first[0][pair + 1]) {
-      *t = {0, 0, (int)(at / (unsigned)p.n_tiles[0]) * 256, (int)(at % (unsigned)p.n_tiles[0]) * p.n[0]};
-      return true;
+    for (int k = 0; k < kClasses; ++k) {
+      const unsigned from = p.first[k][pair], n = p.first[k][pair + 1] - from;
+      if (i < n) {
+        place(p, p.cls[k], from + i, t);
+        return true;
+      }
+      i -= n;
     }
-    at = p.first[1][pair] + (at - p.first[0][pair + 1]);
-    if (at >= p.first[1][pair + 1]) return false;
-    const unsigned per = (unsigned)p.m_tiles[1] * (unsigned)p.n_tiles[1], in = at % per;
-    *t = {1, (int)(at / per), (int)(in / (unsigned)p.n_tiles[1]) * 256, (int)(in % (unsigned)p.n_tiles[1]) * p.n[1]};
-    return true;
+    return false;
   }
 }
 
@@ -203,6 +247,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
   auto sums_full = [&](int s) { return bars + 8u * (2 * kStages + s); };
   auto sums_empty = [&](int s) { return bars + 8u * (2 * kStages + 2 + s); };
 
+  if (warp == 3 && lane == 0) {               // fetch the maps that every tile begins with
+    prefetch_map(&p.a[0]); prefetch_map(&p.b[0]); prefetch_map(&p.b[1]);
+  }
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { barrier_init(full(s), 1); barrier_init(empty(s), 1); }
     for (int s = 0; s < 2; ++s) { barrier_init(sums_full(s), 1); barrier_init(sums_empty(s), 2 * kEpilogueWarps); }
@@ -217,6 +264,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
   pair_sync();                                // the barriers of both CTAs exist before either signals the other's
   fence_after();
   const uint32_t tensor = tensor_base;
+  next_may_launch();
+  wait_for_previous();
 
   if (warp == 0) {
     if (lane == 0) {
@@ -225,10 +274,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
       bool going = true;
       Tile t;
       for (unsigned i = 0; going && tile_at<BACKWARD>(p, pair, pairs, i, &t); ++i) {
-        const int half_n = p.n[t.problem] / 2, kb = p.k_blocks[t.problem];
+        const int half_n = t.columns / 2;
         const int b_boxes = BACKWARD ? (half_n + 63) / 64 : 0;
         const uint32_t bytes = kHalfTile + (BACKWARD ? (uint32_t)b_boxes * 8192u : (uint32_t)half_n * 128u);
-        for (int k = 0; k < kb; ++k) {
+        for (int i_k = 0; i_k < t.k_blocks; ++i_k) {
+          const int k = t.k0 + i_k;
           if (!barrier_wait(empty(stage), phase ^ 1, p.status)) { going = false; break; }
           const uint32_t bar = in_first_cta(full(stage));
           if (rank == 0) barrier_expect(full(stage), 2 * bytes);
@@ -237,13 +287,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
             load_box(to_a, &p.a[0], k * kDeep, t.m0 + (int)rank * 128, bar);
             load_box(to_b, &p.b[rank], k * kDeep, t.n0, bar);
           } else if (t.problem == 0) {
-            const int z = 2 * k >= kb, k0 = (z ? k - kb / 2 : k) * kDeep;
+            const int z = 2 * k >= p.k_total, k0 = (z ? k - p.k_total / 2 : k) * kDeep;
             load_box(to_a, &p.a[z], k0, t.m0 + (int)rank * 128, bar);
             load_box(to_a + 8192, &p.a[z], k0, t.m0 + (int)rank * 128 + 64, bar);
             for (int j = 0; j < b_boxes; ++j) load_box(to_b + j * 8192, &p.b[z], t.n0 + (int)rank * half_n + j * 64, k0, bar);
           } else {
-            load_box(to_a, &p.a2[t.z], t.m0 + (int)rank * 128, k * kDeep, bar);
-            load_box(to_a + 8192, &p.a2[t.z], t.m0 + (int)rank * 128 + 64, k * kDeep, bar);
+            load_box(to_a, &p.a2[t.part], t.m0 + (int)rank * 128, k * kDeep, bar);
+            load_box(to_a + 8192, &p.a2[t.part], t.m0 + (int)rank * 128 + 64, k * kDeep, bar);
             for (int j = 0; j < b_boxes; ++j) load_box(to_b + j * 8192, &p.b2, t.n0 + (int)rank * half_n + j * 64, k * kDeep, bar);
           }
           if (++stage == kStages) { stage = 0; phase ^= 1; }
@@ -265,14 +315,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
         const bool a_across = BACKWARD && t.problem == 1, b_across = BACKWARD;
         // binary32 sums (bit 4), operand types, which operands run across, N / 8, M / 16
         const uint32_t what = (1u << 4) | (p.format << 7) | (p.format << 10) | ((uint32_t)a_across << 15) | ((uint32_t)b_across << 16) |
-                              ((uint32_t)(p.n[t.problem] >> 3) << 17) | (16u << 24);
+                              ((uint32_t)(t.columns >> 3) << 17) | (16u << 24);
         // 16 deep: 32 bytes along a row, or sixteen rows
         const uint32_t step_a = a_across ? 2048 >> 4 : 32 >> 4, step_b = b_across ? 2048 >> 4 : 32 >> 4;
         if (!barrier_wait(sums_empty(acc), acc_phase ^ 1, p.status)) break;
         fence_after();
         const uint32_t sums = tensor + (uint32_t)acc * 256u;
-        const int kb = p.k_blocks[t.problem];
-        for (int k = 0; k < kb; ++k) {
+        for (int k = 0; k < t.k_blocks; ++k) {
           if (!barrier_wait(full(stage), phase, p.status)) { going = false; break; }
           fence_after();
           const uint32_t at = base + (uint32_t)stage * 2 * kHalfTile;
@@ -315,7 +364,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
       if (!barrier_wait(sums_full(acc), acc_phase, p.status)) break;
       fence_after();
       const uint32_t sums = tensor + (uint32_t)acc * 256u + ((uint32_t)quarter << 21);
-      const int width = BACKWARD ? p.n[t.problem] : p.n[0] / 2;
+      const int width = BACKWARD ? t.columns : t.columns / 2;
       const int y = t.m0 + (int)rank * 128 + quarter * 32;
       const bool rows_there = y < p.rows[t.problem];
       for (int c = turn * kChunk; c < width; c += 2 * kChunk) {
@@ -332,9 +381,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
         if (!rows_there || t.n0 + c >= p.cols[t.problem]) continue;
         float v[32];
         if constexpr (BACKWARD) {
+          if (t.problem == 0 && p.partial) {
+            const int row = y + lane;
+            float* const to = p.partial + ((long long)t.part * p.rows[0] + row) * p.cols[0] + t.n0 + c;
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+              if (row < p.rows[0] && t.n0 + c + j < p.cols[0])
+                *reinterpret_cast<float4*>(to + j) = make_float4(__uint_as_float(r[j]), __uint_as_float(r[j + 1]), __uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
+            continue;
+          }
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
-          store(&p.out[t.problem + t.z], v, t.n0 + c, y);
+          store(&p.out[t.problem ? 1 + t.part : 0], v, t.n0 + c, y);
         } else {
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
@@ -371,6 +429,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
 // dg and du to the workspace, eight elements per thread
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256) ffn_dgu_kernel(const FfnGradArgs a) {
+  next_may_launch();
+  wait_for_previous();
   const unsigned per_row = (unsigned)a.inner / 8;
   const unsigned long long n = (unsigned long long)a.rows * per_row;
   for (unsigned long long i = (unsigned long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (unsigned long long)gridDim.x * 256) {
@@ -392,6 +452,122 @@ __global__ void __launch_bounds__(256) ffn_dgu_kernel(const FfnGradArgs a) {
     }
     reinterpret_cast<uint4*>(a.dg)[i] = make_uint4(og[0], og[1], og[2], og[3]);
     reinterpret_cast<uint4*>(a.du)[i] = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+  }
+}
+
+// dx = the sum of its parts, in their order
+template <typename T>
+__global__ void __launch_bounds__(256) ffn_join_kernel(const float* part, int parts, long long rows, int cols, T* out, long long ld) {
+  next_may_launch();
+  wait_for_previous();
+  const unsigned per_row = (unsigned)cols / 8;
+  const unsigned long long n = (unsigned long long)rows * per_row, i = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const unsigned long long r = i / per_row;
+  const unsigned c = (unsigned)(i - r * per_row) * 8;
+  const float4* from = reinterpret_cast<const float4*>(part + r * (unsigned)cols + c);
+  const unsigned long long next = (unsigned long long)rows * (unsigned)cols / 4;
+  float4 a = __ldcs(from), b = __ldcs(from + 1);
+#pragma unroll 4
+  for (int p = 1; p < parts; ++p) {
+    from += next;
+    const float4 c4 = __ldcs(from), d4 = __ldcs(from + 1);
+    a.x += c4.x; a.y += c4.y; a.z += c4.z; a.w += c4.w;
+    b.x += d4.x; b.y += d4.y; b.z += d4.z; b.w += d4.w;
+  }
+  *reinterpret_cast<uint4*>(out + r * ld + c) = make_uint4(Num<T>::close(a.x, a.y), Num<T>::close(a.z, a.w), Num<T>::close(b.x, b.y), Num<T>::close(b.z, b.w));
+}
+
+// ---- forward for few rows ---------------------------------------------------------------------------------------
+//
+// Bound by the weights, 4 * inner * hidden bytes, which every token shares: a CTA takes sixteen rows of Wg and Wu, its eight
+// warps share their depth, and all of the loads are in flight at once (no staging).  The products are warp-level 16 x 8 x 16
+// ones: rows 0..7 of the sixteen are Wg's, rows 8..15 Wu's of the same outputs, columns are tokens.  Which place of the depth a
+// lane's element takes does not matter as long as weights and tokens agree, so each lane loads 16 contiguous bytes of a row
+// and uses them for two products of depth 16.
+
+constexpr int kRowsThreads = 256, kRowsWarps = 8, kRowsAhead = 4;
+constexpr int kFewRows = 32;
+
+__device__ void multiply_warp(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, __half) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ void multiply_warp(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, __nv_bfloat16) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <typename T, int ACT, int TOKENS8>
+__global__ void __launch_bounds__(kRowsThreads) ffn_rows_kernel(const FfnArgs a) {
+  __shared__ float4 sums[kRowsWarps][2 * TOKENS8][32];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const int f0 = blockIdx.x * 16;
+  const int rows = (int)a.rows;
+  const bool there[2] = {true, f0 + 8 < a.inner};            // inner is a multiple of 8
+  const T* const wg = static_cast<const T*>(a.wg) + (long long)(f0 + g) * a.ldw;
+  const T* const wu = static_cast<const T*>(a.wu) + (long long)(f0 + g) * a.ldw;
+  const T* const x = static_cast<const T*>(a.x);
+  float c[2][TOKENS8][4] = {};
+  next_may_launch();
+  wait_for_previous();
+  const int steps = (a.hidden + 31) / 32;
+  for (int s0 = warp; s0 < steps; s0 += kRowsWarps * kRowsAhead) {
+    uint4 vg[kRowsAhead][2], vu[kRowsAhead][2];
+#pragma unroll
+    for (int i = 0; i < kRowsAhead; ++i) {
+      const int k = (s0 + i * kRowsWarps) * 32 + q * 8;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bool in = k < a.hidden && there[t];
+        vg[i][t] = in ? __ldcs(reinterpret_cast<const uint4*>(wg + t * 8 * a.ldw + k)) : make_uint4(0, 0, 0, 0);
+        vu[i][t] = in ? __ldcs(reinterpret_cast<const uint4*>(wu + t * 8 * a.ldw + k)) : make_uint4(0, 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kRowsAhead; ++i) {
+      const int k = (s0 + i * kRowsWarps) * 32 + q * 8;
+#pragma unroll
+      for (int n = 0; n < TOKENS8; ++n) {
+        const int token = n * 8 + g;
+        const uint4 v = k < a.hidden && token < rows ? __ldg(reinterpret_cast<const uint4*>(x + token * a.ldx + k)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          multiply_warp(c[t][n], vg[i][t].x, vu[i][t].x, vg[i][t].y, vu[i][t].y, v.x, v.y, T());
+          multiply_warp(c[t][n], vg[i][t].z, vu[i][t].z, vg[i][t].w, vu[i][t].w, v.z, v.w, T());
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int n = 0; n < TOKENS8; ++n) sums[warp][t * TOKENS8 + n][lane] = make_float4(c[t][n][0], c[t][n][1], c[t][n][2], c[t][n][3]);
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * TOKENS8 * 32; i += kRowsThreads) {
+    const int l = i & 31, t = (i >> 5) / TOKENS8, n = (i >> 5) % TOKENS8;
+    float4 v = sums[0][i >> 5][l];
+#pragma unroll
+    for (int w = 1; w < kRowsWarps; ++w) {
+      const float4 o = sums[w][i >> 5][l];
+      v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+    }
+    const int f = f0 + t * 8 + (l >> 2), token = n * 8 + (l & 3) * 2;
+    if (f >= a.inner) continue;
+    const float gate[2] = {v.x, v.y}, up[2] = {v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (token + j >= rows) break;
+      float act, dact;
+      activation<ACT>(gate[j], &act, &dact);
+      static_cast<T*>(a.h)[(token + j) * a.ldh + f] = Num<T>::one(act * up[j]);
+      if (a.g) {
+        static_cast<T*>(a.g)[(token + j) * a.ldgu + f] = Num<T>::one(gate[j]);
+        static_cast<T*>(a.u)[(token + j) * a.ldgu + f] = Num<T>::one(up[j]);
+      }
+    }
   }
 }
 
@@ -432,31 +608,78 @@ struct Maps {
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-// The rounds of a grid of `tiles` on `pairs`, each of `kb` stages of n columns: a stage's products take 2 n cycles, an
-// epilogue that nothing hides (the last one) about 16 n, filling and draining the pipeline about 1500.
-long long cost(long long tiles, int pairs, int kb, int n) { return ((tiles + pairs - 1) / pairs) * (long long)kb * 2 * n + 16 * n + 1500; }
+// Cycles of a stage of a tile of n columns: its products take 2 n, and its operands, 16384 + 64 n bytes to each
+// multiprocessor, 64 bytes a cycle at most.
+long long stage_cycles(int n) { return 2 * n > 256 + n ? 2 * n : 256 + n; }
 
-template <typename Kernel>
-cudaError_t launch(Kernel kernel, const Products& p, int pairs, cudaStream_t s) {
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
+// Pairs that are on the GPU at the same time: the parts of the chip with an odd number of multiprocessors hold one CTA less.
+// A grid with more would run its last pairs after all others had finished their share.
+cudaError_t resident_pairs(int* pairs) {
+  auto kernel = products_kernel<__half, AQ_ACT_SILU, true>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
   if (e != cudaSuccess) return e;
-  kernel<<<2 * pairs, kFfnThreads, kSharedBytes, s>>>(p);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(2 * kMaxPairs);
+  cfg.blockDim = dim3(kFfnThreads);
+  cfg.dynamicSmemBytes = kSharedBytes;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = 2;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  e = cudaOccupancyMaxActiveClusters(pairs, kernel, &cfg);
+  if (e == cudaSuccess && *pairs < 1) e = cudaErrorInvalidConfiguration;
+  if (*pairs > kMaxPairs) *pairs = kMaxPairs;
+  return e;
 }
 
-template <typename T>
+// A launch that may be placed while the stream's previous kernel drains (the kernels wait for its results themselves).
+template <typename... Params, typename... Args>
+cudaError_t launch(void (*kernel)(Params...), unsigned ctas, unsigned threads, size_t shared, cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = shared;
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <typename T, int ACT, bool BACKWARD>
+cudaError_t launch_products(const Products& p, int pairs, cudaStream_t s) {
+  auto kernel = products_kernel<T, ACT, BACKWARD>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
+  return e != cudaSuccess ? e : launch(kernel, 2u * pairs, kFfnThreads, kSharedBytes, s, p);
+}
+
+template <typename T, int ACT>
+cudaError_t run_rows(const FfnArgs& a, cudaStream_t s) {
+  const unsigned ctas = (unsigned)ceil_div(a.inner, 16);
+  if (a.rows <= 8) return launch(ffn_rows_kernel<T, ACT, 1>, ctas, kRowsThreads, 0, s, a);
+  if (a.rows <= 16) return launch(ffn_rows_kernel<T, ACT, 2>, ctas, kRowsThreads, 0, s, a);
+  return launch(ffn_rows_kernel<T, ACT, 4>, ctas, kRowsThreads, 0, s, a);
+}
+
+template <typename T, int ACT>
 cudaError_t run(const FfnArgs& a, cudaStream_t s) {
-  const int pairs = a.sms / 2 < kMaxPairs ? a.sms / 2 : kMaxPairs;
+  if (a.rows <= kFewRows) return run_rows<T, ACT>(a, s);
   Products p{};
-  p.m_tiles[0] = ceil_div(a.rows, 256);
-  p.k_blocks[0] = ceil_div(a.hidden, kDeep);
+  const int m_tiles = ceil_div(a.rows, 256), kb = ceil_div(a.hidden, kDeep);
   int best = 0;
+  long long least = 0;
   for (int f = 128; f >= 32; f -= 32) {
-    const long long c = cost((long long)p.m_tiles[0] * ceil_div(a.inner, f), pairs, p.k_blocks[0], 2 * f);
-    if (!best || c < cost((long long)p.m_tiles[0] * ceil_div(a.inner, best), pairs, p.k_blocks[0], 2 * best)) best = f;
+    // rounds of the grid, the last one's epilogue, and about 1500 cycles to fill and drain the pipeline
+    const long long tiles = (long long)m_tiles * ceil_div(a.inner, f), c = ((tiles + a.pairs - 1) / a.pairs) * kb * stage_cycles(2 * f) + 32 * f + 1500;
+    if (!best || c < least) { best = f; least = c; }
   }
-  p.n[0] = 2 * best;
-  p.n_tiles[0] = ceil_div(a.inner, best);
+  p.n = 2 * best;
+  p.cls[0] = {0, m_tiles, 0, ceil_div(a.inner, best), 2 * best, 1, kb};
+  p.k_total = kb;
   p.rows[0] = (int)a.rows;
   p.cols[0] = a.inner;
   p.save = a.g != nullptr;
@@ -472,78 +695,145 @@ cudaError_t run(const FfnArgs& a, cudaStream_t s) {
     maps.set<T>(&p.out[2], a.u, a.rows, a.inner, a.ldgu, kChunk, 32);
   }
   if (maps.error != cudaSuccess) return maps.error;
-  const long long tiles = (long long)p.m_tiles[0] * p.n_tiles[0];
-  const int used = tiles < pairs ? (int)tiles : pairs;
-  if (a.act == AQ_ACT_SILU) return launch(products_kernel<T, AQ_ACT_SILU, false>, p, used, s);
-  if (a.act == AQ_ACT_GELU) return launch(products_kernel<T, AQ_ACT_GELU, false>, p, used, s);
-  return launch(products_kernel<T, AQ_ACT_GELU_TANH, false>, p, used, s);
+  const long long tiles = (long long)m_tiles * p.cls[0].count;
+  return launch_products<T, ACT, false>(p, tiles < a.pairs ? (int)tiles : a.pairs, s);
 }
 
-// Tiles of two problems, of different lengths, over the pairs: the first problem's evenly, then the second's one round at
-// a time to whichever pairs (those with a tile more of the first, or those with one less) are less loaded.
-void share(Products* p, long long tiles0, long long tiles1, int pairs) {
-  const long long c0 = (long long)p->k_blocks[0] * p->n[0], c1 = (long long)p->k_blocks[1] * p->n[1];
-  const int more = (int)(tiles0 % pairs);                        // pairs 0..more-1 have one more
-  const long long base = tiles0 / pairs;
-  long long load[2] = {(base + 1) * c0, base * c0}, count[2] = {more, pairs - more}, got[2] = {0, 0}, rest[2] = {0, 0}, left = tiles1;
-  while (left > 0) {
-    const int to = count[0] && (!count[1] || load[0] + c1 <= load[1] + c1) && load[0] <= load[1] ? 0 : count[1] ? 1 : 0;
-    if (left >= count[to]) {
-      ++got[to];
-      left -= count[to];
-      load[to] += c1;
-    } else {
-      rest[to] = left;
-      left = 0;
+// ---- the gradient's plan
+
+constexpr int kMaxRuns = 1 + 2 * kClasses;    // only one run is split in three by a class
+constexpr long long kMostPartialBytes = 256ll << 20;
+
+struct Plan {
+  int n = 256, parts = 1;
+  long long cycles = -1;
+};
+
+// The classes of tiles of a plan, the longest first; their number.
+int classes_of(const Plan& plan, long long rows, int hidden, int inner, bool dx, bool dw, TileClass* out) {
+  const int n = plan.n, full = hidden / n, rest = hidden - full * n, last = (rest + 31) / 32 * 32;
+  const int kb0 = 2 * ceil_div(inner, kDeep), kb1 = ceil_div(rows, kDeep);
+  const int part = ceil_div(kb0, plan.parts);
+  int c = 0;
+  auto add = [&](int problem, int first, int count, int columns) {
+    if (!count) return;
+    out[c++] = problem == 0 ? TileClass{0, ceil_div(rows, 256), first, count, columns, ceil_div(kb0, part), part}
+                            : TileClass{1, ceil_div(inner, 256), first, count, columns, 2, kb1};
+  };
+  if (dx) { add(0, 0, full, n); add(0, full, rest > 0, last); }
+  if (dw) { add(1, 0, full, n); add(1, full, rest > 0, last); }
+  for (int i = 1; i < c; ++i)
+    for (int j = i; j > 0 && out[j].k_blocks * stage_cycles(out[j].columns) > out[j - 1].k_blocks * stage_cycles(out[j - 1].columns); --j) {
+      const TileClass t = out[j];
+      out[j] = out[j - 1];
+      out[j - 1] = t;
+    }
+  return c;
+}
+
+long long tiles_of(const TileClass& c) { return (long long)c.m_tiles * c.count * c.parts; }
+// of one tile: its stages and what starting the next one costs
+long long cycles_of(const TileClass& c) { return (long long)c.k_blocks * stage_cycles(c.columns) + 200; }
+
+// Widths and parts by an estimate of the longest load.  Parts of dx's depth, 2 * inner, serve few rows, whose dx is a
+// handful of very long tiles; joining them is another kernel of about 5000 cycles that moves 8 bytes a value and part, some
+// 3500 a cycle.
+Plan plan_of(const FfnGradArgs& a) {
+  Plan best;
+  const int kb0 = 2 * ceil_div(a.inner, kDeep);
+  for (int parts = 1; parts <= 32 && parts <= kb0; parts *= 2) {
+    if (parts > 1 && (!a.dx || (long long)parts * a.rows * a.hidden * 4 > kMostPartialBytes)) break;
+    for (int n = 256; n >= 64; n -= 32) {
+      Plan plan;
+      plan.n = n;
+      plan.parts = parts;
+      TileClass cls[kClasses];
+      const int count = classes_of(plan, a.rows, a.hidden, a.inner, a.dx != nullptr, a.dwg != nullptr, cls);
+      long long work = 0, tiles = 0;
+      for (int c = 0; c < count; ++c) { work += tiles_of(cls[c]) * cycles_of(cls[c]); tiles += tiles_of(cls[c]); }
+      // dealt longest first, the loads end within about half of the shortest tile of one another
+      plan.cycles = tiles <= a.pairs ? 0 : work / a.pairs + cycles_of(cls[count - 1]) / 2;
+      if (plan.cycles < cycles_of(cls[0])) plan.cycles = cycles_of(cls[0]);
+      plan.cycles += 16 * n + (parts > 1 ? 5000 + (long long)parts * a.rows * a.hidden * 8 / 3500 : 0);
+      if (best.cycles < 0 || plan.cycles < best.cycles) best = plan;
     }
   }
-  uint32_t at0 = 0, at1 = 0;
-  for (int i = 0; i < pairs; ++i) {
-    const int cls = i < more ? 0 : 1, in = i < more ? i : i - more;
-    p->first[0][i] = at0;
-    p->first[1][i] = at1;
-    at0 += (uint32_t)(base + (cls == 0));
-    at1 += (uint32_t)(got[cls] + (in < rest[cls]));
+  return best;
+}
+
+// Neighbouring pairs with the same load.
+struct Run {
+  long long load;
+  int pairs;
+};
+
+// Deals a class of tiles: to whichever pairs have the least to do, until all are dealt.  The pairs of a run differ at most
+// where the last tiles run out, so there are few runs whatever the number of pairs.  first[i] is set to the first tile of pair i.
+int deal(long long tiles, long long cost, Run* runs, int n_runs, uint32_t* first) {
+  auto fits = [&](long long level) {                          // tiles that end at or before the level
+    long long n = 0;
+    for (int i = 0; i < n_runs; ++i) if (runs[i].load < level) n += (level - runs[i].load) / cost * runs[i].pairs;
+    return n;
+  };
+  long long low = runs[0].load, high = runs[0].load, pairs = 0;
+  for (int i = 0; i < n_runs; ++i) {
+    if (runs[i].load < low) low = runs[i].load;
+    if (runs[i].load > high) high = runs[i].load;
+    pairs += runs[i].pairs;
   }
-  p->first[0][pairs] = at0;
-  p->first[1][pairs] = at1;
+  high += cost * (tiles / pairs + 1);
+  while (high - low > 1) {                                    // the lowest level that holds them all
+    const long long mid = low + (high - low) / 2;
+    if (fits(mid) >= tiles) high = mid;
+    else low = mid;
+  }
+  Run now[kMaxRuns];
+  int n_now = 0, pair = 0;
+  long long at = 0;
+  auto give = [&](long long load, int count, long long each) {
+    for (int i = 0; i < count; ++i, ++pair, at += each) first[pair] = (uint32_t)at;
+    if (count) now[n_now++] = {load + each * cost, count};
+  };
+  for (int i = 0; i < n_runs; ++i) {
+    const long long left = tiles - at, each = left && runs[i].load < high ? (high - runs[i].load) / cost : 0;
+    const int whole = each && each * runs[i].pairs > left ? (int)(left / each) : runs[i].pairs;
+    give(runs[i].load, whole, each);
+    if (whole < runs[i].pairs) {
+      give(runs[i].load, 1, tiles - at);
+      give(runs[i].load, runs[i].pairs - whole - 1, 0);
+    }
+  }
+  first[pair] = (uint32_t)at;
+  for (int i = 0; i < n_now; ++i) runs[i] = now[i];
+  return n_now;
 }
 
 template <typename T>
 cudaError_t run_grad(const FfnGradArgs& a, cudaStream_t s) {
   const long long vectors = a.rows * (a.inner / 8), want = (vectors + 255) / 256, most = 16ll * a.sms;
   const unsigned ctas = (unsigned)(want < most ? want : most);
-  if (a.act == AQ_ACT_SILU) ffn_dgu_kernel<T, AQ_ACT_SILU><<<ctas, 256, 0, s>>>(a);
-  else if (a.act == AQ_ACT_GELU) ffn_dgu_kernel<T, AQ_ACT_GELU><<<ctas, 256, 0, s>>>(a);
-  else ffn_dgu_kernel<T, AQ_ACT_GELU_TANH><<<ctas, 256, 0, s>>>(a);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = a.act == AQ_ACT_SILU   ? launch(ffn_dgu_kernel<T, AQ_ACT_SILU>, ctas, 256, 0, s, a)
+                  : a.act == AQ_ACT_GELU ? launch(ffn_dgu_kernel<T, AQ_ACT_GELU>, ctas, 256, 0, s, a)
+                                         : launch(ffn_dgu_kernel<T, AQ_ACT_GELU_TANH>, ctas, 256, 0, s, a);
   if (e != cudaSuccess) return e;
-  const int pairs = a.sms / 2 < kMaxPairs ? a.sms / 2 : kMaxPairs;
+  const Plan plan = plan_of(a);
   Products p{};
   Maps maps;
   p.format = Num<T>::kFormat;
   p.status = a.status;
-  p.m_tiles[0] = ceil_div(a.rows, 256);
-  p.k_blocks[0] = 2 * ceil_div(a.inner, kDeep);
-  p.m_tiles[1] = ceil_div(a.inner, 256);
-  p.k_blocks[1] = ceil_div(a.rows, kDeep);
-  const long long m0 = a.dx ? p.m_tiles[0] : 0, m1 = a.dwg ? 2 * p.m_tiles[1] : 0;
-  long long best = -1;
-  for (int n = 256; n >= 64; n -= 32) {
-    const int nt = ceil_div(a.hidden, n);
-    // the work of all tiles over the pairs, and one shorter tile that the last round leaves uneven
-    const long long c0 = (long long)p.k_blocks[0] * 2 * n, c1 = (long long)p.k_blocks[1] * 2 * n;
-    const long long whole = (m0 * nt * c0 + m1 * nt * c1) / pairs, uneven = m0 && m1 ? (c0 < c1 ? c0 : c1) / 2 : 0;
-    const long long alone = m0 && !m1 ? cost(m0 * nt, pairs, p.k_blocks[0], n) : m1 && !m0 ? cost(m1 * nt, pairs, p.k_blocks[1], n) : 0;
-    const long long least = m0 ? c0 : c1;
-    long long c = alone ? alone : whole + uneven + 16 * n;
-    if (c < least) c = least;
-    if (best < 0 || c < best) { best = c; p.n[0] = p.n[1] = n; }
-  }
-  p.n_tiles[0] = p.n_tiles[1] = ceil_div(a.hidden, p.n[0]);
+  p.n = plan.n;
+  p.k_total = 2 * ceil_div(a.inner, kDeep);
   p.rows[0] = (int)a.rows;
   p.rows[1] = a.inner;
   p.cols[0] = p.cols[1] = a.hidden;
+  p.partial = plan.parts > 1 ? a.partial : nullptr;
+  const int count = classes_of(plan, a.rows, a.hidden, a.inner, a.dx != nullptr, a.dwg != nullptr, p.cls);
+  long long tiles = 0;
+  for (int c = 0; c < count; ++c) tiles += tiles_of(p.cls[c]);
+  const int pairs = tiles < a.pairs ? (int)tiles : a.pairs;
+  Run runs[kMaxRuns] = {{0, pairs}};
+  int n_runs = 1;
+  for (int c = 0; c < count; ++c) n_runs = deal(tiles_of(p.cls[c]), cycles_of(p.cls[c]), runs, n_runs, p.first[c]);
   maps.set<T>(&p.a[0], a.dg, a.rows, a.inner, a.inner, 64, 64);
   maps.set<T>(&p.a[1], a.du, a.rows, a.inner, a.inner, 64, 64);
   p.a2[0] = p.a[0];
@@ -557,16 +847,28 @@ cudaError_t run_grad(const FfnGradArgs& a, cudaStream_t s) {
     maps.set<T>(&p.out[2], a.dwu, a.inner, a.hidden, a.lddw, kChunk, 32);
   }
   if (maps.error != cudaSuccess) return maps.error;
-  const long long tiles0 = m0 * p.n_tiles[0], tiles1 = m1 * p.n_tiles[1];
-  const int used = tiles0 + tiles1 < pairs ? (int)(tiles0 + tiles1) : pairs;
-  share(&p, tiles0, tiles1, used);
-  return launch(products_kernel<T, AQ_ACT_SILU, true>, p, used, s);
+  e = launch_products<T, AQ_ACT_SILU, true>(p, pairs, s);
+  if (e != cudaSuccess || !p.partial) return e;
+  int parts = 1;
+  for (int c = 0; c < count; ++c) if (p.cls[c].problem == 0) parts = p.cls[c].parts;
+  return launch(ffn_join_kernel<T>, (unsigned)((a.rows * (a.hidden / 8) + 255) / 256), 256, 0, s, (const float*)a.partial, parts, a.rows, a.hidden,
+                static_cast<T*>(a.dx), a.lddx);
+}
+
+template <typename T>
+cudaError_t run_act(const FfnArgs& a, cudaStream_t s) {
+  return a.act == AQ_ACT_SILU ? run<T, AQ_ACT_SILU>(a, s) : a.act == AQ_ACT_GELU ? run<T, AQ_ACT_GELU>(a, s) : run<T, AQ_ACT_GELU_TANH>(a, s);
 }
 
 }  // namespace
 
+long long ffn_grad_partial_bytes(const FfnGradArgs& a) {
+  const Plan plan = plan_of(a);
+  return plan.parts > 1 ? (long long)plan.parts * a.rows * a.hidden * 4 : 0;
+}
+cudaError_t ffn_resident_pairs(int* pairs) { return resident_pairs(pairs); }
 cudaError_t launch_ffn(int dtype, const FfnArgs& a, cudaStream_t s) {
-  return dtype == AQ_FP16 ? run<__half>(a, s) : run<__nv_bfloat16>(a, s);
+  return dtype == AQ_FP16 ? run_act<__half>(a, s) : run_act<__nv_bfloat16>(a, s);
 }
 cudaError_t launch_ffn_grad(int dtype, const FfnGradArgs& a, cudaStream_t s) {
   return dtype == AQ_FP16 ? run_grad<__half>(a, s) : run_grad<__nv_bfloat16>(a, s);

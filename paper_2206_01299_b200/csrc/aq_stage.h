@@ -62,7 +62,7 @@ struct FfnArgs {
   void* h; long long ldh;
   void *g, *u; long long ldgu;            // may be null
   uint32_t* status;
-  int sms;
+  int pairs;                              // CTA pairs resident at a time
 };
 
 struct FfnGradArgs {
@@ -74,14 +74,18 @@ struct FfnGradArgs {
   void* dx; long long lddx;               // may be null
   void *dwg, *dwu; long long lddw;        // may be null
   void *dg, *du;                          // T[rows][inner], workspace
+  float* partial;                         // workspace, ffn_grad_partial_bytes of it
   uint32_t* status;
-  int sms;
+  int sms, pairs;
 };
 
 cudaError_t launch_logprob(int dtype, const LogprobArgs& a, cudaStream_t s);
 cudaError_t launch_logprob_grad(int dtype, const LogprobGradArgs& a, cudaStream_t s);
 cudaError_t launch_qk(int dtype, const QkArgs& a, cudaStream_t s);
 cudaError_t launch_qk_grad(int dtype, const QkArgs& a, cudaStream_t s);
+cudaError_t ffn_resident_pairs(int* pairs);       // of the current device
+// bytes of `partial` that a call needs; goes by the sizes, pairs and which outputs there are
+long long ffn_grad_partial_bytes(const FfnGradArgs& a);
 cudaError_t launch_ffn(int dtype, const FfnArgs& a, cudaStream_t s);
 cudaError_t launch_ffn_grad(int dtype, const FfnGradArgs& a, cudaStream_t s);
 

@@ -9,7 +9,7 @@
 #include <new>
 
 struct aq_stage {
-  int device = 0, sms = 0;
+  int device = 0, sms = 0, pairs = 0;
   int dtype = AQ_FP16;
   cudaStream_t stream = nullptr;
   uint32_t* status = nullptr;
@@ -140,6 +140,7 @@ aq_stage* aq_stage_create(void) {
   if (!st) { fail(nullptr, AQ_ENOMEM, "host allocation failed"); return nullptr; }
   cudaError_t e = cudaGetDevice(&st->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&st->sms, cudaDevAttrMultiProcessorCount, st->device);
+  if (e == cudaSuccess) e = aq::ffn_resident_pairs(&st->pairs);
   if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&st->status), 256);
   if (e == cudaSuccess) e = cudaMemset(st->status, 0, 256);
   if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&st->partials), sizeof(float) * aq::kQkGradCtas * 2 * 256);
@@ -247,7 +248,7 @@ int aq_gated_ffn(aq_stage* st, const void* x, int64_t ldx, const void* wg, const
     AQ_TRY(check_matrix(st, who, "u", u, ldgu, inner));
   }
   DeviceGuard guard(st->device);
-  const aq::FfnArgs a{x, ldx, wg, wu, ldw, rows, hidden, inner, act, h, ldh, g, u, ldgu, st->status, st->sms};
+  const aq::FfnArgs a{x, ldx, wg, wu, ldw, rows, hidden, inner, act, h, ldh, g, u, ldgu, st->status, st->pairs};
   return launched(st, aq::launch_ffn(st->dtype, a, st->stream), who);
 }
 
@@ -279,10 +280,13 @@ int aq_gated_ffn_grad(aq_stage* st, const void* dh, int64_t lddh, const void* x,
   AQ_TRY(check_matrix(st, who, "u", u, ldgu, inner));
   if (dx) AQ_TRY(check_matrix(st, who, "dx", dx, lddx, hidden));
   if (!dx && !dwg) return AQ_OK;
-  const size_t half = (size_t)rows * (size_t)inner * 2;
-  AQ_TRY(ensure_work(st, 2 * half));
-  const aq::FfnGradArgs a{dh, lddh, x, ldx, wg, wu, ldw, g, u, ldgu, rows, hidden, inner, act, dx, lddx, dwg, dwu, lddw,
-                          st->work, static_cast<char*>(st->work) + half, st->status, st->sms};
+  const size_t half = (size_t)rows * (size_t)inner * 2;      // a multiple of 16 bytes
+  aq::FfnGradArgs a{dh, lddh, x, ldx, wg, wu, ldw, g, u, ldgu, rows, hidden, inner, act, dx, lddx, dwg, dwu, lddw,
+                    nullptr, nullptr, nullptr, st->status, st->sms, st->pairs};
+  AQ_TRY(ensure_work(st, 2 * half + (size_t)aq::ffn_grad_partial_bytes(a)));
+  a.dg = st->work;
+  a.du = static_cast<char*>(st->work) + half;
+  a.partial = reinterpret_cast<float*>(static_cast<char*>(st->work) + 2 * half);
   return launched(st, aq::launch_ffn_grad(st->dtype, a, st->stream), who);
 }
 
