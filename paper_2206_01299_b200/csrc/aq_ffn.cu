@@ -75,16 +75,21 @@ template <int ACT> __device__ void activation(float g, float* a, float* da) {
 // ---- instructions ------------------------------------------------------------------------------------------------
 
 __device__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-// the address of the pair's first CTA's copy of a shared variable
-__device__ uint32_t in_first_cta(uint32_t addr) { uint32_t r; asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr)); return r; }
 __device__ void barrier_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ void barrier_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+__device__ void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// four bytes into the shared memory of either CTA, counted by that CTA's barrier
+__device__ void send(uint32_t to, uint32_t value, uint32_t bar) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];" ::"r"(to), "r"(value), "r"(bar) : "memory");
+}
+__device__ uint32_t in_cta(uint32_t addr, uint32_t rank) { uint32_t r; asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank)); return r; }
 __device__ void barrier_arrive_remote(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+constexpr uint32_t kSleepNs = 100000;         // how long a try may sleep: a thread that polls takes issue slots and power from the products
 __device__ bool barrier_try(uint32_t bar, uint32_t parity) {
   uint32_t done;
-  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity), "r"(kSleepNs) : "memory");
   return done != 0;
 }
 __device__ unsigned long long now_ns() { unsigned long long t; asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t)); return t; }
@@ -92,7 +97,7 @@ __device__ unsigned long long now_ns() { unsigned long long t; asm volatile("mov
 __device__ __noinline__ bool barrier_wait_long(uint32_t bar, uint32_t parity, uint32_t* status) {
   const unsigned long long until = now_ns() + 4000000000ull;
   do {
-    for (int i = 0; i < 256; ++i)
+    for (int i = 0; i < 64; ++i)
       if (barrier_try(bar, parity)) return true;
   } while (now_ns() < until);
   atomicOr(status, (uint32_t)AQ_ST_STALLED);
@@ -100,7 +105,7 @@ __device__ __noinline__ bool barrier_wait_long(uint32_t bar, uint32_t parity, ui
 }
 __device__ bool barrier_wait(uint32_t bar, uint32_t parity, uint32_t* status) {
 #pragma unroll 1
-  for (int i = 0; i < 64; ++i)
+  for (int i = 0; i < 16; ++i)
     if (barrier_try(bar, parity)) return true;
   return barrier_wait_long(bar, parity, status);
 }
@@ -108,6 +113,12 @@ __device__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.te
 // programmatic launch: the next kernel of the stream may be placed; the results of the previous one are needed from here
 __device__ void next_may_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// one lane waits for its warp
+__device__ bool warp_wait(int lane, uint32_t bar, uint32_t parity, uint32_t* status) {
+  int ok = 1;
+  if (lane == 0) ok = barrier_wait(bar, parity, status);
+  return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
 // a box of this GPU's memory into this CTA's shared memory, counted by the first CTA's barrier
 __device__ void load_box(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
@@ -166,25 +177,25 @@ constexpr int kColumns = 512;                 // tensor memory: two tiles' sums 
 constexpr int kSharedBytes = 1024 + kStages * 2 * kHalfTile + kEpilogueWarps * kOutBuffers * kOutBytes;
 constexpr int kMaxPairs = 128;
 
-constexpr int kClasses = 4;                   // kinds of tiles of one launch: dx and dW, each with full and last columns
+constexpr int kClasses = 2;                   // kinds of tiles of one launch: dx and dW
 
-// Tiles that take the same time: `columns` wide from column tile `first`, `count` of them, in each of m_tiles rows of tiles,
-// `parts` times over (forward and dx: parts of the depth; dW: dWg and dWu).
+// `count` tiles, `columns` wide but for the last, in each of m_tiles rows of tiles, `parts` times over (dx: parts of the
+// depth; dW: dWg and dWu).  The tiles of a row follow one another, so that the pairs at work on them share its operand in L2.
 struct TileClass {
-  int problem, m_tiles, first, count, columns, parts, k_blocks;
+  int problem, m_tiles, count, columns, last, parts, k_blocks;
 };
 
 struct Products {
   CUtensorMap a[2], b[2];                     // forward and dx
   CUtensorMap a2[2], b2;                      // dW: dg and du across their rows, x
   CUtensorMap out[3];                         // forward: h, g, u; backward: dx, dWg, dWu
-  int n;                                      // columns of a tile (both halves of the pair)
   int k_total;                                // stages of the whole depth of forward and dx
   int rows[2], cols[2];                       // of the outputs
   int save;                                   // forward: write g and u
   float* partial;                             // dx in parts: float[parts][rows][cols], else null
   TileClass cls[kClasses];                    // the longest tiles first
-  uint32_t first[kClasses][kMaxPairs + 1];    // the tiles of each class that a pair works on; forward: pair, pair + pairs, ...
+  int tiles;                                  // of all classes
+  uint32_t* next;                             // tiles taken beyond each pair's first; 0 between launches
   uint32_t format;
   uint32_t* status;
 };
@@ -198,32 +209,32 @@ __device__ void place(const Products& p, const TileClass& c, unsigned at, Tile* 
   t->problem = c.problem;
   t->part = (int)(rest / (unsigned)c.m_tiles);
   t->m0 = (int)(rest % (unsigned)c.m_tiles) * 256;
-  t->n0 = (c.first + (int)n) * p.n;
-  t->columns = c.columns;
+  t->n0 = (int)n * c.columns;
+  t->columns = (int)n == c.count - 1 ? c.last : c.columns;
   t->k0 = c.problem == 0 ? t->part * c.k_blocks : 0;
   t->k_blocks = c.problem == 0 ? min(c.k_blocks, p.k_total - t->k0) : c.k_blocks;
 }
 
+// Tile `at` of the launch; false past the last one.
 template <bool BACKWARD>
-__device__ bool tile_at(const Products& p, unsigned pair, unsigned pairs, unsigned i, Tile* t) {
+__device__ bool tile_at(const Products& p, unsigned at, Tile* t) {
+  if (at >= (unsigned)p.tiles) return false;
   if constexpr (!BACKWARD) {
     // rows of tiles fastest: the pairs at work share their columns' weights
     const TileClass& c = p.cls[0];
-    const unsigned at = pair + i * pairs;
-    if (at >= (unsigned)c.m_tiles * (unsigned)c.count) return false;
     *t = {0, 0, (int)(at % (unsigned)c.m_tiles) * 256, (int)(at / (unsigned)c.m_tiles) * (c.columns / 2), c.columns, 0, c.k_blocks};
-    return true;
   } else {
     for (int k = 0; k < kClasses; ++k) {
-      const unsigned from = p.first[k][pair], n = p.first[k][pair + 1] - from;
-      if (i < n) {
-        place(p, p.cls[k], from + i, t);
-        return true;
+      const TileClass& c = p.cls[k];
+      const unsigned n = (unsigned)c.m_tiles * (unsigned)c.count * (unsigned)c.parts;
+      if (at < n) {
+        place(p, c, at, t);
+        break;
       }
-      i -= n;
+      at -= n;
     }
-    return false;
   }
+  return true;
 }
 
 // what the tensor cores are told of a stage's tile in shared memory: rows of 128 bytes swizzled in groups of eight (1024
@@ -235,24 +246,34 @@ __device__ uint64_t describe(uint32_t addr, bool across) {
 template <typename T, int ACT, bool BACKWARD>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) products_kernel(const __grid_constant__ Products p) {
   extern __shared__ uint8_t shared_raw[];
-  __shared__ __align__(8) uint64_t barriers[2 * kStages + 4];
-  __shared__ uint32_t tensor_base;
+  __shared__ __align__(8) uint64_t barriers[2 * kStages + 9];
+  __shared__ uint32_t tensor_base, tile_ids[2];
   const uint32_t base = (shared_address(shared_raw) + 1023u) & ~1023u;
   const uint32_t out_base = base + kStages * 2 * kHalfTile;
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-  const unsigned rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const uint32_t rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const uint32_t bars = shared_address(barriers);
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 8u * (kStages + s); };
   auto sums_full = [&](int s) { return bars + 8u * (2 * kStages + s); };
   auto sums_empty = [&](int s) { return bars + 8u * (2 * kStages + 2 + s); };
+  auto tile_sent = [&](int s) { return bars + 8u * (2 * kStages + 4 + s); };
+  auto tile_read = [&](int s) { return bars + 8u * (2 * kStages + 6 + s); };   // the first CTA's counts both CTAs' readers
+
+  const uint32_t tile_wanted = bars + 8u * (2 * kStages + 8);
 
   if (warp == 3 && lane == 0) {               // fetch the maps that every tile begins with
     prefetch_map(&p.a[0]); prefetch_map(&p.b[0]); prefetch_map(&p.b[1]);
   }
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { barrier_init(full(s), 1); barrier_init(empty(s), 1); }
-    for (int s = 0; s < 2; ++s) { barrier_init(sums_full(s), 1); barrier_init(sums_empty(s), 2 * kEpilogueWarps); }
+    barrier_init(tile_wanted, 1);
+    for (int s = 0; s < 2; ++s) {
+      barrier_init(sums_full(s), 1);
+      barrier_init(sums_empty(s), 2 * kEpilogueWarps);
+      barrier_init(tile_sent(s), 1);
+      barrier_init(tile_read(s), 2 * kEpilogueWarps + 4);      // epilogue warps and loaders of both CTAs, the issuing thread, the second CTA's warp 3
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 2) {
@@ -267,20 +288,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
   next_may_launch();
   wait_for_previous();
 
+  // A pair's first tile is its own number; the next ones are whatever tile nobody has taken yet (the longest come first), so
+  // that pairs end together whatever their speed.  Which pair computes a tile does not touch its result.
+  // `turn` numbers the tiles that this thread or warp has asked for.
+  auto next_tile = [&](int turn, Tile* t) {
+    if (turn == 0) return tile_at<BACKWARD>(p, pair, t);
+    const int slot = (turn - 1) & 1;
+    const bool sent = warp < 4 ? barrier_wait(tile_sent(slot), ((turn - 1) >> 1) & 1, p.status)
+                               : warp_wait(lane, tile_sent(slot), ((turn - 1) >> 1) & 1, p.status);
+    if (!sent) return false;
+    uint32_t at;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(at) : "r"(shared_address(&tile_ids[slot])) : "memory");
+    if (warp >= 4) __syncwarp();
+    if (warp < 4 || lane == 0) barrier_arrive_remote(in_cta(tile_read(slot), 0));
+    return tile_at<BACKWARD>(p, at, t);
+  };
+
   if (warp == 0) {
     if (lane == 0) {
       int stage = 0;
       uint32_t phase = 0;
       bool going = true;
       Tile t;
-      for (unsigned i = 0; going && tile_at<BACKWARD>(p, pair, pairs, i, &t); ++i) {
+      for (int i = 0; going && next_tile(i, &t); ++i) {
+        if (rank == 0) barrier_arrive(tile_wanted);
         const int half_n = t.columns / 2;
         const int b_boxes = BACKWARD ? (half_n + 63) / 64 : 0;
         const uint32_t bytes = kHalfTile + (BACKWARD ? (uint32_t)b_boxes * 8192u : (uint32_t)half_n * 128u);
         for (int i_k = 0; i_k < t.k_blocks; ++i_k) {
           const int k = t.k0 + i_k;
           if (!barrier_wait(empty(stage), phase ^ 1, p.status)) { going = false; break; }
-          const uint32_t bar = in_first_cta(full(stage));
+          const uint32_t bar = in_cta(full(stage), 0);
           if (rank == 0) barrier_expect(full(stage), 2 * bytes);
           const uint32_t to_a = base + (uint32_t)stage * 2 * kHalfTile, to_b = to_a + kHalfTile;
           if constexpr (!BACKWARD) {
@@ -311,7 +349,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
       uint32_t phase = 0, acc_phase = 0;
       bool going = true;
       Tile t;
-      for (unsigned i = 0; going && tile_at<BACKWARD>(p, pair, pairs, i, &t); ++i) {
+      for (int i = 0; going && next_tile(i, &t); ++i) {
         const bool a_across = BACKWARD && t.problem == 1, b_across = BACKWARD;
         // binary32 sums (bit 4), operand types, which operands run across, N / 8, M / 16
         const uint32_t what = (1u << 4) | (p.format << 7) | (p.format << 10) | ((uint32_t)a_across << 15) | ((uint32_t)b_across << 16) |
@@ -334,6 +372,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
         commit(sums_full(acc));
         acc ^= 1;
         if (!acc) acc_phase ^= 1;
+      }
+    }
+  } else if (warp == 3) {
+    if (lane == 0) {
+      // Each CTA says what its barrier is to receive; the first CTA takes a tile when the loader has begun with the one before
+      // (no earlier, so that none waits at a busy pair) and sends it to both.
+      for (int i = 0;; ++i) {
+        const int slot = i & 1;
+        uint32_t at = 0;
+        if (rank == 0) {
+          if (!barrier_wait(tile_wanted, i & 1, p.status) || !barrier_wait(tile_read(slot), ((i >> 1) & 1) ^ 1, p.status)) break;
+          barrier_expect(tile_sent(slot), 4);
+          at = pairs + atomicAdd(p.next, 1u);
+          if (at == (unsigned)p.tiles + pairs - 1) *p.next = 0;      // the last one that any pair takes: for the next launch
+          for (uint32_t r = 0; r < 2; ++r) send(in_cta(shared_address(&tile_ids[slot]), r), at, in_cta(tile_sent(slot), r));
+        } else {
+          barrier_expect(tile_sent(slot), 4);
+          if (!barrier_wait(tile_sent(slot), (i >> 1) & 1, p.status)) break;
+          asm volatile("ld.shared.b32 %0, [%1];" : "=r"(at) : "r"(shared_address(&tile_ids[slot])) : "memory");
+          barrier_arrive_remote(in_cta(tile_read(slot), 0));
+        }
+        if (at >= (unsigned)p.tiles) break;
       }
     }
   } else if (warp >= 4) {
@@ -360,8 +420,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
       buffer ^= 1;
     };
     Tile t;
-    for (unsigned i = 0; tile_at<BACKWARD>(p, pair, pairs, i, &t); ++i) {
-      if (!barrier_wait(sums_full(acc), acc_phase, p.status)) break;
+    for (int i = 0; next_tile(i, &t); ++i) {
+      if (!warp_wait(lane, sums_full(acc), acc_phase, p.status)) break;
       fence_after();
       const uint32_t sums = tensor + (uint32_t)acc * 256u + ((uint32_t)quarter << 21);
       const int width = BACKWARD ? t.columns : t.columns / 2;
@@ -376,7 +436,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
         if (c + 2 * kChunk >= width) {                    // this warp's last columns are in registers
           fence_before();
           __syncwarp();
-          if (lane == 0) barrier_arrive_remote(in_first_cta(sums_empty(acc)));
+          if (lane == 0) barrier_arrive_remote(in_cta(sums_empty(acc), 0));
         }
         if (!rows_there || t.n0 + c >= p.cols[t.problem]) continue;
         float v[32];
@@ -412,7 +472,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
         }
       }
       if (turn * kChunk >= width) {                       // a narrow tile: nothing here for this warp
-        if (lane == 0) barrier_arrive_remote(in_first_cta(sums_empty(acc)));
+        if (lane == 0) barrier_arrive_remote(in_cta(sums_empty(acc), 0));
       }
       acc ^= 1;
       if (!acc) acc_phase ^= 1;
@@ -677,8 +737,7 @@ cudaError_t run(const FfnArgs& a, cudaStream_t s) {
     const long long tiles = (long long)m_tiles * ceil_div(a.inner, f), c = ((tiles + a.pairs - 1) / a.pairs) * kb * stage_cycles(2 * f) + 32 * f + 1500;
     if (!best || c < least) { best = f; least = c; }
   }
-  p.n = 2 * best;
-  p.cls[0] = {0, m_tiles, 0, ceil_div(a.inner, best), 2 * best, 1, kb};
+  p.cls[0] = {0, m_tiles, ceil_div(a.inner, best), 2 * best, 2 * best, 1, kb};
   p.k_total = kb;
   p.rows[0] = (int)a.rows;
   p.cols[0] = a.inner;
@@ -696,12 +755,14 @@ cudaError_t run(const FfnArgs& a, cudaStream_t s) {
   }
   if (maps.error != cudaSuccess) return maps.error;
   const long long tiles = (long long)m_tiles * p.cls[0].count;
+  if (tiles > 0x7fffffff - kMaxPairs) return cudaErrorInvalidValue;
+  p.tiles = (int)tiles;
+  p.next = a.next;
   return launch_products<T, ACT, false>(p, tiles < a.pairs ? (int)tiles : a.pairs, s);
 }
 
 // ---- the gradient's plan
 
-constexpr int kMaxRuns = 1 + 2 * kClasses;    // only one run is split in three by a class
 constexpr long long kMostPartialBytes = 256ll << 20;
 
 struct Plan {
@@ -709,31 +770,28 @@ struct Plan {
   long long cycles = -1;
 };
 
-// The classes of tiles of a plan, the longest first; their number.
+// The classes of tiles of a plan, the longest first; their number.  Columns that a row of full tiles leaves over widen its
+// last tile where they fit, and are a narrow tile of their own otherwise.
 int classes_of(const Plan& plan, long long rows, int hidden, int inner, bool dx, bool dw, TileClass* out) {
-  const int n = plan.n, full = hidden / n, rest = hidden - full * n, last = (rest + 31) / 32 * 32;
-  const int kb0 = 2 * ceil_div(inner, kDeep), kb1 = ceil_div(rows, kDeep);
-  const int part = ceil_div(kb0, plan.parts);
+  int count = hidden / plan.n, last = plan.n;
+  const int rest = (hidden - count * plan.n + 31) / 32 * 32;
+  if (rest && count && plan.n + rest <= 256) last = plan.n + rest;
+  else if (rest) { ++count; last = rest; }
+  const int kb0 = 2 * ceil_div(inner, kDeep), part = ceil_div(kb0, plan.parts);
   int c = 0;
-  auto add = [&](int problem, int first, int count, int columns) {
-    if (!count) return;
-    out[c++] = problem == 0 ? TileClass{0, ceil_div(rows, 256), first, count, columns, ceil_div(kb0, part), part}
-                            : TileClass{1, ceil_div(inner, 256), first, count, columns, 2, kb1};
-  };
-  if (dx) { add(0, 0, full, n); add(0, full, rest > 0, last); }
-  if (dw) { add(1, 0, full, n); add(1, full, rest > 0, last); }
-  for (int i = 1; i < c; ++i)
-    for (int j = i; j > 0 && out[j].k_blocks * stage_cycles(out[j].columns) > out[j - 1].k_blocks * stage_cycles(out[j - 1].columns); --j) {
-      const TileClass t = out[j];
-      out[j] = out[j - 1];
-      out[j - 1] = t;
-    }
+  if (dx) out[c++] = {0, ceil_div(rows, 256), count, plan.n, last, ceil_div(kb0, part), part};
+  if (dw) out[c++] = {1, ceil_div(inner, 256), count, plan.n, last, 2, ceil_div(rows, kDeep)};
+  if (c == 2 && out[1].k_blocks > out[0].k_blocks) {
+    const TileClass t = out[0];
+    out[0] = out[1];
+    out[1] = t;
+  }
   return c;
 }
 
 long long tiles_of(const TileClass& c) { return (long long)c.m_tiles * c.count * c.parts; }
-// of one tile: its stages and what starting the next one costs
-long long cycles_of(const TileClass& c) { return (long long)c.k_blocks * stage_cycles(c.columns) + 200; }
+// of a tile: its stages and what starting the next one costs
+long long cycles_of(const TileClass& c, int columns) { return (long long)c.k_blocks * stage_cycles(columns) + 200; }
 
 // Widths and parts by an estimate of the longest load.  Parts of dx's depth, 2 * inner, serve few rows, whose dx is a
 // handful of very long tiles; joining them is another kernel of about 5000 cycles that moves 8 bytes a value and part, some
@@ -750,62 +808,19 @@ Plan plan_of(const FfnGradArgs& a) {
       TileClass cls[kClasses];
       const int count = classes_of(plan, a.rows, a.hidden, a.inner, a.dx != nullptr, a.dwg != nullptr, cls);
       long long work = 0, tiles = 0;
-      for (int c = 0; c < count; ++c) { work += tiles_of(cls[c]) * cycles_of(cls[c]); tiles += tiles_of(cls[c]); }
-      // dealt longest first, the loads end within about half of the shortest tile of one another
-      plan.cycles = tiles <= a.pairs ? 0 : work / a.pairs + cycles_of(cls[count - 1]) / 2;
-      if (plan.cycles < cycles_of(cls[0])) plan.cycles = cycles_of(cls[0]);
+      for (int c = 0; c < count; ++c) {
+        work += (long long)cls[c].m_tiles * cls[c].parts * ((cls[c].count - 1) * cycles_of(cls[c], n) + cycles_of(cls[c], cls[c].last));
+        tiles += tiles_of(cls[c]);
+      }
+      // taken longest first, the pairs end within about half of a short tile of one another
+      const long long longest = cycles_of(cls[0], cls[0].count > 1 && n > cls[0].last ? n : cls[0].last);
+      plan.cycles = tiles <= a.pairs ? 0 : work / a.pairs + cycles_of(cls[count - 1], n) / 2;
+      if (plan.cycles < longest) plan.cycles = longest;
       plan.cycles += 16 * n + (parts > 1 ? 5000 + (long long)parts * a.rows * a.hidden * 8 / 3500 : 0);
       if (best.cycles < 0 || plan.cycles < best.cycles) best = plan;
     }
   }
   return best;
-}
-
-// Neighbouring pairs with the same load.
-struct Run {
-  long long load;
-  int pairs;
-};
-
-// Deals a class of tiles: to whichever pairs have the least to do, until all are dealt.  The pairs of a run differ at most
-// where the last tiles run out, so there are few runs whatever the number of pairs.  first[i] is set to the first tile of pair i.
-int deal(long long tiles, long long cost, Run* runs, int n_runs, uint32_t* first) {
-  auto fits = [&](long long level) {                          // tiles that end at or before the level
-    long long n = 0;
-    for (int i = 0; i < n_runs; ++i) if (runs[i].load < level) n += (level - runs[i].load) / cost * runs[i].pairs;
-    return n;
-  };
-  long long low = runs[0].load, high = runs[0].load, pairs = 0;
-  for (int i = 0; i < n_runs; ++i) {
-    if (runs[i].load < low) low = runs[i].load;
-    if (runs[i].load > high) high = runs[i].load;
-    pairs += runs[i].pairs;
-  }
-  high += cost * (tiles / pairs + 1);
-  while (high - low > 1) {                                    // the lowest level that holds them all
-    const long long mid = low + (high - low) / 2;
-    if (fits(mid) >= tiles) high = mid;
-    else low = mid;
-  }
-  Run now[kMaxRuns];
-  int n_now = 0, pair = 0;
-  long long at = 0;
-  auto give = [&](long long load, int count, long long each) {
-    for (int i = 0; i < count; ++i, ++pair, at += each) first[pair] = (uint32_t)at;
-    if (count) now[n_now++] = {load + each * cost, count};
-  };
-  for (int i = 0; i < n_runs; ++i) {
-    const long long left = tiles - at, each = left && runs[i].load < high ? (high - runs[i].load) / cost : 0;
-    const int whole = each && each * runs[i].pairs > left ? (int)(left / each) : runs[i].pairs;
-    give(runs[i].load, whole, each);
-    if (whole < runs[i].pairs) {
-      give(runs[i].load, 1, tiles - at);
-      give(runs[i].load, runs[i].pairs - whole - 1, 0);
-    }
-  }
-  first[pair] = (uint32_t)at;
-  for (int i = 0; i < n_now; ++i) runs[i] = now[i];
-  return n_now;
 }
 
 template <typename T>
@@ -821,7 +836,6 @@ cudaError_t run_grad(const FfnGradArgs& a, cudaStream_t s) {
   Maps maps;
   p.format = Num<T>::kFormat;
   p.status = a.status;
-  p.n = plan.n;
   p.k_total = 2 * ceil_div(a.inner, kDeep);
   p.rows[0] = (int)a.rows;
   p.rows[1] = a.inner;
@@ -830,10 +844,10 @@ cudaError_t run_grad(const FfnGradArgs& a, cudaStream_t s) {
   const int count = classes_of(plan, a.rows, a.hidden, a.inner, a.dx != nullptr, a.dwg != nullptr, p.cls);
   long long tiles = 0;
   for (int c = 0; c < count; ++c) tiles += tiles_of(p.cls[c]);
+  if (tiles > 0x7fffffff - kMaxPairs) return cudaErrorInvalidValue;
+  p.tiles = (int)tiles;
+  p.next = a.next;
   const int pairs = tiles < a.pairs ? (int)tiles : a.pairs;
-  Run runs[kMaxRuns] = {{0, pairs}};
-  int n_runs = 1;
-  for (int c = 0; c < count; ++c) n_runs = deal(tiles_of(p.cls[c]), cycles_of(p.cls[c]), runs, n_runs, p.first[c]);
   maps.set<T>(&p.a[0], a.dg, a.rows, a.inner, a.inner, 64, 64);
   maps.set<T>(&p.a[1], a.du, a.rows, a.inner, a.inner, 64, 64);
   p.a2[0] = p.a[0];

@@ -49,7 +49,7 @@ struct QkArgs {
   long long q_out_stride, k_out_stride;
   float *dwq, *dwk;                       // backward only, may be null
   float* partials;                        // [kQkGradCtas][2][256] sums of dwq, dwk of each CTA
-  unsigned* ticket;                       // CTAs that have written theirs; 0 between calls
+  uint32_t* ticket;                       // CTAs that have written theirs; 0 between calls
   uint32_t* status;
   int sms;
 };
@@ -62,6 +62,7 @@ struct FfnArgs {
   void* h; long long ldh;
   void *g, *u; long long ldgu;            // may be null
   uint32_t* status;
+  uint32_t* next;                         // tiles taken; 0 between calls
   int pairs;                              // CTA pairs resident at a time
 };
 
@@ -76,6 +77,7 @@ struct FfnGradArgs {
   void *dg, *du;                          // T[rows][inner], workspace
   float* partial;                         // workspace, ffn_grad_partial_bytes of it
   uint32_t* status;
+  uint32_t* next;
   int sms, pairs;
 };
 

@@ -13,7 +13,7 @@ struct aq_stage {
   int dtype = AQ_FP16;
   cudaStream_t stream = nullptr;
   uint32_t* status = nullptr;
-  unsigned* ticket = nullptr;             // in the status word's allocation
+  uint32_t *ticket = nullptr, *next = nullptr;   // in the status word's allocation
   float* partials = nullptr;              // aq_qk_norm_rope_grad
   void* work = nullptr;                   // aq_gated_ffn_grad
   size_t work_bytes = 0;
@@ -153,7 +153,8 @@ aq_stage* aq_stage_create(void) {
     delete st;
     return nullptr;
   }
-  st->ticket = st->status + 32;
+  st->ticket = st->status + 16;
+  st->next = st->status + 32;
   return st;
 }
 
@@ -187,7 +188,7 @@ int aq_stage_status(aq_stage* st, uint32_t* bits_host) {
   if (!bits_host) return fail(st, AQ_EINVAL, "aq_stage_status: null pointer");
   DeviceGuard guard(st->device);
   cudaError_t e = cudaMemcpyAsync(bits_host, st->status, sizeof(uint32_t), cudaMemcpyDeviceToHost, st->stream);
-  if (e == cudaSuccess) e = cudaMemsetAsync(st->status, 0, sizeof(uint32_t), st->stream);
+  if (e == cudaSuccess) e = cudaMemsetAsync(st->status, 0, 256, st->stream);   // and the counters, which a kernel that gave up leaves as they were
   if (e == cudaSuccess) e = cudaStreamSynchronize(st->stream);
   return launched(st, e, "aq_stage_status");
 }
@@ -248,7 +249,7 @@ int aq_gated_ffn(aq_stage* st, const void* x, int64_t ldx, const void* wg, const
     AQ_TRY(check_matrix(st, who, "u", u, ldgu, inner));
   }
   DeviceGuard guard(st->device);
-  const aq::FfnArgs a{x, ldx, wg, wu, ldw, rows, hidden, inner, act, h, ldh, g, u, ldgu, st->status, st->pairs};
+  const aq::FfnArgs a{x, ldx, wg, wu, ldw, rows, hidden, inner, act, h, ldh, g, u, ldgu, st->status, st->next, st->pairs};
   return launched(st, aq::launch_ffn(st->dtype, a, st->stream), who);
 }
 
@@ -282,7 +283,7 @@ int aq_gated_ffn_grad(aq_stage* st, const void* dh, int64_t lddh, const void* x,
   if (!dx && !dwg) return AQ_OK;
   const size_t half = (size_t)rows * (size_t)inner * 2;      // a multiple of 16 bytes
   aq::FfnGradArgs a{dh, lddh, x, ldx, wg, wu, ldw, g, u, ldgu, rows, hidden, inner, act, dx, lddx, dwg, dwu, lddw,
-                    nullptr, nullptr, nullptr, st->status, st->sms, st->pairs};
+                    nullptr, nullptr, nullptr, st->status, st->next, st->sms, st->pairs};
   AQ_TRY(ensure_work(st, 2 * half + (size_t)aq::ffn_grad_partial_bytes(a)));
   a.dg = st->work;
   a.du = static_cast<char*>(st->work) + half;
