@@ -125,10 +125,6 @@ __device__ void load_box(uint32_t dst, const CUtensorMap* map, int x, int y, uin
                "l"(map), "r"(x), "r"(y), "r"(bar)
                : "memory");
 }
-__device__ void store_box(const CUtensorMap* map, int x, int y, uint32_t src) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
-  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
 __device__ void multiply(uint32_t sums, uint64_t a, uint64_t b, uint32_t what, uint32_t add) {
   asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(sums), "l"(a), "l"(b), "r"(what),
                "r"(add)
@@ -156,6 +152,12 @@ __device__ void sums_read(uint32_t (&r)[32]) {
                :
                : "memory");
 }
+__device__ void write_shared(uint32_t at, uint4 v) { asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); }
+__device__ uint4 read_shared(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
 __device__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ void pair_sync() {
@@ -171,10 +173,9 @@ constexpr int kHalfTile = 128 * kDeep * 2;    // bytes of one CTA's share of A (
 constexpr int kEpilogueWarps = 8;
 constexpr int kFfnThreads = 128 + 32 * kEpilogueWarps;
 constexpr int kChunk = 32;                    // columns an epilogue warp takes at a time
-constexpr int kOutBytes = 32 * kChunk * 2;    // ... of 32 rows: one TMA store
-constexpr int kOutBuffers = 2;
+constexpr int kOutBytes = 32 * kChunk * 4;    // ... of 32 rows, on their way out
 constexpr int kColumns = 512;                 // tensor memory: two tiles' sums of up to 256 columns
-constexpr int kSharedBytes = 1024 + kStages * 2 * kHalfTile + kEpilogueWarps * kOutBuffers * kOutBytes;
+constexpr int kSharedBytes = 1024 + kStages * 2 * kHalfTile + kEpilogueWarps * kOutBytes;
 constexpr int kMaxPairs = 128;
 
 constexpr int kClasses = 2;                   // kinds of tiles of one launch: dx and dW
@@ -188,7 +189,8 @@ struct TileClass {
 struct Products {
   CUtensorMap a[2], b[2];                     // forward and dx
   CUtensorMap a2[2], b2;                      // dW: dg and du across their rows, x
-  CUtensorMap out[3];                         // forward: h, g, u; backward: dx, dWg, dWu
+  void* out[3];                               // forward: h, g, u; backward: dx, dWg, dWu
+  long long ld[3];
   int k_total;                                // stages of the whole depth of forward and dx
   int rows[2], cols[2];                       // of the outputs
   int save;                                   // forward: write g and u
@@ -398,26 +400,42 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
     }
   } else if (warp >= 4) {
     const int quarter = warp & 3, turn = (warp - 4) / 4;
-    const uint32_t out_buf = out_base + (uint32_t)(warp - 4) * kOutBuffers * kOutBytes;
-    int acc = 0, buffer = 0;
+    const uint32_t out_buf = out_base + (uint32_t)(warp - 4) * kOutBytes;
+    int acc = 0;
     uint32_t acc_phase = 0;
-    // 32 rows x 32 columns of binary32, rounded, to the output at (x, y); each lane holds a row
-    auto store = [&](const CUtensorMap* map, const float (&v)[32], int x, int y) {
-      if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kOutBuffers - 1) : "memory");
-      __syncwarp();
-      const uint32_t to = out_buf + (uint32_t)buffer * kOutBytes;
+    // 32 rows x 32 columns, each lane a row, to (y, x) of an output: turned round in shared memory, so that a store covers
+    // whole 64-byte (binary32: 128-byte) stretches of rows.  (TMA stores from there took 1000 cycles each to give their buffer
+    // back: 8600 cycles a tile of three outputs with two buffers.)
+    auto put16 = [&](const uint32_t (&v)[32], int out, int problem, int x, int y) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {                       // 64-byte rows, their 16-byte pieces swizzled over four rows' worth
-        const uint32_t at = to + (uint32_t)lane * 64u + (uint32_t)((j ^ ((lane >> 1) & 3)) * 16);
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(Num<T>::close(v[8 * j], v[8 * j + 1])),
-                     "r"(Num<T>::close(v[8 * j + 2], v[8 * j + 3])), "r"(Num<T>::close(v[8 * j + 4], v[8 * j + 5])),
-                     "r"(Num<T>::close(v[8 * j + 6], v[8 * j + 7]))
-                     : "memory");
+      for (int j = 0; j < 4; ++j) {                       // the 16-byte pieces of a row swizzled over eight rows' worth of banks
+        const float* const f = reinterpret_cast<const float*>(&v[8 * j]);
+        write_shared(out_buf + (uint32_t)lane * 64u + (uint32_t)((j ^ ((lane >> 1) & 3)) * 16),
+                     make_uint4(Num<T>::close(f[0], f[1]), Num<T>::close(f[2], f[3]), Num<T>::close(f[4], f[5]), Num<T>::close(f[6], f[7])));
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) store_box(map, x, y, to);
-      buffer ^= 1;
+      T* const to = static_cast<T*>(p.out[out]) + (long long)(y + lane / 4) * p.ld[out] + x + (lane & 3) * 8;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int row = j * 8 + lane / 4;
+        const uint4 w = read_shared(out_buf + (uint32_t)row * 64u + (uint32_t)(((lane & 3) ^ ((row >> 1) & 3)) * 16));
+        if (y + row < p.rows[problem] && x + (lane & 3) * 8 < p.cols[problem]) *reinterpret_cast<uint4*>(to + j * 8 * p.ld[out]) = w;
+      }
+      __syncwarp();
+    };
+    auto put32 = [&](const uint32_t (&v)[32], float* out, int x, int y) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        write_shared(out_buf + (uint32_t)lane * 128u + (uint32_t)((j ^ (lane & 7)) * 16), make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+      __syncwarp();
+      float* const to = out + (long long)(y + lane / 8) * p.cols[0] + x + (lane & 7) * 4;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int row = j * 4 + lane / 8;
+        const uint4 w = read_shared(out_buf + (uint32_t)row * 128u + (uint32_t)(((lane & 7) ^ (row & 7)) * 16));
+        if (y + row < p.rows[0] && x + (lane & 7) * 4 < p.cols[0]) *reinterpret_cast<uint4*>(to + (long long)j * 4 * p.cols[0]) = w;
+      }
+      __syncwarp();
     };
     Tile t;
     for (int i = 0; next_tile(i, &t); ++i) {
@@ -439,36 +457,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
           if (lane == 0) barrier_arrive_remote(in_cta(sums_empty(acc), 0));
         }
         if (!rows_there || t.n0 + c >= p.cols[t.problem]) continue;
-        float v[32];
         if constexpr (BACKWARD) {
-          if (t.problem == 0 && p.partial) {
-            const int row = y + lane;
-            float* const to = p.partial + ((long long)t.part * p.rows[0] + row) * p.cols[0] + t.n0 + c;
-#pragma unroll
-            for (int j = 0; j < 32; j += 4)
-              if (row < p.rows[0] && t.n0 + c + j < p.cols[0])
-                *reinterpret_cast<float4*>(to + j) = make_float4(__uint_as_float(r[j]), __uint_as_float(r[j + 1]), __uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
-            continue;
-          }
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
-          store(&p.out[t.problem ? 1 + t.part : 0], v, t.n0 + c, y);
+          if (t.problem == 0 && p.partial) put32(r, p.partial + (long long)t.part * p.rows[0] * p.cols[0], t.n0 + c, y);
+          else put16(r, t.problem ? 1 + t.part : 0, t.problem, t.n0 + c, y);
         } else {
+          if (p.save) {
+            put16(r, 1, 0, t.n0 + c, y);
+            put16(q, 2, 0, t.n0 + c, y);
+          }
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
             float act, dact;
             activation<ACT>(__uint_as_float(r[j]), &act, &dact);
-            v[j] = act * __uint_as_float(q[j]);
+            r[j] = __float_as_uint(act * __uint_as_float(q[j]));
           }
-          store(&p.out[0], v, t.n0 + c, y);
-          if (p.save) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
-            store(&p.out[1], v, t.n0 + c, y);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(q[j]);
-            store(&p.out[2], v, t.n0 + c, y);
-          }
+          put16(r, 0, 0, t.n0 + c, y);
         }
       }
       if (turn * kChunk >= width) {                       // a narrow tile: nothing here for this warp
@@ -477,7 +480,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
       acc ^= 1;
       if (!acc) acc_phase ^= 1;
     }
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   __syncwarp();
   fence_before();
@@ -654,14 +656,14 @@ struct Maps {
   EncodeTiled fn = nullptr;
   cudaError_t error = cudaSuccess;
   Maps() { error = encoder(&fn); }
-  // T[rows][ld], `cols` of a row, in boxes of box_cols x box_rows
+  // T[rows][ld], `cols` of a row, in boxes of 64 columns (128 bytes, swizzled) x box_rows
   template <typename T>
-  void set(CUtensorMap* m, const void* p, long long rows, long long cols, long long ld, int box_cols, int box_rows) {
+  void set(CUtensorMap* m, const void* p, long long rows, long long cols, long long ld, int box_rows) {
     if (error != cudaSuccess) return;
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
-    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, one[2] = {1, 1};
+    const cuuint32_t box[2] = {kDeep, (cuuint32_t)box_rows}, one[2] = {1, 1};
     const CUresult r = fn(m, Num<T>::kMap, 2, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          box_cols * 2 == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) error = cudaErrorInvalidValue;
   }
 };
@@ -745,14 +747,14 @@ cudaError_t run(const FfnArgs& a, cudaStream_t s) {
   p.format = Num<T>::kFormat;
   p.status = a.status;
   Maps maps;
-  maps.set<T>(&p.a[0], a.x, a.rows, a.hidden, a.ldx, kDeep, 128);
-  maps.set<T>(&p.b[0], a.wg, a.inner, a.hidden, a.ldw, kDeep, best);
-  maps.set<T>(&p.b[1], a.wu, a.inner, a.hidden, a.ldw, kDeep, best);
-  maps.set<T>(&p.out[0], a.h, a.rows, a.inner, a.ldh, kChunk, 32);
-  if (p.save) {
-    maps.set<T>(&p.out[1], a.g, a.rows, a.inner, a.ldgu, kChunk, 32);
-    maps.set<T>(&p.out[2], a.u, a.rows, a.inner, a.ldgu, kChunk, 32);
-  }
+  maps.set<T>(&p.a[0], a.x, a.rows, a.hidden, a.ldx, 128);
+  maps.set<T>(&p.b[0], a.wg, a.inner, a.hidden, a.ldw, best);
+  maps.set<T>(&p.b[1], a.wu, a.inner, a.hidden, a.ldw, best);
+  p.out[0] = a.h;
+  p.out[1] = a.g;
+  p.out[2] = a.u;
+  p.ld[0] = a.ldh;
+  p.ld[1] = p.ld[2] = a.ldgu;
   if (maps.error != cudaSuccess) return maps.error;
   const long long tiles = (long long)m_tiles * p.cls[0].count;
   if (tiles > 0x7fffffff - kMaxPairs) return cudaErrorInvalidValue;
@@ -848,18 +850,18 @@ cudaError_t run_grad(const FfnGradArgs& a, cudaStream_t s) {
   p.tiles = (int)tiles;
   p.next = a.next;
   const int pairs = tiles < a.pairs ? (int)tiles : a.pairs;
-  maps.set<T>(&p.a[0], a.dg, a.rows, a.inner, a.inner, 64, 64);
-  maps.set<T>(&p.a[1], a.du, a.rows, a.inner, a.inner, 64, 64);
+  maps.set<T>(&p.a[0], a.dg, a.rows, a.inner, a.inner, 64);
+  maps.set<T>(&p.a[1], a.du, a.rows, a.inner, a.inner, 64);
   p.a2[0] = p.a[0];
   p.a2[1] = p.a[1];
-  maps.set<T>(&p.b[0], a.wg, a.inner, a.hidden, a.ldw, 64, 64);
-  maps.set<T>(&p.b[1], a.wu, a.inner, a.hidden, a.ldw, 64, 64);
-  maps.set<T>(&p.b2, a.x, a.rows, a.hidden, a.ldx, 64, 64);
-  if (a.dx) maps.set<T>(&p.out[0], a.dx, a.rows, a.hidden, a.lddx, kChunk, 32);
-  if (a.dwg) {
-    maps.set<T>(&p.out[1], a.dwg, a.inner, a.hidden, a.lddw, kChunk, 32);
-    maps.set<T>(&p.out[2], a.dwu, a.inner, a.hidden, a.lddw, kChunk, 32);
-  }
+  maps.set<T>(&p.b[0], a.wg, a.inner, a.hidden, a.ldw, 64);
+  maps.set<T>(&p.b[1], a.wu, a.inner, a.hidden, a.ldw, 64);
+  maps.set<T>(&p.b2, a.x, a.rows, a.hidden, a.ldx, 64);
+  p.out[0] = a.dx;
+  p.out[1] = a.dwg;
+  p.out[2] = a.dwu;
+  p.ld[0] = a.lddx;
+  p.ld[1] = p.ld[2] = a.lddw;
   if (maps.error != cudaSuccess) return maps.error;
   e = launch_products<T, AQ_ACT_SILU, true>(p, pairs, s);
   if (e != cudaSuccess || !p.partial) return e;
