@@ -152,11 +152,9 @@ __device__ void sums_read(uint32_t (&r)[32]) {
                :
                : "memory");
 }
-__device__ void write_shared(uint32_t at, uint4 v) { asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); }
-__device__ uint4 read_shared(uint32_t at) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-  return v;
+// 32 aligned bytes
+__device__ void write_sector(void* to, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
 }
 __device__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -168,14 +166,13 @@ __device__ void pair_sync() {
 // ---- the kernel --------------------------------------------------------------------------------------------------
 
 constexpr int kDeep = 64;                     // depth of a stage: 128 bytes, one swizzled row
-constexpr int kStages = 6;
+constexpr int kStages = 7;
 constexpr int kHalfTile = 128 * kDeep * 2;    // bytes of one CTA's share of A (or B) of a stage
 constexpr int kEpilogueWarps = 8;
 constexpr int kFfnThreads = 128 + 32 * kEpilogueWarps;
 constexpr int kChunk = 32;                    // columns an epilogue warp takes at a time
-constexpr int kOutBytes = 32 * kChunk * 4;    // ... of 32 rows, on their way out
 constexpr int kColumns = 512;                 // tensor memory: two tiles' sums of up to 256 columns
-constexpr int kSharedBytes = 1024 + kStages * 2 * kHalfTile + kEpilogueWarps * kOutBytes;
+constexpr int kSharedBytes = 1024 + kStages * 2 * kHalfTile;
 constexpr int kMaxPairs = 128;
 
 constexpr int kClasses = 2;                   // kinds of tiles of one launch: dx and dW
@@ -191,6 +188,7 @@ struct Products {
   CUtensorMap a2[2], b2;                      // dW: dg and du across their rows, x
   void* out[3];                               // forward: h, g, u; backward: dx, dWg, dWu
   long long ld[3];
+  int sectors[3];                             // its rows begin on 32-byte boundaries
   int k_total;                                // stages of the whole depth of forward and dx
   int rows[2], cols[2];                       // of the outputs
   int save;                                   // forward: write g and u
@@ -251,7 +249,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
   __shared__ __align__(8) uint64_t barriers[2 * kStages + 9];
   __shared__ uint32_t tensor_base, tile_ids[2];
   const uint32_t base = (shared_address(shared_raw) + 1023u) & ~1023u;
-  const uint32_t out_base = base + kStages * 2 * kHalfTile;
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   const uint32_t rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const uint32_t bars = shared_address(barriers);
@@ -400,42 +397,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
     }
   } else if (warp >= 4) {
     const int quarter = warp & 3, turn = (warp - 4) / 4;
-    const uint32_t out_buf = out_base + (uint32_t)(warp - 4) * kOutBytes;
     int acc = 0;
     uint32_t acc_phase = 0;
-    // 32 rows x 32 columns, each lane a row, to (y, x) of an output: turned round in shared memory, so that a store covers
-    // whole 64-byte (binary32: 128-byte) stretches of rows.  (TMA stores from there took 1000 cycles each to give their buffer
-    // back: 8600 cycles a tile of three outputs with two buffers.)
+    // 32 rows x 32 columns, each lane a row, to (y, x) of an output: 32 bytes (one sector) a store where the output is aligned
+    // for that.  Turning the tile round in shared memory first, for stores along rows or by TMA, took longer beside the products,
+    // whose operands fill that memory's bandwidth (1200 to 1700 cycles for 32 x 32 values of a warp, 800 to 1200 as here), and
+    // took a stage's room.
     auto put16 = [&](const uint32_t (&v)[32], int out, int problem, int x, int y) {
+      const int row = y + lane;
+      if (row >= p.rows[problem]) return;
+      T* const to = static_cast<T*>(p.out[out]) + (long long)row * p.ld[out] + x;
+      uint32_t w[16];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {                       // the 16-byte pieces of a row swizzled over eight rows' worth of banks
-        const float* const f = reinterpret_cast<const float*>(&v[8 * j]);
-        write_shared(out_buf + (uint32_t)lane * 64u + (uint32_t)((j ^ ((lane >> 1) & 3)) * 16),
-                     make_uint4(Num<T>::close(f[0], f[1]), Num<T>::close(f[2], f[3]), Num<T>::close(f[4], f[5]), Num<T>::close(f[6], f[7])));
-      }
-      __syncwarp();
-      T* const to = static_cast<T*>(p.out[out]) + (long long)(y + lane / 4) * p.ld[out] + x + (lane & 3) * 8;
+      for (int j = 0; j < 16; ++j) w[j] = Num<T>::close(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+      if (p.sectors[out] && x + kChunk <= p.cols[problem]) {
+        write_sector(to, w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]);
+        write_sector(to + 16, w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]);
+      } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int row = j * 8 + lane / 4;
-        const uint4 w = read_shared(out_buf + (uint32_t)row * 64u + (uint32_t)(((lane & 3) ^ ((row >> 1) & 3)) * 16));
-        if (y + row < p.rows[problem] && x + (lane & 3) * 8 < p.cols[problem]) *reinterpret_cast<uint4*>(to + j * 8 * p.ld[out]) = w;
+        for (int j = 0; j < 4; ++j)
+          if (x + j * 8 < p.cols[problem]) *reinterpret_cast<uint4*>(to + j * 8) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
       }
-      __syncwarp();
     };
     auto put32 = [&](const uint32_t (&v)[32], float* out, int x, int y) {
+      const int row = y + lane;
+      if (row >= p.rows[0]) return;
+      float* const to = out + (long long)row * p.cols[0] + x;
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        write_shared(out_buf + (uint32_t)lane * 128u + (uint32_t)((j ^ (lane & 7)) * 16), make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
-      __syncwarp();
-      float* const to = out + (long long)(y + lane / 8) * p.cols[0] + x + (lane & 7) * 4;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int row = j * 4 + lane / 8;
-        const uint4 w = read_shared(out_buf + (uint32_t)row * 128u + (uint32_t)(((lane & 7) ^ (row & 7)) * 16));
-        if (y + row < p.rows[0] && x + (lane & 7) * 4 < p.cols[0]) *reinterpret_cast<uint4*>(to + (long long)j * 4 * p.cols[0]) = w;
-      }
-      __syncwarp();
+      for (int j = 0; j < 4; ++j)                         // cols is a multiple of 8
+        if (x + j * 8 < p.cols[0]) write_sector(to + j * 8, v[8 * j], v[8 * j + 1], v[8 * j + 2], v[8 * j + 3], v[8 * j + 4], v[8 * j + 5], v[8 * j + 6], v[8 * j + 7]);
     };
     Tile t;
     for (int i = 0; next_tile(i, &t); ++i) {
@@ -713,7 +703,8 @@ cudaError_t launch(void (*kernel)(Params...), unsigned ctas, unsigned threads, s
 }
 
 template <typename T, int ACT, bool BACKWARD>
-cudaError_t launch_products(const Products& p, int pairs, cudaStream_t s) {
+cudaError_t launch_products(Products& p, int pairs, cudaStream_t s) {
+  for (int i = 0; i < 3; ++i) p.sectors[i] = (reinterpret_cast<uintptr_t>(p.out[i]) & 31) == 0 && p.ld[i] % 16 == 0;
   auto kernel = products_kernel<T, ACT, BACKWARD>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
   return e != cudaSuccess ? e : launch(kernel, 2u * pairs, kFfnThreads, kSharedBytes, s, p);

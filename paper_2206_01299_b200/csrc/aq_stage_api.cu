@@ -281,7 +281,7 @@ int aq_gated_ffn_grad(aq_stage* st, const void* dh, int64_t lddh, const void* x,
   AQ_TRY(check_matrix(st, who, "u", u, ldgu, inner));
   if (dx) AQ_TRY(check_matrix(st, who, "dx", dx, lddx, hidden));
   if (!dx && !dwg) return AQ_OK;
-  const size_t half = (size_t)rows * (size_t)inner * 2;      // a multiple of 16 bytes
+  const size_t half = ((size_t)rows * (size_t)inner * 2 + 255) & ~(size_t)255;
   aq::FfnGradArgs a{dh, lddh, x, ldx, wg, wu, ldw, g, u, ldgu, rows, hidden, inner, act, dx, lddx, dwg, dwu, lddw,
                     nullptr, nullptr, nullptr, st->status, st->next, st->sms, st->pairs};
   AQ_TRY(ensure_work(st, 2 * half + (size_t)aq::ffn_grad_partial_bytes(a)));
