@@ -8,7 +8,7 @@ CSRC = os.path.join(HERE, "csrc")
 CODEC_SOURCES = [os.path.join(CSRC, f) for f in ("aq_api.cu", "aq_kernels.cu", "aq_lowbit.cu", "aq_anygroup.cu", "aq_noalloc.cu")]
 STAGE_SOURCES = [os.path.join(CSRC, f) for f in ("aq_stage_api.cu", "aq_logprob.cu", "aq_qknorm.cu", "aq_ffn.cu")]
 SOURCES = CODEC_SOURCES + STAGE_SOURCES
-HEADERS = [os.path.join(CSRC, "aq_internal.h"), os.path.join(CSRC, "aq_device.cuh"), os.path.join(CSRC, "aq_stage.h"),
+HEADERS = [os.path.join(CSRC, "aq_internal.h"), os.path.join(CSRC, "aq_device.cuh"), os.path.join(CSRC, "aq_stage.h"), os.path.join(CSRC, "aq_stage_device.cuh"),
            os.path.join(os.path.dirname(HERE), "include", "aq_b200.h")]
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libaq_b200.so")

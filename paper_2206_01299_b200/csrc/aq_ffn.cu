@@ -13,29 +13,21 @@
 //   dW        A = dg (du) read across its rows (M-major), B = x N-major: the sum runs over the tokens
 
 #include <cuda.h>
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
 
-#include "../../include/aq_b200.h"
 #include "aq_stage.h"
+#include "aq_stage_device.cuh"
 
 namespace aq {
 namespace {
 
-template <typename T> struct Num;
-template <> struct Num<__half> {
+template <typename T> struct Operand;        // how the tensor cores and TMA name a type
+template <> struct Operand<__half> {
   static constexpr CUtensorMapDataType kMap = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   static constexpr uint32_t kFormat = 0;
-  static __device__ __half one(float x) { return __float2half_rn(x); }
-  static __device__ float2 open(uint32_t u) { return __half22float2(*reinterpret_cast<__half2*>(&u)); }
-  static __device__ uint32_t close(float a, float b) { const __half2 p = __floats2half2_rn(a, b); return *reinterpret_cast<const uint32_t*>(&p); }
 };
-template <> struct Num<__nv_bfloat16> {
+template <> struct Operand<__nv_bfloat16> {
   static constexpr CUtensorMapDataType kMap = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   static constexpr uint32_t kFormat = 1;
-  static __device__ __nv_bfloat16 one(float x) { return __float2bfloat16_rn(x); }
-  static __device__ float2 open(uint32_t u) { return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)); }
-  static __device__ uint32_t close(float a, float b) { const __nv_bfloat162 p = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t*>(&p); }
 };
 
 // Phi(-|g|), the normal distribution's tail: e^(-g^2/2) times a polynomial in t = 1 / (1 + 0.375 |g| / sqrt(2)), fitted to
@@ -74,51 +66,13 @@ template <int ACT> __device__ void activation(float g, float* a, float* da) {
 
 // ---- instructions ------------------------------------------------------------------------------------------------
 
-__device__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ void barrier_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
-__device__ void barrier_expect(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 // four bytes into the shared memory of either CTA, counted by that CTA's barrier
 __device__ void send(uint32_t to, uint32_t value, uint32_t bar) {
   asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];" ::"r"(to), "r"(value), "r"(bar) : "memory");
 }
 __device__ uint32_t in_cta(uint32_t addr, uint32_t rank) { uint32_t r; asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank)); return r; }
 __device__ void barrier_arrive_remote(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
-constexpr uint32_t kSleepNs = 100000;         // how long a try may sleep: a thread that polls takes issue slots and power from the products
-__device__ bool barrier_try(uint32_t bar, uint32_t parity) {
-  uint32_t done;
-  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity), "r"(kSleepNs) : "memory");
-  return done != 0;
-}
-__device__ unsigned long long now_ns() { unsigned long long t; asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t)); return t; }
-// Waits for a phase; false (and the status bit) when it has not come within four seconds: the caller leaves its loop.
-__device__ __noinline__ bool barrier_wait_long(uint32_t bar, uint32_t parity, uint32_t* status) {
-  const unsigned long long until = now_ns() + 4000000000ull;
-  do {
-    for (int i = 0; i < 64; ++i)
-      if (barrier_try(bar, parity)) return true;
-  } while (now_ns() < until);
-  atomicOr(status, (uint32_t)AQ_ST_STALLED);
-  return false;
-}
-__device__ bool barrier_wait(uint32_t bar, uint32_t parity, uint32_t* status) {
-#pragma unroll 1
-  for (int i = 0; i < 16; ++i)
-    if (barrier_try(bar, parity)) return true;
-  return barrier_wait_long(bar, parity, status);
-}
 __device__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
-// programmatic launch: the next kernel of the stream may be placed; the results of the previous one are needed from here
-__device__ void next_may_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-// one lane waits for its warp
-__device__ bool warp_wait(int lane, uint32_t bar, uint32_t parity, uint32_t* status) {
-  int ok = 1;
-  if (lane == 0) ok = barrier_wait(bar, parity, status);
-  return __shfl_sync(0xffffffffu, ok, 0) != 0;
-}
 // a box of this GPU's memory into this CTA's shared memory, counted by the first CTA's barrier
 __device__ void load_box(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
@@ -652,7 +606,7 @@ struct Maps {
     if (error != cudaSuccess) return;
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
     const cuuint32_t box[2] = {kDeep, (cuuint32_t)box_rows}, one[2] = {1, 1};
-    const CUresult r = fn(m, Num<T>::kMap, 2, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    const CUresult r = fn(m, Operand<T>::kMap, 2, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) error = cudaErrorInvalidValue;
   }
@@ -684,22 +638,6 @@ cudaError_t resident_pairs(int* pairs) {
   if (e == cudaSuccess && *pairs < 1) e = cudaErrorInvalidConfiguration;
   if (*pairs > kMaxPairs) *pairs = kMaxPairs;
   return e;
-}
-
-// A launch that may be placed while the stream's previous kernel drains (the kernels wait for its results themselves).
-template <typename... Params, typename... Args>
-cudaError_t launch(void (*kernel)(Params...), unsigned ctas, unsigned threads, size_t shared, cudaStream_t s, Args... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(ctas);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = shared;
-  cfg.stream = s;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 template <typename T, int ACT, bool BACKWARD>
@@ -735,7 +673,7 @@ cudaError_t run(const FfnArgs& a, cudaStream_t s) {
   p.rows[0] = (int)a.rows;
   p.cols[0] = a.inner;
   p.save = a.g != nullptr;
-  p.format = Num<T>::kFormat;
+  p.format = Operand<T>::kFormat;
   p.status = a.status;
   Maps maps;
   maps.set<T>(&p.a[0], a.x, a.rows, a.hidden, a.ldx, 128);
@@ -827,7 +765,7 @@ cudaError_t run_grad(const FfnGradArgs& a, cudaStream_t s) {
   const Plan plan = plan_of(a);
   Products p{};
   Maps maps;
-  p.format = Num<T>::kFormat;
+  p.format = Operand<T>::kFormat;
   p.status = a.status;
   p.k_total = 2 * ceil_div(a.inner, kDeep);
   p.rows[0] = (int)a.rows;

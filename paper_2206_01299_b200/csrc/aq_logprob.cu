@@ -9,12 +9,10 @@
 // costs no digits.
 
 #include <cooperative_groups.h>
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
 #include <math_constants.h>
 
-#include "../../include/aq_b200.h"
 #include "aq_stage.h"
+#include "aq_stage_device.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -23,6 +21,7 @@ namespace {
 
 constexpr int kRowThreads = 256;
 constexpr int kRowWarps = kRowThreads / 32;
+constexpr int kRowCtas = 7;                   // CTAs on a multiprocessor: registers for it are cut to 36 a thread
 constexpr int kGroups = kRowThreads / 4;      // four neighbouring threads share one maximum for the alternatives
 constexpr int kCandidates = 1024;             // logits that may tie with or beat the threshold before the slow way is taken
 static_assert(kGroups >= kMaxTop, "the threshold needs as many group maxima as alternatives");
@@ -31,70 +30,76 @@ static_assert(kCluster * kMaxTop <= kCandidates, "the lists of a cluster are mer
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLog2eRest = 1.925963e-8f;    // log2(e) - kLog2e
-constexpr float kUnset = -1e38f;              // reference before the first finite value
+constexpr float kUnset = -1e6f;               // reference before the first larger value: what lies below it adds 0
 constexpr float kGone = -1e4f;                // exponents below give exactly 0; also keeps 0 * -infinity out of t
-constexpr float kFar = 1e7f;                  // largest |y| whose rounding (half a unit there) the sums take in their stride
+constexpr float kClear = 200.0f;              // exponentials this far below the largest are 0 in binary32 sums
+constexpr float kFar = 1e6f;                  // largest |y| of a row's maximum that the sums take in their stride: its rounding is 1/32 there
 constexpr float kSlack = 8.0f;                // how far a value may exceed the reference before it is moved: 2^8 is
                                               // nothing to a binary32 sum, and the move leaves the loop's common path
 
-// 16 bytes of logits.
+__device__ float warp_max(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ float warp_sum(float x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+__device__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+// max(x, bound) that keeps a NaN
+__device__ float at_least(float x, float bound) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(bound)); return y; }
+
+// 16 bytes of logits.  So that nothing is ever infinity times 0, masked ones (-infinity, or anything below kLow) are raised to
+// kLow first where that takes half an instruction each (fp16): their exponentials stay 0 as long as the row's largest logit is
+// far above.  Elsewhere kLow is -infinity and the exponents are held at kGone.  NaNs stay either way.
 template <typename T> struct Pack;
 template <> struct Pack<float> {
   static constexpr int N = 4;
-  static __device__ float top(uint4 v) {
-    return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
-  }
+  static constexpr float kLow = -__builtin_huge_valf();
+  static __device__ void raise(uint32_t (&)[4]) {}
+  static __device__ float held(float d) { return at_least(d, kGone); }
+  static __device__ uint32_t larger(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+  static __device__ float largest(uint32_t a) { return __uint_as_float(a); }
+  static __device__ float2 open2(const uint32_t (&w)[4], int i) { return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1])); }
   static __device__ void open(uint4 v, float* f) { f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w); }
   static __device__ uint4 close(const float* f) { return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])); }
   static __device__ float one(float x) { return x; }
   static __device__ float round(float x) { return x; }
 };
-template <> struct Pack<__half> {
+template <typename T, typename T2> struct Pack16 {
   static constexpr int N = 8;
-  static __device__ __half2 h(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
-  static __device__ float top(uint4 v) {
-    const float2 f = __half22float2(__hmax2(__hmax2(h(v.x), h(v.y)), __hmax2(h(v.z), h(v.w))));
-    return fmaxf(f.x, f.y);
-  }
+  static __device__ T2 h(uint32_t u) { return *reinterpret_cast<T2*>(&u); }
+  static __device__ uint32_t u(T2 v) { return *reinterpret_cast<const uint32_t*>(&v); }
+  static __device__ uint32_t larger(uint32_t a, uint32_t b) { return u(__hmax2(h(a), h(b))); }
+  static __device__ float largest(uint32_t a) { const float2 f = Num<T>::open(a); return fmaxf(f.x, f.y); }
+  static __device__ float2 open2(const uint32_t (&w)[4], int i) { return Num<T>::open(w[i]); }
   static __device__ void open(uint4 v, float* f) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { const float2 p = __half22float2(h(w[i])); f[2 * i] = p.x; f[2 * i + 1] = p.y; }
+    for (int i = 0; i < 4; ++i) { const float2 p = Num<T>::open(w[i]); f[2 * i] = p.x; f[2 * i + 1] = p.y; }
   }
   static __device__ uint4 close(const float* f) {
-    uint32_t w[4];
+    return make_uint4(Num<T>::close(f[0], f[1]), Num<T>::close(f[2], f[3]), Num<T>::close(f[4], f[5]), Num<T>::close(f[6], f[7]));
+  }
+  static __device__ T round(float x) { return Num<T>::one(x); }
+};
+template <> struct Pack<__half> : Pack16<__half, __half2> {
+  static constexpr float kLow = -65504.0f;
+  static __device__ float held(float d) { return d; }
+  static __device__ void raise(uint32_t (&w)[4]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { const __half2 p = __floats2half2_rn(f[2 * i], f[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&p); }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < 4; ++i) w[i] = u(__hmax2_nan(h(w[i]), h(0xfbfffbffu)));
   }
   static __device__ float one(__half x) { return __half2float(x); }
-  static __device__ __half round(float x) { return __float2half_rn(x); }
 };
-template <> struct Pack<__nv_bfloat16> {
-  static constexpr int N = 8;
-  static __device__ __nv_bfloat162 h(uint32_t u) { return *reinterpret_cast<__nv_bfloat162*>(&u); }
-  static __device__ float top(uint4 v) {
-    const float2 f = __bfloat1622float2(__hmax2(__hmax2(h(v.x), h(v.y)), __hmax2(h(v.z), h(v.w))));
-    return fmaxf(f.x, f.y);
-  }
-  static __device__ void open(uint4 v, float* f) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-  }
-  static __device__ uint4 close(const float* f) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&p); }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-  }
+template <> struct Pack<__nv_bfloat16> : Pack16<__nv_bfloat16, __nv_bfloat162> {
+  static constexpr float kLow = -__builtin_huge_valf();
+  static __device__ void raise(uint32_t (&)[4]) {}
+  static __device__ float held(float d) { return at_least(d, kGone); }
   static __device__ float one(__nv_bfloat16 x) { return __bfloat162float(x); }
-  static __device__ __nv_bfloat16 round(float x) { return __float2bfloat16_rn(x); }
 };
-
-__device__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-// max(x, bound) that keeps a NaN
-__device__ float at_least(float x, float bound) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(bound)); return y; }
 
 struct Sums {
   float m = kUnset, s = 0.0f, t = 0.0f;
@@ -109,14 +114,38 @@ struct Sums {
     s += e;
     t = fmaf(e, d, t);
   }
-  __device__ void join(float m2, float s2, float t2) {
+};
+
+// The same while a thread reads: even and odd elements apart.
+struct Sums2 {
+  float m = kUnset, s0 = 0.0f, s1 = 0.0f, t0 = 0.0f, t1 = 0.0f;
+  // one or more raised vectors whose largest element is `here`
+  template <typename T, int COUNT>
+  __device__ void add(const uint32_t (&w)[COUNT][4], float here, float c) {
+    if (here * c > m + kSlack) {
+      const float d = fmaxf(m - here * c, kGone), e = exp2_fast(d);
+      t0 = fmaf(s0, d, t0) * e;
+      t1 = fmaf(s1, d, t1) * e;
+      s0 *= e;
+      s1 *= e;
+      m = here * c;
+    }
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i)
+#pragma unroll
+      for (int j = 0; j < Pack<T>::N / 2; ++j) {
+        const float2 v = Pack<T>::open2(w[i], j);
+        const float d0 = Pack<T>::held(fmaf(v.x, c, -m)), d1 = Pack<T>::held(fmaf(v.y, c, -m)), e0 = exp2_fast(d0), e1 = exp2_fast(d1);
+        s0 += e0;
+        s1 += e1;
+        t0 = fmaf(e0, d0, t0);
+        t1 = fmaf(e1, d1, t1);
+      }
+  }
+  __device__ Sums whole() const {
     Sums o;
-    o.m = m2; o.s = s2; o.t = t2;
-    const float to = fmaxf(m, m2);
-    move_to(to);
-    o.move_to(to);
-    s += o.s;
-    t += o.t;
+    o.m = m; o.s = s0 + s1; o.t = t0 + t1;
+    return o;
   }
 };
 
@@ -131,16 +160,21 @@ __device__ float value_of(unsigned long long key) {
   return __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
 }
 
+// What the CTAs of a row send to the first of them: sums, largest logit and alternatives.
+struct FromCta {
+  float m, s, t, top;
+  unsigned long long list[kMaxTop];
+};
+
 struct RowShared {
   float m[kRowWarps], s[kRowWarps], t[kRowWarps], top[kRowWarps];
   float group_top[kGroups];
   int groups[kGroups];
   int n_groups, n_found;
-  float threshold;
+  float threshold, row_s, row_top;
   unsigned long long best[kRowWarps];
   unsigned long long found[kCandidates];
   unsigned long long list[kMaxTop];          // this CTA's alternatives, falling
-  float cta_m, cta_s, cta_t, cta_top;        // this CTA's sums and largest logit
 };
 
 // The part of a row that one CTA reads: `head` elements up to the first 16-byte boundary, whole vectors, `tail`
@@ -176,67 +210,85 @@ template <typename T> struct Part {
   }
 };
 
-// The k largest of sh.found[0..n) (unique keys) to sh.list, falling; missing places 0.
+// The k largest of sh.found[0..n) (unique keys) to sh.list, falling; missing places 0.  One warp.
 __device__ void select_found(RowShared& sh, int n, int k) {
-  const int tid = threadIdx.x;
-  if (tid < k) sh.list[tid] = 0ull;
-  __syncthreads();
-  for (int i = tid; i < n; i += kRowThreads) {
+  const int lane = threadIdx.x & 31;
+  if (lane < k) sh.list[lane] = 0ull;
+  __syncwarp();
+  for (int i = lane; i < n; i += 32) {
     const unsigned long long mine = sh.found[i];
     int rank = 0;
     for (int j = 0; j < n; ++j) rank += sh.found[j] > mine;
     if (rank < k && mine) sh.list[rank] = mine;
   }
-  __syncthreads();
+  __syncwarp();
 }
 
-// This CTA's k alternatives to sh.list.  The k-th largest of the 64 group maxima is a lower bound of the k-th
-// largest logit, and only groups whose maximum reaches it can hold one: about k of them, whose elements are read
-// again (from L2) and compared.  Measured beside the pass that needs the maxima anyway, this is what keeps the
-// alternatives nearly free; a sorted list in every thread would cost the loop a compare and a branch per element.
+// The k-th largest of the group maxima, and the groups that reach it.  One warp, two groups a lane.
 template <typename T>
-__device__ void alternatives(RowShared& sh, const Part<T>& part, float my_top, int k) {
-  constexpr int N = Pack<T>::N;
-  const int tid = threadIdx.x;
-  float g = fmaxf(my_top, __shfl_xor_sync(0xffffffffu, my_top, 1));
-  g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
-  if ((tid & 3) == 0) sh.group_top[tid >> 2] = g;
-  if (tid == 0) { sh.n_groups = 0; sh.n_found = 0; }
-  __syncthreads();
-  if (tid < kGroups) {
-    const float mine = sh.group_top[tid];
-    int rank = 0;
-    for (int j = 0; j < kGroups; ++j) { const float o = sh.group_top[j]; rank += o > mine || (o == mine && j < tid); }
-    if (rank == k - 1) sh.threshold = mine;
+__device__ void find_groups(RowShared& sh, int k) {
+  static_assert(kGroups == 64, "two groups a lane");
+  const int lane = threadIdx.x & 31;
+  const float g0 = sh.group_top[lane], g1 = sh.group_top[lane + 32];
+  float v0 = g0, v1 = g1, threshold = -CUDART_INF_F;
+  for (int i = 0; i < k; ++i) {                    // takes the largest away, k times
+    const float largest = fmaxf(v0, v1);
+    threshold = warp_max(largest);
+    if (threshold <= Pack<T>::kLow) break;         // masked logits were raised to kLow
+    const unsigned have = __ballot_sync(0xffffffffu, largest == threshold);
+    if (lane == __ffs(have) - 1) { if (v0 == threshold) v0 = -CUDART_INF_F; else v1 = -CUDART_INF_F; }
   }
-  __syncthreads();
+  if (threshold <= Pack<T>::kLow) threshold = -CUDART_INF_F;
+  const unsigned in0 = __ballot_sync(0xffffffffu, g0 >= threshold), in1 = __ballot_sync(0xffffffffu, g1 >= threshold), below = (1u << lane) - 1u;
+  if (g0 >= threshold) sh.groups[__popc(in0 & below)] = lane;
+  if (g1 >= threshold) sh.groups[__popc(in0) + __popc(in1 & below)] = lane + 32;
+  if (lane == 0) { sh.threshold = threshold; sh.n_groups = __popc(in0) + __popc(in1); sh.n_found = 0; }
+}
+
+// The logits of this warp's share of those groups, read again, that reach the threshold.
+template <typename T>
+__device__ void collect(RowShared& sh, const Part<T>& part) {
+  constexpr int N = Pack<T>::N, U = 4;
+  const int tid = threadIdx.x, lane = tid & 31, rounds = (part.n_vec + kRowThreads - 1) / kRowThreads;
   const float threshold = sh.threshold;
-  if (tid < kGroups && sh.group_top[tid] >= threshold) sh.groups[atomicAdd(&sh.n_groups, 1)] = tid;
-  __syncthreads();
-  const int n_groups = sh.n_groups, rounds = (part.n_vec + kRowThreads - 1) / kRowThreads;
   auto offer = [&](float x, unsigned id) {
-    if (x >= threshold) {
+    if (x >= threshold && x > -CUDART_INF_F) {
       const int at = atomicAdd(&sh.n_found, 1);
       if (at < kCandidates) sh.found[at] = key_of(x, id);
     }
   };
-  for (long long w = tid; w < 4ll * n_groups * rounds; w += kRowThreads) {
-    const int rest = (int)(w >> 2), v = (rest / n_groups) * kRowThreads + sh.groups[rest % n_groups] * 4 + (int)(w & 3);
-    if (v < part.n_vec) {
-      float f[N];
-      Pack<T>::open(__ldg(part.vec + v), f);
+  const int n_groups = sh.n_groups;
+  for (int g = tid >> 5; g < n_groups; g += kRowWarps) {
+    const int first = sh.groups[g] * 4 + (lane & 3);
+    for (int r = lane >> 2; r < rounds; r += 8 * U) {          // eight rounds of the group's four threads at a time
+      uint4 v[U];
 #pragma unroll
-      for (int i = 0; i < N; ++i) offer(f[i], part.vec_first + (unsigned)v * N + i);
+      for (int i = 0; i < U; ++i) {
+        const int at = (r + 8 * i) * kRowThreads + first;
+        if (at < part.n_vec) v[i] = __ldg(part.vec + at);
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int at = (r + 8 * i) * kRowThreads + first;
+        if (at < part.n_vec) {
+          float f[N];
+          Pack<T>::open(v[i], f);
+#pragma unroll
+          for (int j = 0; j < N; ++j) offer(f[j], part.vec_first + (unsigned)at * N + j);
+        }
+      }
     }
   }
   unsigned id;
   if (part.edge(tid, &id)) offer(Pack<T>::one(part.row[id]), id);
-  __syncthreads();
-  if (sh.n_found <= kCandidates) {
-    select_found(sh, sh.n_found, k);
-    return;
-  }
-  // too many logits at or above the threshold (whole stretches of equal ones): the next largest key, k times
+}
+
+// Too many logits at or above the threshold (whole stretches of equal ones): the next largest key, k times.  The whole CTA.
+template <typename T>
+__device__ void next_largest(RowShared& sh, const Part<T>& part, int k) {
+  constexpr int N = Pack<T>::N;
+  const int tid = threadIdx.x;
+  unsigned id;
   unsigned long long below = ~0ull;
   for (int r = 0; r < k; ++r) {
     unsigned long long best = 0ull;
@@ -267,57 +319,122 @@ __device__ void alternatives(RowShared& sh, const Part<T>& part, float my_top, i
   }
 }
 
-__device__ float warp_max(float x) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-  return x;
+// Sums of a warp's lanes, relative to the largest reference among them.
+__device__ void join_lanes(Sums& a) {
+  const float to = warp_max(a.m);
+  a.move_to(to);
+  a.s = warp_sum(a.s);
+  a.t = warp_sum(a.t);
 }
 
-// One row, or one of gridDim's clusters' shares of it: kRanks CTAs to a row.
-template <typename T, int kRanks>
-__global__ void __launch_bounds__(kRowThreads) logprob_kernel(const LogprobArgs a) {
+// Whether the sums of a pass do not stand: logits so large that rounding the reference already moves it by whole units, or so
+// low (all of them masked, perhaps) that raising the masked ones to kLow would show.
+template <typename T> __device__ bool far(float top, float s, float c) {
+  if (top == -CUDART_INF_F && s == 0.0f) return false;         // nothing but -infinity
+  return fabsf(top) * c > kFar || (Pack<T>::kLow > -CUDART_INF_F && (top - Pack<T>::kLow) * c < kClear);
+}
+
+// Calls f with every logit of a row; the whole CTA, `part` being all of the row.
+template <typename T, typename F> __device__ void each_logit(const Part<T>& part, F f) {
   constexpr int N = Pack<T>::N, U = 4;
+  for (int v0 = threadIdx.x; v0 < part.n_vec; v0 += U * kRowThreads) {
+    uint4 v[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) if (v0 + i * kRowThreads < part.n_vec) v[i] = __ldg(part.vec + v0 + i * kRowThreads);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (v0 + i * kRowThreads < part.n_vec) {
+        float x[N];
+        Pack<T>::open(v[i], x);
+#pragma unroll
+        for (int j = 0; j < N; ++j) f(x[j]);
+      }
+    }
+  }
+  unsigned id;
+  if (part.edge(threadIdx.x, &id)) f(Pack<T>::one(part.row[id]));
+}
+
+// The sums of such a row once more, relative to its largest logit as it stands: s, t and top to sh.  The whole CTA.
+template <typename T>
+__device__ void far_row(RowShared& sh, const Part<T>& part, float scale) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float c = scale * kLog2e;
+  float top = -CUDART_INF_F, s = 0.0f, t = 0.0f;
+  each_logit(part, [&](float x) { top = fmaxf(top, x); });
+  top = warp_max(top);
+  __syncthreads();
+  if (lane == 0) sh.top[warp] = top;
+  __syncthreads();
+  top = warp_max(lane < kRowWarps ? sh.top[lane] : -CUDART_INF_F);
+  const bool empty = scale * top == -CUDART_INF_F;             // NaNs apart, which the sum is to show
+  each_logit(part, [&](float x) {
+    if (empty && x == x) return;
+    const float d = at_least((x - top) * c, kGone), e = exp2_fast(d);
+    s += e;
+    t = fmaf(e, d, t);
+  });
+  s = warp_sum(s);
+  t = warp_sum(t);
+  __syncthreads();
+  if (lane == 0) { sh.top[warp] = top; sh.s[warp] = s; sh.t[warp] = t; sh.m[warp] = 0.0f; }
+  __syncthreads();
+}
+
+// COUNT vectors of a thread
+template <typename T, int COUNT>
+__device__ void take(uint32_t (&w)[COUNT][4], Sums2& sums, float& top, float c) {
+  uint32_t large = 0;
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i) {
+    Pack<T>::raise(w[i]);
+    const uint32_t l = Pack<T>::larger(Pack<T>::larger(w[i][0], w[i][1]), Pack<T>::larger(w[i][2], w[i][3]));
+    large = i ? Pack<T>::larger(large, l) : l;
+  }
+  const float here = Pack<T>::largest(large);
+  top = fmaxf(top, here);
+  sums.template add<T, COUNT>(w, here, c);
+}
+
+// One row to a CTA, or (few rows) to a cluster of kRanks, each with its share of it; the first one joins what they send it.
+// The alternatives: the k-th largest of the 64 maxima of four neighbouring threads is a lower bound of the k-th
+// largest logit, and only groups whose maximum reaches it can hold one: about k of them, whose elements are read again (from
+// L2) and compared.  The pass itself needs the maxima anyway, so that the alternatives cost it nothing; a sorted list in every
+// thread would cost a compare and a branch per element.  What follows the pass is left to one warp where it can be: done by
+// all eight it was as many instructions as the pass.
+template <typename T, int kRanks>
+__global__ void __launch_bounds__(kRowThreads, kRanks > 1 ? 1 : kRowCtas) logprob_kernel(const LogprobArgs a) {
+  constexpr int U = 4;
   __shared__ RowShared sh;
-  const int tid = threadIdx.x;
+  __shared__ FromCta from[kRanks];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  next_may_launch();
+  wait_for_previous();
   const unsigned rank = kRanks > 1 ? blockIdx.x % kRanks : 0;
   const long long row = blockIdx.x / kRanks;
   const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
   const Part<T> part(x, (unsigned)a.vocab, rank, kRanks);
   const float c = a.scale * kLog2e;
+  if constexpr (kRanks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
 
-  Sums acc;
-  float top = -CUDART_INF_F;
+  Sums2 sums;
+  float top = Pack<T>::kLow;
   for (int v0 = tid; v0 < part.n_vec; v0 += U * kRowThreads) {
-    uint4 v[U];
-    float f[N];
     if (v0 + (U - 1) * kRowThreads < part.n_vec) {
+      uint32_t w[U][4];
 #pragma unroll
-      for (int i = 0; i < U; ++i) v[i] = __ldcs(part.vec + v0 + i * kRowThreads);
-      float here = Pack<T>::top(v[0]);
-#pragma unroll
-      for (int i = 1; i < U; ++i) here = fmaxf(here, Pack<T>::top(v[i]));
-      top = fmaxf(top, here);
-      if (here * c > acc.m + kSlack) acc.move_to(here * c);
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        Pack<T>::open(v[i], f);
-#pragma unroll
-        for (int j = 0; j < N; ++j) acc.add(f[j], c);
-      }
+      for (int i = 0; i < U; ++i) { const uint4 v = __ldcs(part.vec + v0 + i * kRowThreads); w[i][0] = v.x; w[i][1] = v.y; w[i][2] = v.z; w[i][3] = v.w; }
+      take<T, U>(w, sums, top, c);
     } else {
-#pragma unroll
-      for (int i = 0; i < U - 1; ++i) {
-        if (v0 + i * kRowThreads >= part.n_vec) break;
-        v[0] = __ldcs(part.vec + v0 + i * kRowThreads);
-        const float here = Pack<T>::top(v[0]);
-        top = fmaxf(top, here);
-        if (here * c > acc.m + kSlack) acc.move_to(here * c);
-        Pack<T>::open(v[0], f);
-#pragma unroll
-        for (int j = 0; j < N; ++j) acc.add(f[j], c);
+#pragma unroll 1
+      for (int v1 = v0; v1 < part.n_vec; v1 += kRowThreads) {
+        const uint4 v = __ldcs(part.vec + v1);
+        uint32_t w[1][4] = {{v.x, v.y, v.z, v.w}};
+        take<T, 1>(w, sums, top, c);
       }
     }
   }
+  Sums acc = sums.whole();
   unsigned id;
   if (part.edge(tid, &id)) {
     const float e = Pack<T>::one(x[id]);
@@ -326,104 +443,109 @@ __global__ void __launch_bounds__(kRowThreads) logprob_kernel(const LogprobArgs 
     acc.add(e, c);
   }
 
-  const float my_top = top;
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    acc.join(__shfl_xor_sync(0xffffffffu, acc.m, o), __shfl_xor_sync(0xffffffffu, acc.s, o), __shfl_xor_sync(0xffffffffu, acc.t, o));
-  }
-  top = warp_max(top);
-  if ((tid & 31) == 0) { sh.m[tid >> 5] = acc.m; sh.s[tid >> 5] = acc.s; sh.t[tid >> 5] = acc.t; sh.top[tid >> 5] = top; }
-  __syncthreads();
-  Sums cta;
-  float cta_top = -CUDART_INF_F;
-#pragma unroll
-  for (int w = 0; w < kRowWarps; ++w) { cta.join(sh.m[w], sh.s[w], sh.t[w]); cta_top = fmaxf(cta_top, sh.top[w]); }
   const int k = a.top_k;
   if (k) {
-    if (cta_top == -CUDART_INF_F && cta.s == cta.s) {          // nothing but -infinity: the first ids
-      if (tid < k) sh.list[tid] = (unsigned)tid < part.count ? key_of(-CUDART_INF_F, part.first + tid) : 0ull;
-      __syncthreads();
-    } else {
-      alternatives(sh, part, my_top, k);
-    }
+    float g = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
+    if ((tid & 3) == 0) sh.group_top[tid >> 2] = g;
   }
-
+  join_lanes(acc);
+  top = warp_max(top);
+  if (lane == 0) { sh.m[warp] = acc.m; sh.s[warp] = acc.s; sh.t[warp] = acc.t; sh.top[warp] = top; }
+  __syncthreads();
+  if (k) {
+    if (warp == 0) find_groups<T>(sh, k);
+    __syncthreads();
+    collect(sh, part);
+    __syncthreads();
+    if (sh.n_found > kCandidates) next_largest(sh, part, k);
+  }
+  if (warp == 0) {
+    if (k && sh.n_found <= kCandidates) {
+      const int n = sh.n_found;
+      select_found(sh, n, k);
+      if (lane == 0 && n < k) {                   // fewer than k above -infinity: the first ids that hold -infinity follow
+        int at = n;
+        for (unsigned i = 0; at < k && i < part.count; ++i)
+          if (Pack<T>::one(x[part.first + i]) == -CUDART_INF_F) sh.list[at++] = key_of(-CUDART_INF_F, part.first + i);
+      }
+      __syncwarp();
+    }
+    acc = Sums();
+    if (lane < kRowWarps) { acc.m = sh.m[lane]; acc.s = sh.s[lane]; acc.t = sh.t[lane]; }
+    join_lanes(acc);
+    top = warp_max(lane < kRowWarps ? sh.top[lane] : Pack<T>::kLow);
+  }
   if constexpr (kRanks > 1) {
-    cg::cluster_group cluster = cg::this_cluster();
-    if (tid == 0) { sh.cta_m = cta.m; sh.cta_s = cta.s; sh.cta_t = cta.t; sh.cta_top = cta_top; }
-    cluster.sync();
-    if (rank == 0) {
-      for (int r = 1; r < kRanks; ++r) {
-        const RowShared* o = cluster.map_shared_rank(&sh, r);
-        cta.join(o->cta_m, o->cta_s, o->cta_t);
-        cta_top = fmaxf(cta_top, o->cta_top);
-      }
-      for (int i = tid; i < kRanks * k; i += kRowThreads) sh.found[i] = cluster.map_shared_rank(&sh, i / k)->list[i % k];
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");           // all of the row's CTAs have begun: the first one's memory is there
+    if (warp == 0) {
+      FromCta* const to = cg::this_cluster().map_shared_rank(from, 0) + rank;
+      if (lane == 0) { to->m = acc.m; to->s = acc.s; to->t = acc.t; to->top = top; }
+      if (lane < k) to->list[lane] = sh.list[lane];
+      __syncwarp();
     }
-    cluster.sync();                                            // the other CTAs' shared memory is no longer needed
-    if (rank != 0) return;
-    if (k) select_found(sh, kRanks * k, k);
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (rank != 0) return;                                     // nobody reads the memory of the others
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (warp == 0) {
+      acc = Sums();
+      if (lane < kRanks) { acc.m = from[lane].m; acc.s = from[lane].s; acc.t = from[lane].t; }
+      join_lanes(acc);
+      top = warp_max(lane < kRanks ? from[lane].top : Pack<T>::kLow);
+      if (k) {
+        for (int i = lane; i < kRanks * k; i += 32) sh.found[i] = from[i / k].list[i % k];
+        __syncwarp();
+        select_found(sh, kRanks * k, k);
+      }
+    }
   }
+  if (tid == 0) { sh.row_s = acc.s; sh.row_top = top; }
+  __syncthreads();
+  const bool again = far<T>(sh.row_top, sh.row_s, c);
+  if (again) {
+    far_row(sh, Part<T>(x, (unsigned)a.vocab, 0, 1), a.scale);
+    acc = Sums();
+    acc.m = 0.0f;
+    if (lane < kRowWarps) { acc.s = sh.s[lane]; acc.t = sh.t[lane]; }
+    acc.s = warp_sum(acc.s);
+    acc.t = warp_sum(acc.t);
+    top = sh.top[0];
+  }
+  if (warp != 0) return;
 
-  // statistics of the row
-  float ln_s, lse, entropy;
-  bool none = false;
-  if (fabsf(cta_top) * c > kFar && cta_top > -CUDART_INF_F) {
-    // logits so large that rounding the reference already moves it by whole units: once more, relative to the largest
-    float s = 0.0f, t = 0.0f;
-    if (a.scale * cta_top > -CUDART_INF_F) {
-      for (long long i = tid; i < a.vocab; i += kRowThreads) {
-        const float d = at_least((Pack<T>::one(x[i]) - cta_top) * c, kGone), e = exp2_fast(d);
-        s += e;
-        t = fmaf(e, d, t);
-      }
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) { s += __shfl_xor_sync(0xffffffffu, s, o); t += __shfl_xor_sync(0xffffffffu, t, o); }
-    __syncthreads();
-    if ((tid & 31) == 0) { sh.s[tid >> 5] = s; sh.t[tid >> 5] = t; }
-    __syncthreads();
-    s = t = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kRowWarps; ++w) { s += sh.s[w]; t += sh.t[w]; }
-    none = s == 0.0f;
-    ln_s = logf(s);
-    entropy = ln_s - kLn2 * (t / s);
-  } else {
-    none = cta.s == 0.0f;
-    ln_s = kLn2 * (log2f(cta.s) - fmaf(cta_top, c, -cta.m));
-    entropy = kLn2 * (log2f(cta.s) - cta.t / cta.s);
-  }
-  lse = fmaf(a.scale, cta_top, ln_s);
-  if (none) { lse = -CUDART_INF_F; entropy = 0.0f; }
-  if (tid == 0) {
-    if (a.lse) a.lse[row] = lse;
-    if (a.entropy) a.entropy[row] = entropy;
+  // acc is relative to the reference acc.m, or (again) to the largest logit itself
+  const float log2s = log2f(acc.s), ln_s = kLn2 * (again ? log2s : log2s - fmaf(top, c, -acc.m));
+  const bool none = acc.s == 0.0f;
+  if (lane == 0) {
+    if (a.lse) a.lse[row] = none ? -CUDART_INF_F : fmaf(a.scale, top, ln_s);
+    if (a.entropy) a.entropy[row] = none ? 0.0f : kLn2 * (log2s - acc.t / acc.s);
     if (a.targets) {
       const int32_t target = a.targets[row];
       float lp = 0.0f;
-      if (target >= 0 && target < a.vocab) lp = none ? -CUDART_INF_F : a.scale * (Pack<T>::one(x[target]) - cta_top) - ln_s;
+      if (target >= 0 && target < a.vocab) lp = none ? -CUDART_INF_F : a.scale * (Pack<T>::one(x[target]) - top) - ln_s;
       else if (target >= 0) atomicOr(a.status, (uint32_t)AQ_ST_BAD_ID);
       if (a.logprob) a.logprob[row] = lp;
     }
   }
-  if (tid < k) {
-    const unsigned long long key = sh.list[tid];
-    if (a.top_ids) a.top_ids[row * k + tid] = key ? (int32_t)id_of(key) : -1;
-    if (a.top_logprobs) a.top_logprobs[row * k + tid] = !key ? CUDART_NAN_F : none ? -CUDART_INF_F : a.scale * (value_of(key) - cta_top) - ln_s;
+  if (lane < k) {
+    const unsigned long long key = sh.list[lane];
+    if (a.top_ids) a.top_ids[row * k + lane] = key ? (int32_t)id_of(key) : -1;
+    if (a.top_logprobs) a.top_logprobs[row * k + lane] = !key ? CUDART_NAN_F : none ? -CUDART_INF_F : a.scale * (value_of(key) - top) - ln_s;
   }
 }
 
 // ---- gradient ------------------------------------------------------------------------------------------------
 
 constexpr float kFarLse = 4096.0f;            // half a unit of lse in its last place there is 1/4096
-constexpr int kGradVecs = 4;                  // 16-byte vectors per thread
+constexpr int kGradVecs = 8;                  // 16-byte vectors per thread
 
 // One piece of one row: d = scale p (A + B log2 p) and the target's term, where ln p = z - lse.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const LogprobGradArgs a, int pieces) {
   constexpr int N = Pack<T>::N;
   const int tid = threadIdx.x;
+  next_may_launch();
+  wait_for_previous();
   const long long row = blockIdx.x / (unsigned)pieces;
   const unsigned piece = blockIdx.x % (unsigned)pieces;
   const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
@@ -442,9 +564,11 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
   const float gl = target >= 0 && a.d_logprob ? a.d_logprob[row] : 0.0f;
   const float at_target = gl * a.scale;
 
-  if (!(fabsf(lse) <= kFarLse)) {
+  const float ref = lse * kLog2e;
+  if (!(fabsf(lse) <= kFarLse) || Pack<T>::kLow * c - ref > -kClear) {
     // the first piece's CTA does the whole row: zeros where the row has no distribution; else the logits are so large
-    // that lse has no digits left for ln p, and the row's own sum is formed again, relative to its largest logit
+    // that lse has no digits left for ln p (or so low or little scaled that raising the masked ones would show), and the row's own sum is
+    // formed again, relative to its largest logit
     if (piece) return;
     __shared__ float part[kRowWarps];
     float top = -CUDART_INF_F;
@@ -457,8 +581,7 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
     __syncthreads();
     float s = 0.0f;
     for (unsigned i = tid; i < vocab; i += kRowThreads) s += exp2_fast(at_least((Pack<T>::one(x[i]) - top) * c, kGone));
-#pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    s = warp_sum(s);
     if ((tid & 31) == 0) part[tid >> 5] = s;
     __syncthreads();
     s = 0.0f;
@@ -475,18 +598,12 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
   }
 
   // p = 2^(x c - lse log2(e)) with the rounding of the second product put back as a factor of the coefficients
-  const float ref = lse * kLog2e;
   const float back = exp2_fast(-fmaf(lse, kLog2eRest, fmaf(lse, kLog2e, -ref)));
   const float coef_a = -a.scale * back * fmaf(gh, entropy, gl), coef_b = -a.scale * back * gh * kLn2;
-  auto grad = [&](float v) {
-    float d;
-    if (sizeof(T) == 4) {
-      v = at_least(v, -1e36f);                                   // -infinity times c_lo could be +infinity
-      d = fmaf(v, c_lo, fmaf(v, c, -ref));
-    } else {
-      d = fmaf(v, c, -ref);
-    }
-    d = at_least(d, kGone);
+  auto grad = [&](float v) {                                      // of a raised logit
+    float d = fmaf(v, c, -ref);
+    if (sizeof(T) == 4) d = fmaf(at_least(v, -1e30f), c_lo, d);    // -infinity times c_lo could be +infinity
+    d = Pack<T>::held(d);
     return exp2_fast(d) * fmaf(coef_b, d, coef_a);
   };
   const unsigned per = kRowThreads * kGradVecs * N;
@@ -506,9 +623,14 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
       const unsigned at = v0 + i * kRowThreads;
       if (at < n_vec) {
         float f[N];
-        Pack<T>::open(v[i], f);
+        uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+        Pack<T>::raise(w);
 #pragma unroll
-        for (int j = 0; j < N; ++j) f[j] = grad(f[j]);
+        for (int j = 0; j < N / 2; ++j) {
+          const float2 x2 = Pack<T>::open2(w, j);
+          f[2 * j] = grad(x2.x);
+          f[2 * j + 1] = grad(x2.y);
+        }
         const unsigned t = (unsigned)target - head - at * N;     // target's place in this vector, if it is in it
         if (t < (unsigned)N) {
 #pragma unroll
@@ -521,33 +643,32 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
       unsigned i = 0xffffffffu;
       if ((unsigned)tid < head) i = tid;
       else if (tid >= 32 && (unsigned)(tid - 32) < tail) i = head + n_vec * N + (tid - 32);
-      if (i != 0xffffffffu) out[i] = Pack<T>::round(grad(Pack<T>::one(x[i])) + (i == (unsigned)target ? at_target : 0.0f));
+      if (i != 0xffffffffu) out[i] = Pack<T>::round(grad(at_least(Pack<T>::one(x[i]), Pack<T>::kLow)) + (i == (unsigned)target ? at_target : 0.0f));
     }
   } else {
     // rows that no common vector boundary serves: element by element
     const unsigned i0 = piece * per, i1 = min(i0 + per, vocab);
     for (unsigned i = i0 + tid; i < i1; i += kRowThreads)
-      out[i] = Pack<T>::round(grad(Pack<T>::one(x[i])) + (i == (unsigned)target ? at_target : 0.0f));
+      out[i] = Pack<T>::round(grad(at_least(Pack<T>::one(x[i]), Pack<T>::kLow)) + (i == (unsigned)target ? at_target : 0.0f));
   }
 }
 
 template <typename T>
 cudaError_t run(const LogprobArgs& a, cudaStream_t s) {
   // A row to a CTA when there are rows for half of the multiprocessors; below, a cluster of eight to a row.
-  if (a.rows * 2 >= a.sms || a.vocab < 4096) {
-    logprob_kernel<T, 1><<<(unsigned)a.rows, kRowThreads, 0, s>>>(a);
-    return cudaGetLastError();
-  }
+  if (a.rows * 2 >= a.sms || a.vocab < 4096) return launch(logprob_kernel<T, 1>, dim3((unsigned)a.rows), kRowThreads, 0, s, a);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)a.rows * kCluster);
   cfg.blockDim = dim3(kRowThreads);
   cfg.stream = s;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = kCluster;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kCluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, logprob_kernel<T, kCluster>, a);
 }
 
@@ -560,8 +681,7 @@ cudaError_t run_grad(const LogprobGradArgs& a, cudaStream_t s) {
   LogprobGradArgs b = a;
   for (long long r = 0; r < a.rows; r += most) {
     b.rows = a.rows - r < most ? a.rows - r : most;
-    logprob_grad_kernel<T><<<(unsigned)(b.rows * pieces), kRowThreads, 0, s>>>(b, (int)pieces);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch(logprob_grad_kernel<T>, dim3((unsigned)(b.rows * pieces)), kRowThreads, 0, s, b, (int)pieces);
     if (e != cudaSuccess) return e;
     b.logits = static_cast<const T*>(b.logits) + b.rows * b.ld;
     b.d_logits = static_cast<T*>(b.d_logits) + b.rows * b.ld_d;

@@ -5,103 +5,112 @@
 // (not rotated).  The gradient turns back with -sn and then, with n = x r and g = w dy,
 //   dx = r (g - n mean(g n)),   dw = sum over rows and heads of dy n.
 //
-// Bound by memory: 2 T per element forward, 3 T backward, and a position's factors once per token.  A warp takes one
-// token; the lanes of a head are the next power of two of its 16-byte pieces, so a warp holds 32 / lanes heads at a time
-// and every lane keeps the same elements of all of them: their weights and rotation factors are loaded once per token.
+// Bound by memory: 2 T per element forward, 3 T backward, and a position's factors once per token and tensor.  The lanes of a
+// head are the next power of two of its 16-byte pieces, so a warp holds 32 / lanes heads at a time (a pass) and every lane
+// keeps the same elements of all of them: their weights and factors are formed once, as a_e = w_e cos_e and
+// b_e = w_partner sn_e, and a head costs o_e = r (a_e x_e + b_e x_partner).  Partners are exchanged as they were loaded, two
+// values a word.  A warp's loads are all issued before it waits for its token's position.
 
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
-#include "../../include/aq_b200.h"
 #include "aq_stage.h"
+#include "aq_stage_device.cuh"
 
 namespace aq {
 namespace {
 
 constexpr int kQkThreads = 256, kQkWarps = kQkThreads / 32;
-constexpr int kInFlight = 4;                  // passes whose loads are issued together
+constexpr int kPasses = 8;                    // passes of a forward warp at most: its loads in flight
+constexpr int kGradPasses = 2;                // ... of a backward warp, two loads each
 
-template <typename T> struct Half2;
-template <> struct Half2<__half> {
-  static __device__ float2 open(uint32_t u) { return __half22float2(*reinterpret_cast<__half2*>(&u)); }
-  static __device__ uint32_t close(float a, float b) { const __half2 p = __floats2half2_rn(a, b); return *reinterpret_cast<const uint32_t*>(&p); }
-};
-template <> struct Half2<__nv_bfloat16> {
-  static __device__ float2 open(uint32_t u) { return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)); }
-  static __device__ uint32_t close(float a, float b) { const __nv_bfloat162 p = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t*>(&p); }
-};
 template <typename T> __device__ void open8(uint4 v, float* f) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { const float2 p = Half2<T>::open(w[i]); f[2 * i] = p.x; f[2 * i + 1] = p.y; }
+  for (int i = 0; i < 4; ++i) { const float2 p = Num<T>::open(w[i]); f[2 * i] = p.x; f[2 * i + 1] = p.y; }
 }
 template <typename T> __device__ uint4 close8(const float* f) {
-  return make_uint4(Half2<T>::close(f[0], f[1]), Half2<T>::close(f[2], f[3]), Half2<T>::close(f[4], f[5]), Half2<T>::close(f[6], f[7]));
+  return make_uint4(Num<T>::close(f[0], f[1]), Num<T>::close(f[2], f[3]), Num<T>::close(f[4], f[5]), Num<T>::close(f[6], f[7]));
 }
 
 // how a lane reaches the other members of its pairs
 enum { kPairsInLane = 0, kPairsByShuffle = 1, kPairsByShared = 2 };
 
-// One lane's view of its token: which elements of a head it holds, and their factors.
+// Which elements of a head a lane holds, and where their partners are.
 template <typename T, int W, int MODE>
 struct Lane {
   int lane, piece, slot;                      // 16-byte piece of the head; head within the pass
   bool holds;
   int partner;                                // kPairsByShuffle: lane of the pairs' other members
-  float cs[8], sn[8];
-  float* shared;                              // kPairsByShared: 256 floats of this warp
+  int half;
+  T* shared;                                  // kPairsByShared: 256 values of this warp
 
-  __device__ Lane(const QkArgs& a, float* sh) {
+  __device__ Lane(const QkArgs& a, T* sh) {
     lane = threadIdx.x & 31;
     piece = lane & (W - 1);
     slot = lane / W;
     holds = piece < a.head_dim / 8;
     shared = sh;
+    half = a.rot_dim / 2;
     const int step = a.rot_dim / 16;          // pieces between the members of a pair
     partner = lane;
     if (MODE == kPairsByShuffle && piece < 2 * step) partner = lane + (piece < step ? step : -step);
   }
-  __device__ void factors(const QkArgs& a, int position) {
+  __device__ int partner_of(const QkArgs& a, int e) const {
+    if (e >= a.rot_dim) return e;
+    return a.interleaved ? e ^ 1 : e < half ? e + half : e - half;
+  }
+  // cs, sn: factors of the lane's elements
+  __device__ void factors(const QkArgs& a, int position, float* cs, float* sn) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { cs[j] = 1.0f; sn[j] = 0.0f; }
+    const int e0 = piece * 8;
+    if (e0 >= a.rot_dim) return;
     const float* const table = a.cos_sin + (long long)position * a.rot_dim;
-    const int half = a.rot_dim / 2;
+    if (MODE == kPairsByShuffle) {            // whole pieces: eight consecutive pairs, all first or all second members
+      const bool second = e0 >= half;
+      const float4* const c = reinterpret_cast<const float4*>(table + (second ? e0 - half : e0));
+      const float4* const s = reinterpret_cast<const float4*>(table + (second ? e0 : e0 + half));
+      const float4 c0 = __ldg(c), c1 = __ldg(c + 1), s0 = __ldg(s), s1 = __ldg(s + 1);
+      const float sign = second ? 1.0f : -1.0f;
+      cs[0] = c0.x; cs[1] = c0.y; cs[2] = c0.z; cs[3] = c0.w; cs[4] = c1.x; cs[5] = c1.y; cs[6] = c1.z; cs[7] = c1.w;
+      sn[0] = sign * s0.x; sn[1] = sign * s0.y; sn[2] = sign * s0.z; sn[3] = sign * s0.w;
+      sn[4] = sign * s1.x; sn[5] = sign * s1.y; sn[6] = sign * s1.z; sn[7] = sign * s1.w;
+      return;
+    }
+    if (MODE == kPairsInLane && a.rot_dim % 8 == 0) {   // four consecutive pairs
+      const float4 c = __ldg(reinterpret_cast<const float4*>(table + e0 / 2)), s = __ldg(reinterpret_cast<const float4*>(table + half + e0 / 2));
+      cs[0] = cs[1] = c.x; cs[2] = cs[3] = c.y; cs[4] = cs[5] = c.z; cs[6] = cs[7] = c.w;
+      sn[0] = -s.x; sn[1] = s.x; sn[2] = -s.y; sn[3] = s.y; sn[4] = -s.z; sn[5] = s.z; sn[6] = -s.w; sn[7] = s.w;
+      return;
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int e = piece * 8 + j;
-      cs[j] = 1.0f;
-      sn[j] = 0.0f;
-      if (holds && e < a.rot_dim) {
-        const bool second = a.interleaved ? e & 1 : e >= half;
-        const int i = a.interleaved ? e >> 1 : second ? e - half : e;
-        cs[j] = __ldg(table + i);
-        const float s = __ldg(table + half + i);
-        sn[j] = second ? s : -s;
-      }
+      const int e = e0 + j;
+      if (e >= a.rot_dim) break;
+      const bool second = a.interleaved ? e & 1 : e >= half;
+      const int i = a.interleaved ? e >> 1 : second ? e - half : e;
+      cs[j] = __ldg(table + i);
+      const float s = __ldg(table + half + i);
+      sn[j] = second ? s : -s;
     }
   }
-  // y_e cos_e + y_partner(e) sn_e * sign
-  __device__ void rotate(const QkArgs& a, float* y, float sign) {
-    float other[8];
+  // values of the partners of a lane's elements; x: the lane's own
+  __device__ void partners(const QkArgs& a, uint4 v, const float* x, float* xp) const {
     if (MODE == kPairsInLane) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) other[j] = y[j ^ 1];
+      for (int j = 0; j < 8; ++j) xp[j] = x[j ^ 1];
     } else if (MODE == kPairsByShuffle) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) other[j] = __shfl_sync(0xffffffffu, y[j], partner);
+      uint4 o;
+      o.x = __shfl_sync(0xffffffffu, v.x, partner);
+      o.y = __shfl_sync(0xffffffffu, v.y, partner);
+      o.z = __shfl_sync(0xffffffffu, v.z, partner);
+      o.w = __shfl_sync(0xffffffffu, v.w, partner);
+      open8<T>(o, xp);
     } else {
       __syncwarp();
-#pragma unroll
-      for (int j = 0; j < 8; ++j) shared[lane * 8 + j] = y[j];
+      reinterpret_cast<uint4*>(shared)[lane] = v;
       __syncwarp();
-      const int half = a.rot_dim / 2;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int e = piece * 8 + j;
-        const int to = e >= a.rot_dim ? e : e < half ? e + half : e - half;
-        other[j] = shared[slot * W * 8 + to];
-      }
+      for (int j = 0; j < 8; ++j) xp[j] = (float)shared[slot * W * 8 + partner_of(a, piece * 8 + j)];
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = fmaf(y[j], cs[j], other[j] * (sn[j] * sign));
   }
 };
 
@@ -111,6 +120,7 @@ template <int W> __device__ float sum_over_head(float x) {
   return x;
 }
 
+// weights of the lane's elements
 template <typename T> __device__ void load_weights(const void* w, int piece, bool holds, float* f) {
   if (w && holds) {
     open8<T>(__ldg(static_cast<const uint4*>(w) + piece), f);
@@ -123,151 +133,145 @@ template <typename T> __device__ void load_weights(const void* w, int piece, boo
 // Position of a token; -1 and the status bit when it is outside the table.
 __device__ int position_of(const QkArgs& a, long long token) {
   if (!a.rot_dim) return 0;
-  const int p = a.positions[token];
+  const int p = __ldg(a.positions + token);
   if (p >= 0 && p < a.n_positions) return p;
   if ((threadIdx.x & 31) == 0) atomicOr(a.status, (uint32_t)AQ_ST_BAD_ID);
   return -1;
 }
 
-// Passes [p0, p1) over the heads of one tensor of one token.
+// blockIdx.y: a batch of `per` passes of the queries' heads (the first batches_q) or the keys'
 template <typename T, int W, int MODE>
-__device__ void forward_heads(const QkArgs& a, Lane<T, W, MODE>& l, const void* in, void* out, int heads, const float* w, bool valid, int p0, int p1) {
-  const uint4* const src = static_cast<const uint4*>(in);
-  uint4* const dst = static_cast<uint4*>(out);
-  const int pieces = a.head_dim / 8;
-  const float inv = 1.0f / (float)a.head_dim;
-  for (int p = p0; p < p1; p += kInFlight) {
-    uint4 v[kInFlight];
-#pragma unroll
-    for (int i = 0; i < kInFlight; ++i) {
-      const int head = (p + i) * (32 / W) + l.slot;
-      v[i] = make_uint4(0, 0, 0, 0);
-      if (p + i < p1 && head < heads && l.holds) v[i] = __ldcs(src + head * pieces + l.piece);
-    }
-#pragma unroll
-    for (int i = 0; i < kInFlight; ++i) {
-      if (p + i >= p1) break;
-      const int head = (p + i) * (32 / W) + l.slot;
-      float y[8], ss = 0.0f;
-      open8<T>(v[i], y);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) ss = fmaf(y[j], y[j], ss);
-      const float r = rsqrtf(fmaf(sum_over_head<W>(ss), inv, a.eps));
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] *= r * w[j];
-      l.rotate(a, y, 1.0f);
-      if (head < heads && l.holds) dst[head * pieces + l.piece] = valid ? close8<T>(y) : make_uint4(0, 0, 0, 0);
-    }
-  }
-}
-
-template <typename T, int W, int MODE>
-__global__ void __launch_bounds__(kQkThreads) qk_kernel(const QkArgs a, int splits, int passes_per_task) {
-  __shared__ float exchange[MODE == kPairsByShared ? kQkWarps * 256 : 1];
-  const long long task = (long long)blockIdx.x * kQkWarps + threadIdx.x / 32;
-  const long long token = task / splits;
+__global__ void __launch_bounds__(kQkThreads) qk_kernel(const QkArgs a, int batches_q, int per) {
+  __shared__ __align__(16) T exchange[MODE == kPairsByShared ? kQkWarps * 256 : 8];
+  constexpr int H = 32 / W;
+  const long long token = (long long)blockIdx.x * kQkWarps + threadIdx.x / 32;
+  next_may_launch();
+  wait_for_previous();
   if (token >= a.rows) return;
-  const int passes_q = (a.heads_q + 32 / W - 1) / (32 / W), passes = passes_q + (a.heads_k + 32 / W - 1) / (32 / W);
-  const int p0 = (int)(task % splits) * passes_per_task, p1 = min(p0 + passes_per_task, passes);
-  Lane<T, W, MODE> l(a, exchange + (MODE == kPairsByShared ? (threadIdx.x / 32) * 256 : 0));
+  const bool keys = (int)blockIdx.y >= batches_q;
+  const int heads = keys ? a.heads_k : a.heads_q, pieces = a.head_dim / 8;
+  const int p0 = ((int)blockIdx.y - (keys ? batches_q : 0)) * per;
+  const Lane<T, W, MODE> l(a, exchange + (MODE == kPairsByShared ? (threadIdx.x / 32) * 256 : 0));
+  const int head0 = p0 * H + l.slot, mine = l.holds ? min(per, (heads - head0 + H - 1) / H) : 0;   // heads of this lane
+  const int passes = min(per, (heads - p0 * H + H - 1) / H);
+  const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const T*>(keys ? a.k : a.q) + token * (keys ? a.k_stride : a.q_stride)) + head0 * pieces + l.piece;
+  uint4* const dst = reinterpret_cast<uint4*>(static_cast<T*>(keys ? a.k_out : a.q_out) + token * (keys ? a.k_out_stride : a.q_out_stride)) + head0 * pieces + l.piece;
+  uint4 v[kPasses];
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) v[i] = i < mine ? __ldcs(src + i * H * pieces) : make_uint4(0, 0, 0, 0);
   const int position = position_of(a, token);
-  l.factors(a, max(position, 0));
-  float w[8];
-  if (p0 < passes_q) {
-    load_weights<T>(a.wq, l.piece, l.holds, w);
-    forward_heads<T, W, MODE>(a, l, static_cast<const T*>(a.q) + token * a.q_stride, static_cast<T*>(a.q_out) + token * a.q_out_stride,
-                              a.heads_q, w, position >= 0, p0, min(p1, passes_q));
+  float fa[8], fb[8];
+  {
+    float w[8], wp[8];
+    const void* const weights = keys ? a.wk : a.wq;
+    load_weights<T>(weights, l.piece, l.holds, w);
+    if (MODE == kPairsInLane) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) wp[j] = w[j ^ 1];
+    } else if (MODE == kPairsByShuffle) {
+      load_weights<T>(weights, l.partner & (W - 1), l.holds, wp);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) wp[j] = weights && l.holds ? (float)static_cast<const T*>(weights)[l.partner_of(a, l.piece * 8 + j)] : 1.0f;
+    }
+    l.factors(a, max(position, 0), fa, fb);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { fa[j] *= w[j]; fb[j] *= wp[j]; }
   }
-  if (p1 > passes_q) {
-    load_weights<T>(a.wk, l.piece, l.holds, w);
-    forward_heads<T, W, MODE>(a, l, static_cast<const T*>(a.k) + token * a.k_stride, static_cast<T*>(a.k_out) + token * a.k_out_stride,
-                              a.heads_k, w, position >= 0, max(p0 - passes_q, 0), p1 - passes_q);
+  const float inv = 1.0f / (float)a.head_dim;
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    if (i >= passes) break;
+    float x[8], xp[8], ss = 0.0f;
+    open8<T>(v[i], x);
+    l.partners(a, v[i], x, xp);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss = fmaf(x[j], x[j], ss);
+    const float r = rsqrtf(fmaf(sum_over_head<W>(ss), inv, a.eps));
+    float o[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = r * fmaf(fa[j], x[j], fb[j] * xp[j]);
+    if (i < mine) dst[i * H * pieces] = position >= 0 ? close8<T>(o) : make_uint4(0, 0, 0, 0);
   }
 }
 
 // ---- gradient ------------------------------------------------------------------------------------------------
 
+// CTAs [0, ctas_q) take the queries' heads, the others the keys'.
 template <typename T, int W, int MODE>
-__device__ void backward_heads(const QkArgs& a, Lane<T, W, MODE>& l, const void* in, const void* grad, void* out, int heads, const float* w,
-                               float* dw, bool valid) {
-  const uint4* const src = static_cast<const uint4*>(in);
-  const uint4* const gsrc = static_cast<const uint4*>(grad);
-  uint4* const dst = static_cast<uint4*>(out);
-  const int pieces = a.head_dim / 8;
-  const float inv = 1.0f / (float)a.head_dim;
-  const int passes = (heads + 32 / W - 1) / (32 / W);
-  constexpr int U = kInFlight / 2;
-  for (int p = 0; p < passes; p += U) {
-    uint4 v[U], g[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int head = (p + i) * (32 / W) + l.slot;
-      v[i] = g[i] = make_uint4(0, 0, 0, 0);
-      if (head < heads && l.holds) { v[i] = __ldcs(src + head * pieces + l.piece); g[i] = __ldcs(gsrc + head * pieces + l.piece); }
-    }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      if (p + i >= passes) break;
-      const int head = (p + i) * (32 / W) + l.slot;
-      const bool mine = head < heads && l.holds;
-      float n[8], dy[8], ss = 0.0f, dot = 0.0f;
-      open8<T>(v[i], n);
-      open8<T>(g[i], dy);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) ss = fmaf(n[j], n[j], ss);
-      const float r = rsqrtf(fmaf(sum_over_head<W>(ss), inv, a.eps));
-      l.rotate(a, dy, -1.0f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        n[j] *= r;
-        if (mine && valid) dw[j] = fmaf(dy[j], n[j], dw[j]);
-        dy[j] *= w[j];
-        dot = fmaf(dy[j], n[j], dot);
-      }
-      const float mean = sum_over_head<W>(dot) * inv;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) dy[j] = r * (dy[j] - n[j] * mean);
-      if (mine) dst[head * pieces + l.piece] = valid ? close8<T>(dy) : make_uint4(0, 0, 0, 0);
-    }
-  }
-}
-
-template <typename T, int W, int MODE>
-__global__ void __launch_bounds__(kQkThreads) qk_grad_kernel(const QkArgs a) {
-  __shared__ float exchange[MODE == kPairsByShared ? kQkWarps * 256 : 1];
-  __shared__ float sums[kQkWarps][2][256];
+__global__ void __launch_bounds__(kQkThreads, 2) qk_grad_kernel(const QkArgs a, int ctas_q) {
+  __shared__ __align__(16) T exchange[MODE == kPairsByShared ? kQkWarps * 256 : 8];
+  __shared__ float sums[kQkWarps][256];
+  __shared__ float4 joined[kQkThreads];
   __shared__ bool last;
+  constexpr int H = 32 / W;
   const int warp = threadIdx.x / 32, tid = threadIdx.x;
-  Lane<T, W, MODE> l(a, exchange + (MODE == kPairsByShared ? warp * 256 : 0));
-  float wq[8], wk[8], dwq[8] = {}, dwk[8] = {};
-  load_weights<T>(a.wq, l.piece, l.holds, wq);
-  load_weights<T>(a.wk, l.piece, l.holds, wk);
-  for (long long token = (long long)blockIdx.x * kQkWarps + warp; token < a.rows; token += (long long)gridDim.x * kQkWarps) {
-    const int position = position_of(a, token);
-    l.factors(a, max(position, 0));
-    backward_heads<T, W, MODE>(a, l, static_cast<const T*>(a.q) + token * a.q_stride, static_cast<const T*>(a.gq) + token * a.gq_stride,
-                               static_cast<T*>(a.q_out) + token * a.q_out_stride, a.heads_q, wq, dwq, position >= 0);
-    backward_heads<T, W, MODE>(a, l, static_cast<const T*>(a.k) + token * a.k_stride, static_cast<const T*>(a.gk) + token * a.gk_stride,
-                               static_cast<T*>(a.k_out) + token * a.k_out_stride, a.heads_k, wk, dwk, position >= 0);
+  next_may_launch();
+  wait_for_previous();
+  const bool keys = (int)blockIdx.x >= ctas_q;
+  const int heads = keys ? a.heads_k : a.heads_q, pieces = a.head_dim / 8;
+  const int cta = (int)blockIdx.x - (keys ? ctas_q : 0), ctas = keys ? (int)gridDim.x - ctas_q : ctas_q;
+  const Lane<T, W, MODE> l(a, exchange + (MODE == kPairsByShared ? warp * 256 : 0));
+  float w[8], dw[8] = {};
+  load_weights<T>(keys ? a.wk : a.wq, l.piece, l.holds, w);
+  const int passes = (heads + H - 1) / H, mine = l.holds ? (heads - l.slot + H - 1) / H : 0;
+  const float inv = 1.0f / (float)a.head_dim;
+  for (long long token = (long long)cta * kQkWarps + warp; token < a.rows; token += (long long)ctas * kQkWarps) {
+    const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const T*>(keys ? a.k : a.q) + token * (keys ? a.k_stride : a.q_stride)) + l.slot * pieces + l.piece;
+    const uint4* const gsrc = reinterpret_cast<const uint4*>(static_cast<const T*>(keys ? a.gk : a.gq) + token * (keys ? a.gk_stride : a.gq_stride)) + l.slot * pieces + l.piece;
+    uint4* const dst = reinterpret_cast<uint4*>(static_cast<T*>(keys ? a.k_out : a.q_out) + token * (keys ? a.k_out_stride : a.q_out_stride)) + l.slot * pieces + l.piece;
+    float cs[8], sn[8];
+    int position = 0;
+    for (int p = 0; p < passes; p += kGradPasses) {
+      uint4 v[kGradPasses], g[kGradPasses];
+#pragma unroll
+      for (int i = 0; i < kGradPasses; ++i) {
+        const bool in = p + i < mine;
+        v[i] = in ? __ldcs(src + (p + i) * H * pieces) : make_uint4(0, 0, 0, 0);
+        g[i] = in ? __ldcs(gsrc + (p + i) * H * pieces) : make_uint4(0, 0, 0, 0);
+      }
+      if (p == 0) {
+        position = position_of(a, token);
+        l.factors(a, max(position, 0), cs, sn);
+      }
+#pragma unroll
+      for (int i = 0; i < kGradPasses; ++i) {
+        if (p + i >= passes) break;
+        float x[8], dy[8], dyp[8], ss = 0.0f, dot = 0.0f;
+        open8<T>(v[i], x);
+        open8<T>(g[i], dy);
+        l.partners(a, g[i], dy, dyp);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          dy[j] = fmaf(dy[j], cs[j], -dyp[j] * sn[j]);           // turned back
+          ss = fmaf(x[j], x[j], ss);
+          dyp[j] = dy[j] * w[j];
+          dot = fmaf(dyp[j], x[j], dot);
+        }
+        const float r = rsqrtf(fmaf(sum_over_head<W>(ss), inv, a.eps));
+        const float mean = sum_over_head<W>(dot) * inv * r * r * r, rw = position >= 0 ? r : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          dw[j] = fmaf(dy[j] * rw, x[j], dw[j]);
+          dyp[j] = fmaf(dyp[j], r, -x[j] * mean);
+        }
+        if (p + i < mine) dst[(p + i) * H * pieces] = position >= 0 ? close8<T>(dyp) : make_uint4(0, 0, 0, 0);
+      }
+    }
   }
   // the sums of dw: heads of a warp, warps of a CTA, then CTAs, each in a fixed order
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
 #pragma unroll
-    for (int o = 16; o >= W; o >>= 1) {
-      dwq[j] += __shfl_xor_sync(0xffffffffu, dwq[j], o);
-      dwk[j] += __shfl_xor_sync(0xffffffffu, dwk[j], o);
-    }
-    if (l.slot == 0) { sums[warp][0][l.piece * 8 + j] = dwq[j]; sums[warp][1][l.piece * 8 + j] = dwk[j]; }
+    for (int o = 16; o >= W; o >>= 1) dw[j] += __shfl_xor_sync(0xffffffffu, dw[j], o);
+    if (l.slot == 0) sums[warp][l.piece * 8 + j] = dw[j];
   }
   __syncthreads();
-  float* const mine = a.partials + (long long)blockIdx.x * 512;
-  for (int i = tid; i < 2 * a.head_dim; i += kQkThreads) {
-    const int t = i / a.head_dim, e = i % a.head_dim;
+  if (tid < a.head_dim) {
     float s = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kQkWarps; ++w) s += sums[w][t][e];
-    mine[t * 256 + e] = s;
+    for (int i = 0; i < kQkWarps; ++i) s += sums[i][tid];
+    a.partials[(long long)blockIdx.x * 256 + tid] = s;
   }
   __threadfence();
   __syncthreads();
@@ -275,32 +279,57 @@ __global__ void __launch_bounds__(kQkThreads) qk_grad_kernel(const QkArgs a) {
   __syncthreads();
   if (!last) return;
   __threadfence();
-  for (int i = tid; i < 2 * a.head_dim; i += kQkThreads) {
-    const int t = i / a.head_dim, e = i % a.head_dim;
-    float s = 0.0f;
-    for (unsigned b = 0; b < gridDim.x; ++b) s += __ldcg(a.partials + (long long)b * 512 + t * 256 + e);
+  // the last CTA: a thread has four columns of every n-th CTA's sums; the threads of a column then join
+  const int columns = a.head_dim / 4, n = kQkThreads / columns, column = tid % columns, row = tid / columns;
+  for (int t = 0; t < 2; ++t) {
+    const int from = t ? ctas_q : 0, to = t ? (int)gridDim.x : ctas_q;
+    float4 s = make_float4(0, 0, 0, 0);
+    if (row < n) {
+#pragma unroll 8
+      for (int b = from + row; b < to; b += n) {
+        const float4 o = __ldcg(reinterpret_cast<const float4*>(a.partials + (long long)b * 256) + column);
+        s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
+      }
+    }
+    joined[tid] = s;
+    __syncthreads();
     float* const out = t ? a.dwk : a.dwq;
-    if (out) out[e] = s;
+    if (row == 0 && out) {
+      for (int i = 1; i < n; ++i) {
+        const float4 o = joined[i * columns + column];
+        s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
+      }
+      out[column * 4] = s.x; out[column * 4 + 1] = s.y; out[column * 4 + 2] = s.z; out[column * 4 + 3] = s.w;
+    }
+    __syncthreads();
   }
   if (tid == 0) *a.ticket = 0;
 }
 
 template <typename T, int W, int MODE>
 cudaError_t run(const QkArgs& a, bool backward, cudaStream_t s) {
-  const int per_pass = 32 / W;
+  constexpr int H = 32 / W;
+  const int passes_q = (a.heads_q + H - 1) / H, passes_k = (a.heads_k + H - 1) / H;
+  const long long token_ctas = (a.rows + kQkWarps - 1) / kQkWarps;
   if (backward) {
-    const long long ctas = (a.rows + kQkWarps - 1) / kQkWarps, most = 4ll * a.sms < kQkGradCtas ? 4ll * a.sms : kQkGradCtas;
-    qk_grad_kernel<T, W, MODE><<<(unsigned)(ctas < most ? ctas : most), kQkThreads, 0, s>>>(a);
-    return cudaGetLastError();
+    // two resident CTAs to a multiprocessor, shared between queries and keys by their passes
+    const int most = 2 * a.sms < kQkGradCtas ? 2 * a.sms : kQkGradCtas;
+    int nq = passes_q ? (int)((long long)most * passes_q / (passes_q + passes_k)) : 0;
+    if (passes_q && nq < 1) nq = 1;
+    if (passes_k && nq > most - 1) nq = most - 1;
+    int nk = passes_k ? most - nq : 0;
+    if (nq > token_ctas) nq = (int)token_ctas;
+    if (nk > token_ctas) nk = (int)token_ctas;
+    return launch(qk_grad_kernel<T, W, MODE>, dim3((unsigned)(nq + nk)), kQkThreads, 0, s, a, nq);
   }
-  const int passes = (a.heads_q + per_pass - 1) / per_pass + (a.heads_k + per_pass - 1) / per_pass;
-  // few tokens: several warps share one, down to a pass each, until every multiprocessor has sixteen warps
-  int per_task = passes;
-  while (per_task > 1 && a.rows * ((passes + per_task - 1) / per_task) < 16ll * a.sms) per_task = (per_task + 1) / 2;
-  const int splits = (passes + per_task - 1) / per_task;
-  const long long ctas = (a.rows * splits + kQkWarps - 1) / kQkWarps;
-  qk_kernel<T, W, MODE><<<(unsigned)ctas, kQkThreads, 0, s>>>(a, splits, per_task);
-  return cudaGetLastError();
+  // batches of as equal a number of passes as possible; few tokens: smaller ones, down to a pass each, until every
+  // multiprocessor has sixteen warps
+  auto batches = [&](int passes, int per) { return (passes + per - 1) / per; };
+  const int longest = passes_q > passes_k ? passes_q : passes_k;
+  int per = (longest + batches(longest, kPasses) - 1) / batches(longest, kPasses);
+  while (per > 1 && a.rows * (batches(passes_q, per) + batches(passes_k, per)) < 16ll * a.sms) per = (per + 1) / 2;
+  const int nq = batches(passes_q, per), nk = batches(passes_k, per);
+  return launch(qk_kernel<T, W, MODE>, dim3((unsigned)token_ctas, (unsigned)(nq + nk)), kQkThreads, 0, s, a, nq, per);
 }
 
 template <typename T, int W>
