@@ -72,8 +72,8 @@ SIGNATURES = {
     "aq_token_logprobs_grad": (_I, [_P, _P, _L, _L, _L, _P, _F, _P, _P, _P, _P, _P, _L]),
     "aq_gated_ffn": (_I, [_P, _P, _L, _P, _P, _L, _L, _I, _I, _I, _P, _L, _P, _P, _L]),
     "aq_gated_ffn_grad": (_I, [_P, _P, _L, _P, _L, _P, _P, _L, _P, _P, _L, _L, _I, _I, _I, _P, _L, _P, _P, _L]),
-    "aq_qk_norm_rope": (_I, [_P, C.POINTER(QkShape), _L, _P, _L, _P, _L, _P, _P, _P, _P, _P, _L, _P, _L]),
-    "aq_qk_norm_rope_grad": (_I, [_P, C.POINTER(QkShape), _L, _P, _L, _P, _L, _P, _L, _P, _L, _P, _P, _P, _P, _P, _L, _P, _L, _P, _P]),
+    "aq_qk_norm_rope": (_I, [_P, _P, _L, _P, _L, _P, _L, _P, _P, _P, _P, _P, _L, _P, _L]),
+    "aq_qk_norm_rope_grad": (_I, [_P, _P, _L, _P, _L, _P, _L, _P, _L, _P, _L, _P, _P, _P, _P, _P, _L, _P, _L, _P, _P]),
 }
 
 _lib = None
@@ -257,20 +257,27 @@ def aq_import_sample(h, sample_id, m_host, seen):
     return _check(h, lib().aq_import_sample(h, sample_id, _ptr(m_host), int(bool(seen))))
 
 
-# ---- stage operators: buffers are named with their row strides, so a tensor may be a slice whose rows are contiguous
+# ---- stage operators: buffers are named with their row strides, so a tensor may be a slice whose rows are contiguous.  A small
+# call takes a few microseconds on the GPU, so these wrappers do as little as they can.
 
 def _row(x):
     """Address of a tensor whose rows (last dimension) are contiguous, of an int address, or None."""
-    if x is None or isinstance(x, int):
+    if x is None or type(x) is int:
         return x
-    assert x.numel() < 2 or x.stride(-1) == 1 or x.shape[-1] == 1, "rows must be contiguous"
+    assert x.is_contiguous() or x.stride(-1) == 1 or x.shape[-1] == 1, "rows must be contiguous"
     return x.data_ptr()
 
 
-def _check_stage(st, rc):
-    if rc != AQ_OK:
-        raise AqError(rc, aq_stage_last_error(st))
-    return rc
+def _whole(x):
+    """Address of a contiguous tensor, an int address, or None."""
+    if x is None or type(x) is int:
+        return x
+    assert x.is_contiguous(), "tensor must be contiguous"
+    return x.data_ptr()
+
+
+def _stage_error(st, rc):
+    raise AqError(rc, aq_stage_last_error(st))
 
 
 def aq_stage_create():
@@ -285,13 +292,14 @@ def aq_stage_destroy(st):
 
 
 def aq_stage_configure(st, key, value):
-    return _check_stage(st, lib().aq_stage_configure(st, key, value))
+    rc = lib().aq_stage_configure(st, key, value)
+    return rc and _stage_error(st, rc)
 
 
 def aq_stage_status(st):
     v = C.c_uint32(0)
-    _check_stage(st, lib().aq_stage_status(st, C.byref(v)))
-    return v.value
+    rc = lib().aq_stage_status(st, C.byref(v))
+    return _stage_error(st, rc) if rc else v.value
 
 
 def aq_stage_last_error(st):
@@ -303,33 +311,39 @@ def aq_stage_last_error_code(st):
 
 
 def aq_token_logprobs(st, logits, rows, vocab, ld, targets, scale, top_k, logprob, entropy, lse, top_ids, top_logprobs):
-    return _check_stage(st, lib().aq_token_logprobs(st, _row(logits), rows, vocab, ld, _ptr(targets), scale, top_k, _ptr(logprob),
-                                                    _ptr(entropy), _ptr(lse), _ptr(top_ids), _ptr(top_logprobs)))
+    rc = (_lib or lib()).aq_token_logprobs(st, _row(logits), rows, vocab, ld, _whole(targets), scale, top_k, _whole(logprob),
+                                           _whole(entropy), _whole(lse), _whole(top_ids), _whole(top_logprobs))
+    return rc and _stage_error(st, rc)
 
 
 def aq_token_logprobs_grad(st, logits, rows, vocab, ld, targets, scale, lse, entropy, d_logprob, d_entropy, d_logits, ld_d):
-    return _check_stage(st, lib().aq_token_logprobs_grad(st, _row(logits), rows, vocab, ld, _ptr(targets), scale, _ptr(lse),
-                                                         _ptr(entropy), _ptr(d_logprob), _ptr(d_entropy), _row(d_logits), ld_d))
+    rc = (_lib or lib()).aq_token_logprobs_grad(st, _row(logits), rows, vocab, ld, _whole(targets), scale, _whole(lse), _whole(entropy),
+                                                _whole(d_logprob), _whole(d_entropy), _row(d_logits), ld_d)
+    return rc and _stage_error(st, rc)
 
 
 def aq_gated_ffn(st, x, ldx, wg, wu, ldw, rows, hidden, inner, act, h, ldh, g, u, ldgu):
-    return _check_stage(st, lib().aq_gated_ffn(st, _row(x), ldx, _row(wg), _row(wu), ldw, rows, hidden, inner, act, _row(h), ldh,
-                                               _row(g), _row(u), ldgu))
+    rc = (_lib or lib()).aq_gated_ffn(st, _row(x), ldx, _row(wg), _row(wu), ldw, rows, hidden, inner, act, _row(h), ldh, _row(g),
+                                      _row(u), ldgu)
+    return rc and _stage_error(st, rc)
 
 
 def aq_gated_ffn_grad(st, dh, lddh, x, ldx, wg, wu, ldw, g, u, ldgu, rows, hidden, inner, act, dx, lddx, dwg, dwu, lddw):
-    return _check_stage(st, lib().aq_gated_ffn_grad(st, _row(dh), lddh, _row(x), ldx, _row(wg), _row(wu), ldw, _row(g), _row(u), ldgu,
-                                                    rows, hidden, inner, act, _row(dx), lddx, _row(dwg), _row(dwu), lddw))
+    rc = (_lib or lib()).aq_gated_ffn_grad(st, _row(dh), lddh, _row(x), ldx, _row(wg), _row(wu), ldw, _row(g), _row(u), ldgu, rows,
+                                           hidden, inner, act, _row(dx), lddx, _row(dwg), _row(dwu), lddw)
+    return rc and _stage_error(st, rc)
 
 
 def aq_qk_norm_rope(st, shape, rows, q, q_stride, k, k_stride, wq, wk, cos_sin, positions, q_out, q_out_stride, k_out, k_out_stride):
     """shape: a QkShape."""
-    return _check_stage(st, lib().aq_qk_norm_rope(st, shape, rows, _row(q), q_stride, _row(k), k_stride, _ptr(wq), _ptr(wk),
-                                                  _ptr(cos_sin), _ptr(positions), _row(q_out), q_out_stride, _row(k_out), k_out_stride))
+    rc = (_lib or lib()).aq_qk_norm_rope(st, C.addressof(shape), rows, _row(q), q_stride, _row(k), k_stride, _whole(wq), _whole(wk),
+                                         _whole(cos_sin), _whole(positions), _row(q_out), q_out_stride, _row(k_out), k_out_stride)
+    return rc and _stage_error(st, rc)
 
 
 def aq_qk_norm_rope_grad(st, shape, rows, dq_out, dq_out_stride, dk_out, dk_out_stride, q, q_stride, k, k_stride, wq, wk, cos_sin,
                          positions, dq, dq_stride, dk, dk_stride, dwq, dwk):
-    return _check_stage(st, lib().aq_qk_norm_rope_grad(st, shape, rows, _row(dq_out), dq_out_stride, _row(dk_out), dk_out_stride,
-                                                       _row(q), q_stride, _row(k), k_stride, _ptr(wq), _ptr(wk), _ptr(cos_sin),
-                                                       _ptr(positions), _row(dq), dq_stride, _row(dk), dk_stride, _ptr(dwq), _ptr(dwk)))
+    rc = (_lib or lib()).aq_qk_norm_rope_grad(st, C.addressof(shape), rows, _row(dq_out), dq_out_stride, _row(dk_out), dk_out_stride,
+                                              _row(q), q_stride, _row(k), k_stride, _whole(wq), _whole(wk), _whole(cos_sin),
+                                              _whole(positions), _row(dq), dq_stride, _row(dk), dk_stride, _whole(dwq), _whole(dwk))
+    return rc and _stage_error(st, rc)

@@ -14,6 +14,8 @@
 
 #include <cuda.h>
 
+#include <atomic>
+
 #include "aq_stage.h"
 #include "aq_stage_device.cuh"
 
@@ -644,8 +646,17 @@ template <typename T, int ACT, bool BACKWARD>
 cudaError_t launch_products(Products& p, int pairs, cudaStream_t s) {
   for (int i = 0; i < 3; ++i) p.sectors[i] = (reinterpret_cast<uintptr_t>(p.out[i]) & 31) == 0 && p.ld[i] % 16 == 0;
   auto kernel = products_kernel<T, ACT, BACKWARD>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
-  return e != cudaSuccess ? e : launch(kernel, 2u * pairs, kFfnThreads, kSharedBytes, s, p);
+  static std::atomic<uint64_t> allowed{0};    // devices on which this kernel may have that much shared memory
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = device < 64 ? 1ull << device : 0;
+  if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
+    if (e != cudaSuccess) return e;
+    allowed.fetch_or(bit, std::memory_order_relaxed);
+  }
+  return launch(kernel, 2u * pairs, kFfnThreads, kSharedBytes, s, p);
 }
 
 template <typename T, int ACT>
