@@ -520,6 +520,11 @@ __global__ void __launch_bounds__(kRowsThreads) ffn_rows_kernel(const FfnArgs a)
   const T* const x = static_cast<const T*>(a.x);
   float c[2][TOKENS8][4] = {};
   next_may_launch();
+  // a hint while the stream's previous kernel drains: the weights into L2, a row of each matrix a lane of the first warp
+  if (warp == 0 && f0 + (lane & 15) < a.inner) {
+    const T* const row = static_cast<const T*>(lane < 16 ? a.wg : a.wu) + (long long)(f0 + (lane & 15)) * a.ldw;
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(row), "r"(a.hidden * 2) : "memory");
+  }
   wait_for_previous();
   const int steps = (a.hidden + 31) / 32;
   for (int s0 = warp; s0 < steps; s0 += kRowsWarps * kRowsAhead) {

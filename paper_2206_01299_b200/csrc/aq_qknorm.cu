@@ -18,8 +18,13 @@ namespace aq {
 namespace {
 
 constexpr int kQkThreads = 256, kQkWarps = kQkThreads / 32;
-constexpr int kPasses = 8;                    // passes of a forward warp at most: its loads in flight
-constexpr int kGradPasses = 2;                // ... of a backward warp, two loads each
+constexpr int kCtas = 4, kGradCtas = 2;       // CTAs on a multiprocessor that the registers are cut for
+// Passes of a forward warp at most, whose loads are all in flight: seven are what 64 registers hold.  At 32768 tokens of 50
+// heads of 64, 77 us; with eight 84 us (three CTAs) or 86 us (four, spilling), with four 94 us (a token's factors are formed
+// again for every batch).
+constexpr int kPasses = 7;
+constexpr int kGradPasses = 2;                // ... of a backward warp at a time, two loads each, and the next ones': 55 us at 16384 tokens of
+                                              // 32 heads of 64; with one 70 us, with three 59 us
 
 template <typename T> __device__ void open8(uint4 v, float* f) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -139,9 +144,11 @@ __device__ int position_of(const QkArgs& a, long long token) {
   return -1;
 }
 
+__device__ float inverse_root(float x) { float y; asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
 // blockIdx.y: a batch of `per` passes of the queries' heads (the first batches_q) or the keys'
 template <typename T, int W, int MODE>
-__global__ void __launch_bounds__(kQkThreads) qk_kernel(const QkArgs a, int batches_q, int per) {
+__global__ void __launch_bounds__(kQkThreads, kCtas) qk_kernel(const QkArgs a, int batches_q, int per) {
   __shared__ __align__(16) T exchange[MODE == kPairsByShared ? kQkWarps * 256 : 8];
   constexpr int H = 32 / W;
   const long long token = (long long)blockIdx.x * kQkWarps + threadIdx.x / 32;
@@ -150,20 +157,27 @@ __global__ void __launch_bounds__(kQkThreads) qk_kernel(const QkArgs a, int batc
   if (token >= a.rows) return;
   const bool keys = (int)blockIdx.y >= batches_q;
   const int heads = keys ? a.heads_k : a.heads_q, pieces = a.head_dim / 8;
-  const int p0 = ((int)blockIdx.y - (keys ? batches_q : 0)) * per;
+  const int p0 = ((int)blockIdx.y - (keys ? batches_q : 0)) * per, passes = min(per, (heads - p0 * H + H - 1) / H);
   const Lane<T, W, MODE> l(a, exchange + (MODE == kPairsByShared ? (threadIdx.x / 32) * 256 : 0));
-  const int head0 = p0 * H + l.slot, mine = l.holds ? min(per, (heads - head0 + H - 1) / H) : 0;   // heads of this lane
-  const int passes = min(per, (heads - p0 * H + H - 1) / H);
-  const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const T*>(keys ? a.k : a.q) + token * (keys ? a.k_stride : a.q_stride)) + head0 * pieces + l.piece;
-  uint4* const dst = reinterpret_cast<uint4*>(static_cast<T*>(keys ? a.k_out : a.q_out) + token * (keys ? a.k_out_stride : a.q_out_stride)) + head0 * pieces + l.piece;
+  // 16-byte pieces of the row; a lane without one in a pass reads the row's last and stores nothing
+  const int step = H * pieces, last = heads * pieces - 1, at = (p0 * H + l.slot) * pieces + l.piece;
+  const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const T*>(keys ? a.k : a.q) + token * (keys ? a.k_stride : a.q_stride));
+  uint4* const dst = reinterpret_cast<uint4*>(static_cast<T*>(keys ? a.k_out : a.q_out) + token * (keys ? a.k_out_stride : a.q_out_stride));
   uint4 v[kPasses];
 #pragma unroll
-  for (int i = 0; i < kPasses; ++i) v[i] = i < mine ? __ldcs(src + i * H * pieces) : make_uint4(0, 0, 0, 0);
+  for (int i = 0; i < kPasses; ++i)
+    if (i < passes) v[i] = __ldcs(src + min(at + i * step, last));
   const int position = position_of(a, token);
+  if (position < 0) {
+    for (int i = 0; i < passes; ++i)
+      if (l.holds && at + i * step <= last) dst[at + i * step] = make_uint4(0, 0, 0, 0);
+    return;
+  }
   float fa[8], fb[8];
-  {
+  l.factors(a, position, fa, fb);
+  const void* const weights = keys ? a.wk : a.wq;
+  if (weights) {
     float w[8], wp[8];
-    const void* const weights = keys ? a.wk : a.wq;
     load_weights<T>(weights, l.piece, l.holds, w);
     if (MODE == kPairsInLane) {
 #pragma unroll
@@ -172,9 +186,8 @@ __global__ void __launch_bounds__(kQkThreads) qk_kernel(const QkArgs a, int batc
       load_weights<T>(weights, l.partner & (W - 1), l.holds, wp);
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) wp[j] = weights && l.holds ? (float)static_cast<const T*>(weights)[l.partner_of(a, l.piece * 8 + j)] : 1.0f;
+      for (int j = 0; j < 8; ++j) wp[j] = l.holds ? (float)static_cast<const T*>(weights)[l.partner_of(a, l.piece * 8 + j)] : 1.0f;
     }
-    l.factors(a, max(position, 0), fa, fb);
 #pragma unroll
     for (int j = 0; j < 8; ++j) { fa[j] *= w[j]; fb[j] *= wp[j]; }
   }
@@ -187,24 +200,25 @@ __global__ void __launch_bounds__(kQkThreads) qk_kernel(const QkArgs a, int batc
     l.partners(a, v[i], x, xp);
 #pragma unroll
     for (int j = 0; j < 8; ++j) ss = fmaf(x[j], x[j], ss);
-    const float r = rsqrtf(fmaf(sum_over_head<W>(ss), inv, a.eps));
+    const float r = inverse_root(fmaf(sum_over_head<W>(l.holds ? ss : 0.0f), inv, a.eps));
     float o[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[j] = r * fmaf(fa[j], x[j], fb[j] * xp[j]);
-    if (i < mine) dst[i * H * pieces] = position >= 0 ? close8<T>(o) : make_uint4(0, 0, 0, 0);
+    if (l.holds && at + i * step <= last) dst[at + i * step] = close8<T>(o);
   }
 }
 
 // ---- gradient ------------------------------------------------------------------------------------------------
 
-// CTAs [0, ctas_q) take the queries' heads, the others the keys'.
+// CTAs [0, ctas_q) take the queries' heads, the others the keys'.  A warp walks over tokens, kGradPasses passes at a time, the
+// next ones on their way while these are worked on.
 template <typename T, int W, int MODE>
-__global__ void __launch_bounds__(kQkThreads, 2) qk_grad_kernel(const QkArgs a, int ctas_q) {
+__global__ void __launch_bounds__(kQkThreads, kGradCtas) qk_grad_kernel(const QkArgs a, int ctas_q) {
   __shared__ __align__(16) T exchange[MODE == kPairsByShared ? kQkWarps * 256 : 8];
   __shared__ float sums[kQkWarps][256];
   __shared__ float4 joined[kQkThreads];
-  __shared__ bool last;
-  constexpr int H = 32 / W;
+  __shared__ bool last_cta;
+  constexpr int H = 32 / W, U = kGradPasses;
   const int warp = threadIdx.x / 32, tid = threadIdx.x;
   next_may_launch();
   wait_for_previous();
@@ -214,28 +228,48 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_grad_kernel(const QkArgs a, 
   const Lane<T, W, MODE> l(a, exchange + (MODE == kPairsByShared ? warp * 256 : 0));
   float w[8], dw[8] = {};
   load_weights<T>(keys ? a.wk : a.wq, l.piece, l.holds, w);
-  const int passes = (heads + H - 1) / H, mine = l.holds ? (heads - l.slot + H - 1) / H : 0;
+  const int passes = (heads + H - 1) / H, step = H * pieces, last = heads * pieces - 1, at = l.slot * pieces + l.piece;
   const float inv = 1.0f / (float)a.head_dim;
-  for (long long token = (long long)cta * kQkWarps + warp; token < a.rows; token += (long long)ctas * kQkWarps) {
-    const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const T*>(keys ? a.k : a.q) + token * (keys ? a.k_stride : a.q_stride)) + l.slot * pieces + l.piece;
-    const uint4* const gsrc = reinterpret_cast<const uint4*>(static_cast<const T*>(keys ? a.gk : a.gq) + token * (keys ? a.gk_stride : a.gq_stride)) + l.slot * pieces + l.piece;
-    uint4* const dst = reinterpret_cast<uint4*>(static_cast<T*>(keys ? a.k_out : a.q_out) + token * (keys ? a.k_out_stride : a.q_out_stride)) + l.slot * pieces + l.piece;
-    float cs[8], sn[8];
+  const T* const x_rows = static_cast<const T*>(keys ? a.k : a.q);
+  const T* const g_rows = static_cast<const T*>(keys ? a.gk : a.gq);
+  T* const o_rows = static_cast<T*>(keys ? a.k_out : a.q_out);
+  const long long x_stride = keys ? a.k_stride : a.q_stride, g_stride = keys ? a.gk_stride : a.gq_stride, o_stride = keys ? a.k_out_stride : a.q_out_stride;
+  const long long stride = (long long)ctas * kQkWarps;
+  long long token = (long long)cta * kQkWarps + warp;
+  uint4 nv[U], ng[U];
+  int next_position = 0;
+  auto load = [&](long long t, int p) {
+    const uint4* const src = reinterpret_cast<const uint4*>(x_rows + t * x_stride);
+    const uint4* const gsrc = reinterpret_cast<const uint4*>(g_rows + t * g_stride);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int from = min(at + (p + i) * step, last);         // a lane without a piece reads the row's last and uses nothing of it
+      nv[i] = __ldcs(src + from);
+      ng[i] = __ldcs(gsrc + from);
+    }
+    if (p == 0 && a.rot_dim) next_position = __ldg(a.positions + t);
+  };
+  if (token < a.rows) load(token, 0);
+  float cs[8], sn[8];
+  for (; token < a.rows; token += stride) {
     int position = 0;
-    for (int p = 0; p < passes; p += kGradPasses) {
-      uint4 v[kGradPasses], g[kGradPasses];
-#pragma unroll
-      for (int i = 0; i < kGradPasses; ++i) {
-        const bool in = p + i < mine;
-        v[i] = in ? __ldcs(src + (p + i) * H * pieces) : make_uint4(0, 0, 0, 0);
-        g[i] = in ? __ldcs(gsrc + (p + i) * H * pieces) : make_uint4(0, 0, 0, 0);
+    if (a.rot_dim) {
+      position = next_position;
+      if (position < 0 || position >= a.n_positions) {
+        if ((tid & 31) == 0) atomicOr(a.status, (uint32_t)AQ_ST_BAD_ID);
+        position = -1;
       }
-      if (p == 0) {
-        position = position_of(a, token);
-        l.factors(a, max(position, 0), cs, sn);
-      }
+    }
+    l.factors(a, max(position, 0), cs, sn);
+    uint4* const dst = reinterpret_cast<uint4*>(o_rows + token * o_stride);
+    for (int p = 0; p < passes; p += U) {
+      uint4 v[U], g[U];
 #pragma unroll
-      for (int i = 0; i < kGradPasses; ++i) {
+      for (int i = 0; i < U; ++i) { v[i] = nv[i]; g[i] = ng[i]; }
+      if (p + U < passes) load(token, p + U);
+      else if (token + stride < a.rows) load(token + stride, 0);
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
         if (p + i >= passes) break;
         float x[8], dy[8], dyp[8], ss = 0.0f, dot = 0.0f;
         open8<T>(v[i], x);
@@ -248,14 +282,15 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_grad_kernel(const QkArgs a, 
           dyp[j] = dy[j] * w[j];
           dot = fmaf(dyp[j], x[j], dot);
         }
-        const float r = rsqrtf(fmaf(sum_over_head<W>(ss), inv, a.eps));
-        const float mean = sum_over_head<W>(dot) * inv * r * r * r, rw = position >= 0 ? r : 0.0f;
+        const bool mine = l.holds && at + (p + i) * step <= last;
+        const float r = inverse_root(fmaf(sum_over_head<W>(l.holds ? ss : 0.0f), inv, a.eps));
+        const float mean = sum_over_head<W>(l.holds ? dot : 0.0f) * inv * r * r * r, rw = mine && position >= 0 ? r : 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           dw[j] = fmaf(dy[j] * rw, x[j], dw[j]);
           dyp[j] = fmaf(dyp[j], r, -x[j] * mean);
         }
-        if (p + i < mine) dst[(p + i) * H * pieces] = position >= 0 ? close8<T>(dyp) : make_uint4(0, 0, 0, 0);
+        if (mine) dst[at + (p + i) * step] = position >= 0 ? close8<T>(dyp) : make_uint4(0, 0, 0, 0);
       }
     }
   }
@@ -275,9 +310,9 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_grad_kernel(const QkArgs a, 
   }
   __threadfence();
   __syncthreads();
-  if (tid == 0) last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+  if (tid == 0) last_cta = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
   __syncthreads();
-  if (!last) return;
+  if (!last_cta) return;
   __threadfence();
   // the last CTA: a thread has four columns of every n-th CTA's sums; the threads of a column then join
   const int columns = a.head_dim / 4, n = kQkThreads / columns, column = tid % columns, row = tid / columns;
@@ -312,8 +347,8 @@ cudaError_t run(const QkArgs& a, bool backward, cudaStream_t s) {
   const int passes_q = (a.heads_q + H - 1) / H, passes_k = (a.heads_k + H - 1) / H;
   const long long token_ctas = (a.rows + kQkWarps - 1) / kQkWarps;
   if (backward) {
-    // two resident CTAs to a multiprocessor, shared between queries and keys by their passes
-    const int most = 2 * a.sms < kQkGradCtas ? 2 * a.sms : kQkGradCtas;
+    // one wave of CTAs, shared between queries and keys by their passes
+    const int most = kGradCtas * a.sms < kQkGradCtas ? kGradCtas * a.sms : kQkGradCtas;
     int nq = passes_q ? (int)((long long)most * passes_q / (passes_q + passes_k)) : 0;
     if (passes_q && nq < 1) nq = 1;
     if (passes_k && nq > most - 1) nq = most - 1;
