@@ -210,16 +210,34 @@ template <typename T> struct Part {
   }
 };
 
+// The largest key of a warp's lanes.
+__device__ unsigned long long warp_best(unsigned long long key) {
+  const unsigned high = __reduce_max_sync(0xffffffffu, (unsigned)(key >> 32));
+  const unsigned low = __reduce_max_sync(0xffffffffu, (unsigned)(key >> 32) == high ? (unsigned)key : 0u);
+  return ((unsigned long long)high << 32) | low;
+}
+
 // The k largest of sh.found[0..n) (unique keys) to sh.list, falling; missing places 0.  One warp.
 __device__ void select_found(RowShared& sh, int n, int k) {
   const int lane = threadIdx.x & 31;
-  if (lane < k) sh.list[lane] = 0ull;
-  __syncwarp();
-  for (int i = lane; i < n; i += 32) {
-    const unsigned long long mine = sh.found[i];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += sh.found[j] > mine;
-    if (rank < k && mine) sh.list[rank] = mine;
+  if (n <= 128) {                                  // every key counts those above it
+    if (lane < k) sh.list[lane] = 0ull;
+    __syncwarp();
+    for (int i = lane; i < n; i += 32) {
+      const unsigned long long mine = sh.found[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += sh.found[j] > mine;
+      if (rank < k && mine) sh.list[rank] = mine;
+    }
+    __syncwarp();
+    return;
+  }
+  unsigned long long below = ~0ull;                // the largest that is left, k times
+  for (int r = 0; r < k; ++r) {
+    unsigned long long best = 0ull;
+    for (int i = lane; i < n; i += 32) { const unsigned long long key = sh.found[i]; if (key < below && key > best) best = key; }
+    below = warp_best(best);
+    if (lane == 0) sh.list[r] = below;
   }
   __syncwarp();
 }
@@ -534,6 +552,92 @@ __global__ void __launch_bounds__(kRowThreads, kRanks > 1 ? 1 : kRowCtas) logpro
   }
 }
 
+// ---- short rows ----------------------------------------------------------------------------------------------
+//
+// A row of up to kShort logits is a warp's: it stays in registers, so that the largest logit is known before the sums are
+// formed, relative to it, and the alternatives are taken from the registers one by one.  8192 rows of 257 bf16 logits
+// with twenty alternatives 39 us, without any 7 us (a CTA to a row: 230 and 17 us).
+
+constexpr int kShort = 1024;
+
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads) logprob_short_kernel(const LogprobArgs a) {
+  constexpr int N = Pack<T>::N, kVecs = kShort / N / 32;
+  const int lane = threadIdx.x & 31;
+  const long long row = (long long)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+  next_may_launch();
+  wait_for_previous();
+  if (row >= a.rows) return;
+  const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
+  const Part<T> part(x, (unsigned)a.vocab, 0, 1);
+  uint4 v[kVecs];
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) if (lane + 32 * i < part.n_vec) v[i] = __ldcs(part.vec + lane + 32 * i);
+  // the elements before the first and after the last vector: lanes 0.. and 16..
+  const bool edge = lane < part.head || (lane >= 16 && lane - 16 < part.tail);
+  const unsigned edge_id = lane < part.head ? (unsigned)lane : part.tail_first + (unsigned)(lane - 16);
+  const float edge_x = edge ? Pack<T>::one(x[edge_id]) : 0.0f;
+  // f(value, id) of all of this lane's logits
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      if (32 * i >= part.n_vec) break;
+      if (lane + 32 * i < part.n_vec) {
+        float e[N];
+        Pack<T>::open(v[i], e);
+#pragma unroll
+        for (int j = 0; j < N; ++j) f(e[j], part.vec_first + (unsigned)(lane + 32 * i) * N + j);
+      }
+    }
+    if (edge) f(edge_x, edge_id);
+  };
+  const float c = a.scale * kLog2e;
+  float top = -CUDART_INF_F, s = 0.0f, t = 0.0f;
+  each([&](float e, unsigned) { top = fmaxf(top, e); });
+  top = warp_max(top);
+  const bool empty = a.scale * top == -CUDART_INF_F;           // NaNs apart, which the sum is to show
+  each([&](float e, unsigned) {
+    if (empty && e == e) return;
+    const float d = at_least((e - top) * c, kGone), p = exp2_fast(d);
+    s += p;
+    t = fmaf(p, d, t);
+  });
+  s = warp_sum(s);
+  t = warp_sum(t);
+  const bool none = s == 0.0f;
+  const float log2s = log2f(s), ln_s = kLn2 * log2s;
+  if (lane == 0) {
+    if (a.lse) a.lse[row] = none ? -CUDART_INF_F : fmaf(a.scale, top, ln_s);
+    if (a.entropy) a.entropy[row] = none ? 0.0f : kLn2 * (log2s - t / s);
+    if (a.targets) {
+      const int32_t target = a.targets[row];
+      float lp = 0.0f;
+      if (target >= 0 && target < a.vocab) lp = none ? -CUDART_INF_F : a.scale * (Pack<T>::one(x[target]) - top) - ln_s;
+      else if (target >= 0) atomicOr(a.status, (uint32_t)AQ_ST_BAD_ID);
+      if (a.logprob) a.logprob[row] = lp;
+    }
+  }
+  const int k = a.top_k;
+  unsigned long long mine = 0ull, taken = ~0ull, best = 0ull;  // this lane's place in the list; the last key taken; this lane's best below it
+  for (int r = 0; r < k; ++r) {
+    if (best >= taken || r == 0) {
+      best = 0ull;
+      each([&](float e, unsigned id) {
+        const unsigned long long key = e == e ? key_of(e, id) : 0ull;
+        if (key < taken && key > best) best = key;
+      });
+    }
+    __syncwarp();
+    taken = warp_best(best);
+    if (lane == r) mine = taken;
+    if (!taken) break;                                         // nothing left
+  }
+  if (lane < k) {
+    if (a.top_ids) a.top_ids[row * k + lane] = mine ? (int32_t)id_of(mine) : -1;
+    if (a.top_logprobs) a.top_logprobs[row * k + lane] = !mine ? CUDART_NAN_F : none ? -CUDART_INF_F : a.scale * (value_of(mine) - top) - ln_s;
+  }
+}
+
 // ---- gradient ------------------------------------------------------------------------------------------------
 
 constexpr float kFarLse = 4096.0f;            // half a unit of lse in its last place there is 1/4096
@@ -564,11 +668,15 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
   const float gl = target >= 0 && a.d_logprob ? a.d_logprob[row] : 0.0f;
   const float at_target = gl * a.scale;
 
+  if (lse == -CUDART_INF_F) {                                    // no distribution: zeros
+    const unsigned i0 = piece * (kRowThreads * kGradVecs * N), i1 = min(i0 + kRowThreads * kGradVecs * N, vocab);
+    for (unsigned i = i0 + tid; i < i1; i += kRowThreads) out[i] = Pack<T>::round(0.0f);
+    return;
+  }
   const float ref = lse * kLog2e;
   if (!(fabsf(lse) <= kFarLse) || Pack<T>::kLow * c - ref > -kClear) {
-    // the first piece's CTA does the whole row: zeros where the row has no distribution; else the logits are so large
-    // that lse has no digits left for ln p (or so low or little scaled that raising the masked ones would show), and the row's own sum is
-    // formed again, relative to its largest logit
+    // the first piece's CTA does the whole row: the logits are so large that lse has no digits left for ln p (or so low or little
+    // scaled that raising the masked ones would show), and the row's own sum is formed again, relative to its largest logit
     if (piece) return;
     __shared__ float part[kRowWarps];
     float top = -CUDART_INF_F;
@@ -587,12 +695,11 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
     s = 0.0f;
 #pragma unroll
     for (int w = 0; w < kRowWarps; ++w) s += part[w];
-    const bool none = lse == -CUDART_INF_F;
     const float log2s = log2f(s);
     for (unsigned i = tid; i < vocab; i += kRowThreads) {
       const float d = at_least((Pack<T>::one(x[i]) - top) * c - log2s, kGone), p = exp2_fast(d);
       const float v = -a.scale * p * (gl + gh * (d * kLn2 + entropy)) + (i == (unsigned)target ? at_target : 0.0f);
-      out[i] = Pack<T>::round(none ? 0.0f : v);
+      out[i] = Pack<T>::round(v);
     }
     return;
   }
@@ -655,6 +762,9 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
 
 template <typename T>
 cudaError_t run(const LogprobArgs& a, cudaStream_t s) {
+  // Short rows; up to half of that where many alternatives are asked for, which the short kernel takes one by one (8192 rows of
+  // 1000 bf16 logits: with 5 alternatives 34 us on either, with 20 103 us against 68; of 257: 39 against 230).
+  if (a.vocab <= (a.top_k <= 8 ? kShort : kShort / 2)) return launch(logprob_short_kernel<T>, dim3((unsigned)((a.rows + kRowWarps - 1) / kRowWarps)), kRowThreads, 0, s, a);
   // A row to a CTA when there are rows for half of the multiprocessors; below, a cluster of eight to a row.
   if (a.rows * 2 >= a.sms || a.vocab < 4096) return launch(logprob_kernel<T, 1>, dim3((unsigned)a.rows), kRowThreads, 0, s, a);
   cudaLaunchConfig_t cfg{};
