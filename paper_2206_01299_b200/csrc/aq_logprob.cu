@@ -643,15 +643,17 @@ __global__ void __launch_bounds__(kRowThreads) logprob_short_kernel(const Logpro
 constexpr float kFarLse = 4096.0f;            // half a unit of lse in its last place there is 1/4096
 constexpr int kGradVecs = 8;                  // 16-byte vectors per thread
 
-// One piece of one row: d = scale p (A + B log2 p) and the target's term, where ln p = z - lse.
-template <typename T>
+// One piece of one row: d = scale p (A + B log2 p) and the target's term, where ln p = z - lse.  LANES threads to a piece: a CTA,
+// or a warp where that holds a whole row (8192 rows of 257 bf16 logits: 8 us against 22).
+template <typename T, int LANES>
 __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const LogprobGradArgs a, int pieces) {
   constexpr int N = Pack<T>::N;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x % LANES;
   next_may_launch();
   wait_for_previous();
-  const long long row = blockIdx.x / (unsigned)pieces;
-  const unsigned piece = blockIdx.x % (unsigned)pieces;
+  const long long row = LANES == 32 ? (long long)blockIdx.x * kRowWarps + threadIdx.x / 32 : blockIdx.x / (unsigned)pieces;
+  const unsigned piece = LANES == 32 ? 0u : blockIdx.x % (unsigned)pieces;
+  if (LANES == 32 && row >= a.rows) return;
   const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
   T* const out = static_cast<T*>(a.d_logits) + row * a.ld_d;
   const unsigned vocab = (unsigned)a.vocab;
@@ -669,8 +671,8 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
   const float at_target = gl * a.scale;
 
   if (lse == -CUDART_INF_F) {                                    // no distribution: zeros
-    const unsigned i0 = piece * (kRowThreads * kGradVecs * N), i1 = min(i0 + kRowThreads * kGradVecs * N, vocab);
-    for (unsigned i = i0 + tid; i < i1; i += kRowThreads) out[i] = Pack<T>::round(0.0f);
+    const unsigned i0 = piece * (LANES * kGradVecs * N), i1 = min(i0 + LANES * kGradVecs * N, vocab);
+    for (unsigned i = i0 + tid; i < i1; i += LANES) out[i] = Pack<T>::round(0.0f);
     return;
   }
   const float ref = lse * kLog2e;
@@ -680,23 +682,27 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
     if (piece) return;
     __shared__ float part[kRowWarps];
     float top = -CUDART_INF_F;
-    for (unsigned i = tid; i < vocab; i += kRowThreads) top = fmaxf(top, Pack<T>::one(x[i]));
+    for (unsigned i = tid; i < vocab; i += LANES) top = fmaxf(top, Pack<T>::one(x[i]));
     top = warp_max(top);
-    if ((tid & 31) == 0) part[tid >> 5] = top;
-    __syncthreads();
+    if (LANES > 32) {
+      if ((tid & 31) == 0) part[tid >> 5] = top;
+      __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kRowWarps; ++w) top = fmaxf(top, part[w]);
-    __syncthreads();
+      for (int w = 0; w < kRowWarps; ++w) top = fmaxf(top, part[w]);
+      __syncthreads();
+    }
     float s = 0.0f;
-    for (unsigned i = tid; i < vocab; i += kRowThreads) s += exp2_fast(at_least((Pack<T>::one(x[i]) - top) * c, kGone));
+    for (unsigned i = tid; i < vocab; i += LANES) s += exp2_fast(at_least((Pack<T>::one(x[i]) - top) * c, kGone));
     s = warp_sum(s);
-    if ((tid & 31) == 0) part[tid >> 5] = s;
-    __syncthreads();
-    s = 0.0f;
+    if (LANES > 32) {
+      if ((tid & 31) == 0) part[tid >> 5] = s;
+      __syncthreads();
+      s = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kRowWarps; ++w) s += part[w];
+      for (int w = 0; w < kRowWarps; ++w) s += part[w];
+    }
     const float log2s = log2f(s);
-    for (unsigned i = tid; i < vocab; i += kRowThreads) {
+    for (unsigned i = tid; i < vocab; i += LANES) {
       const float d = at_least((Pack<T>::one(x[i]) - top) * c - log2s, kGone), p = exp2_fast(d);
       const float v = -a.scale * p * (gl + gh * (d * kLn2 + entropy)) + (i == (unsigned)target ? at_target : 0.0f);
       out[i] = Pack<T>::round(v);
@@ -713,7 +719,7 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
     d = Pack<T>::held(d);
     return exp2_fast(d) * fmaf(coef_b, d, coef_a);
   };
-  const unsigned per = kRowThreads * kGradVecs * N;
+  const unsigned per = LANES * kGradVecs * N;
   const unsigned misalign = (unsigned)(reinterpret_cast<uintptr_t>(out) & 15u);
   if (misalign == (unsigned)(reinterpret_cast<uintptr_t>(x) & 15u)) {
     const unsigned off = ((16u - misalign) & 15u) / (unsigned)sizeof(T);
@@ -721,13 +727,13 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
     const unsigned n_vec = (vocab - head) / N, tail = vocab - head - n_vec * N;
     const uint4* const vx = reinterpret_cast<const uint4*>(x + head);
     uint4* const vo = reinterpret_cast<uint4*>(out + head);
-    const unsigned v0 = piece * (kRowThreads * kGradVecs) + tid;
+    const unsigned v0 = piece * (LANES * kGradVecs) + tid;
     uint4 v[kGradVecs];
 #pragma unroll
-    for (int i = 0; i < kGradVecs; ++i) if (v0 + i * kRowThreads < n_vec) v[i] = __ldcs(vx + v0 + i * kRowThreads);
+    for (int i = 0; i < kGradVecs; ++i) if (v0 + i * LANES < n_vec) v[i] = __ldcs(vx + v0 + i * LANES);
 #pragma unroll
     for (int i = 0; i < kGradVecs; ++i) {
-      const unsigned at = v0 + i * kRowThreads;
+      const unsigned at = v0 + i * LANES;
       if (at < n_vec) {
         float f[N];
         uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
@@ -749,13 +755,13 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
     if (piece == 0) {                                            // the elements before the first and after the last vector
       unsigned i = 0xffffffffu;
       if ((unsigned)tid < head) i = tid;
-      else if (tid >= 32 && (unsigned)(tid - 32) < tail) i = head + n_vec * N + (tid - 32);
+      else if (tid >= 16 && (unsigned)(tid - 16) < tail) i = head + n_vec * N + (tid - 16);
       if (i != 0xffffffffu) out[i] = Pack<T>::round(grad(at_least(Pack<T>::one(x[i]), Pack<T>::kLow)) + (i == (unsigned)target ? at_target : 0.0f));
     }
   } else {
     // rows that no common vector boundary serves: element by element
     const unsigned i0 = piece * per, i1 = min(i0 + per, vocab);
-    for (unsigned i = i0 + tid; i < i1; i += kRowThreads)
+    for (unsigned i = i0 + tid; i < i1; i += LANES)
       out[i] = Pack<T>::round(grad(at_least(Pack<T>::one(x[i]), Pack<T>::kLow)) + (i == (unsigned)target ? at_target : 0.0f));
   }
 }
@@ -785,13 +791,14 @@ cudaError_t run(const LogprobArgs& a, cudaStream_t s) {
 template <typename T>
 cudaError_t run_grad(const LogprobGradArgs& a, cudaStream_t s) {
   const long long per = (long long)kRowThreads * kGradVecs * Pack<T>::N;
+  if (a.vocab <= per / kRowWarps) return launch(logprob_grad_kernel<T, 32>, dim3((unsigned)((a.rows + kRowWarps - 1) / kRowWarps)), kRowThreads, 0, s, a, 1);
   const long long pieces = (a.vocab + per - 1) / per;
   // a grid has at most 2^31 - 1 CTAs: more rows go in several launches
   const long long most = 0x7fffffffll / pieces;
   LogprobGradArgs b = a;
   for (long long r = 0; r < a.rows; r += most) {
     b.rows = a.rows - r < most ? a.rows - r : most;
-    const cudaError_t e = launch(logprob_grad_kernel<T>, dim3((unsigned)(b.rows * pieces)), kRowThreads, 0, s, b, (int)pieces);
+    const cudaError_t e = launch(logprob_grad_kernel<T, kRowThreads>, dim3((unsigned)(b.rows * pieces)), kRowThreads, 0, s, b, (int)pieces);
     if (e != cudaSuccess) return e;
     b.logits = static_cast<const T*>(b.logits) + b.rows * b.ld;
     b.d_logits = static_cast<T*>(b.d_logits) + b.rows * b.ld_d;
