@@ -8,8 +8,8 @@ torch does the plain products, the softmax of the attention and the chain rule b
 
     python examples/finetune_two_stages.py [--epochs N]
 
-The data are sequences of a made-up language in which every token has four possible successors, so that the loss of a model that
-has learnt it is near ln 4 = 1.39, and ln 96 = 4.56 before.
+The data are sequences of a made-up language in which every token has four possible successors: the loss of a guess is
+ln 96 = 4.56, that of a model that knows the language ln 4 = 1.39, and less as it comes to know the sequences themselves.
 """
 import argparse
 import math

@@ -509,7 +509,7 @@ __device__ void multiply_warp(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t 
 }
 
 template <typename T, int ACT, int TOKENS8>
-__global__ void __launch_bounds__(kRowsThreads) ffn_rows_kernel(const FfnArgs a) {
+__global__ void __launch_bounds__(kRowsThreads, TOKENS8 == 2 ? 3 : 1) ffn_rows_kernel(const FfnArgs a) {
   __shared__ float4 sums[kRowsWarps][2 * TOKENS8][32];
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int f0 = blockIdx.x * 16;

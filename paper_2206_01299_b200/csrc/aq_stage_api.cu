@@ -36,6 +36,7 @@ int fail(aq_stage* st, int code, const char* fmt, ...) {
 }
 
 int cuda_fail(aq_stage* st, cudaError_t e, const char* what) {
+  cudaGetLastError();                        // reported here, not by whatever asks the runtime next
   return fail(st, e == cudaErrorMemoryAllocation ? AQ_ENOMEM : AQ_ECUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
@@ -68,10 +69,7 @@ int ensure_work(aq_stage* st, size_t bytes) {
   st->work = nullptr;
   st->work_bytes = 0;
   e = cudaMalloc(&st->work, bytes);
-  if (e != cudaSuccess) {
-    cudaGetLastError();
-    return cuda_fail(st, e, "workspace");
-  }
+  if (e != cudaSuccess) return cuda_fail(st, e, "workspace");
   st->work_bytes = bytes;
   return AQ_OK;
 }
@@ -147,7 +145,6 @@ aq_stage* aq_stage_create(void) {
   if (e == cudaSuccess) e = cudaDeviceSynchronize();                    // the memset above is on another stream than the handle's may be
   if (e != cudaSuccess) {
     cuda_fail(nullptr, e, "aq_stage_create");
-    cudaGetLastError();
     cudaFree(st->status);
     cudaFree(st->partials);
     delete st;

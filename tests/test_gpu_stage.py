@@ -128,6 +128,58 @@ def test_logprobs_ties_go_to_the_lowest_id(aq, stage, dtype, rows):
     check_logprobs(x.double(), targets, 1.0, 32, run_logprobs(aq, stage, buf, targets, 1.0, 32))
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("rows,vocab,k,pad", [(3, 512, 32, 0), (9, 513, 9, 1), (9, 1024, 8, 3), (2, 1024, 32, 0), (5, 1025, 32, 0), (90, 2049, 20, 1), (17, 40, 32, 5)])
+def test_logprobs_where_the_way_of_working_changes(aq, stage, dtype, rows, vocab, k, pad):
+    """Row lengths and numbers of alternatives on both sides of every choice; half of the logits masked."""
+    set_type(aq, stage, dtype)
+    g = torch.Generator().manual_seed(vocab + k)
+    x = 3 * torch.randn((rows, vocab), generator=g)
+    x[torch.rand((rows, vocab), generator=g) < 0.5] = -math.inf
+    x = x.to(forms.TYPES[dtype])
+    targets = torch.randint(0, vocab, (rows,), generator=g, dtype=torch.int32)
+    buf = Guarded(rows, vocab, forms.TYPES[dtype], pad, 1).put(x)
+    check_logprobs(x.double(), targets, 1.0, k, run_logprobs(aq, stage, buf, targets, 1.0, k))
+    buf.check()
+
+
+@pytest.mark.parametrize("rows,vocab", [(2, 700), (2, 6001), (120, 6001)])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+def test_logprobs_fewer_tokens_left_than_alternatives(aq, stage, dtype, rows, vocab):
+    """Three tokens of a row are allowed, twenty alternatives asked for: then come the lowest ids that are masked."""
+    set_type(aq, stage, dtype)
+    x = torch.full((rows, vocab), -math.inf)
+    allowed = torch.tensor([5, vocab // 2, vocab - 1])
+    x[:, allowed] = torch.tensor([0.5, -1.0, 2.0])
+    x[1, allowed] = torch.tensor([1.0, 1.0, 1.0])
+    x = x.to(forms.TYPES[dtype])
+    targets = torch.full((rows,), vocab - 1, dtype=torch.int32)
+    buf = Guarded(rows, vocab, forms.TYPES[dtype], 1, 0).put(x)
+    check_logprobs(x.double(), targets, 1.0, 20, run_logprobs(aq, stage, buf, targets, 1.0, 20))
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_logprobs_of_barely_scaled_logits(aq, stage, dtype):
+    """A scale at which the type's lowest value and -infinity are not the same thing any more."""
+    set_type(aq, stage, dtype)
+    vocab, scale = 5000, 1e-4
+    x = 100 * torch.randn((90, vocab), generator=torch.Generator().manual_seed(9))
+    x[:, ::3] = -math.inf
+    x[:, 1::3] = torch.finfo(forms.TYPES[dtype]).min if dtype == "fp16" else -60000.0
+    x = x.to(forms.TYPES[dtype])
+    targets = torch.full((90,), 4, dtype=torch.int32)
+    buf = Guarded(90, vocab, forms.TYPES[dtype]).put(x)
+    got = run_logprobs(aq, stage, buf, targets, scale, 3)
+    check_logprobs(x.double(), targets, scale, 3, got)
+    out = Guarded(90, vocab, forms.TYPES[dtype])
+    gl = torch.full((90,), 512.0)
+    run_logprobs_grad(aq, stage, buf, out, targets.cuda(), scale, got[2].float().cuda(), None, gl.cuda(), None)
+    s32 = torch.tensor(scale, dtype=torch.float32).double().item()
+    for r in (0, 89):
+        want = forms.logprobs_grad(x[r].double(), 4, s32, 512.0, 0.0)
+        within(out.view[r], want, forms.UNIT[dtype] * want.abs() * 1.1 + forms.TINY[dtype] + 1e-4 * want.abs())
+
+
 @pytest.mark.parametrize("rows", [3, 200])
 @pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
 def test_logprobs_masked_rows(aq, stage, dtype, rows):
@@ -201,7 +253,8 @@ def run_logprobs_grad(aq, st, buf, out, targets, scale, lse, h, gl, gh):
 @pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
 @pytest.mark.parametrize("rows,vocab,pad,offset,pad_d,offset_d", [
     (1, 1, 0, 0, 0, 0), (3, 2, 1, 1, 1, 1), (2, 7, 0, 3, 2, 1), (4, 50, 3, 0, 3, 8), (3, 257, 0, 1, 0, 1), (20, 1000, 0, 2, 4, 0),
-    (2, 8192, 0, 0, 0, 0), (2, 8193, 7, 0, 7, 0), (3, 50257, 0, 1, 0, 1), (2, 20000, 1, 0, 0, 0)])
+    (2, 8192, 0, 0, 0, 0), (2, 8193, 7, 0, 7, 0), (3, 50257, 0, 1, 0, 1), (2, 20000, 1, 0, 0, 0), (9, 1024, 0, 0, 0, 0), (5, 1025, 0, 1, 0, 1),
+    (9, 2048, 3, 5, 3, 13), (5, 2049, 0, 0, 0, 0)])
 def test_logprobs_gradient(aq, stage, dtype, rows, vocab, pad, offset, pad_d, offset_d):
     """d within one rounding of the type of the formula's, plus binary32's: ln p is known to (|z| + |lse|) 2e, and so
     is p to that times its size; the terms' sum adds 4e of their magnitudes."""
@@ -613,6 +666,78 @@ def test_another_stream_and_a_captured_graph(aq, stage):
         h.zero_()
     assert refused == [aq.AQ_EUNSUPPORTED]
     aq.aq_stage_configure(stage, aq.AQ_STREAM, 0)
+
+
+def test_two_handles_on_two_streams(aq):
+    """The same calls on two handles side by side, many times: each has its own counters and workspace."""
+    rows, hidden, inner = 700, 200, 1000
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rnd = lambda *s: torch.randn(s, generator=gen, device="cuda").bfloat16()  # noqa: E731
+    x, wg, wu, dh = rnd(rows, hidden), rnd(inner, hidden) / 14, rnd(inner, hidden) / 14, rnd(rows, inner)
+    qk, dqk, cs, pos = rnd(rows, 6 * 64), rnd(rows, 6 * 64), table(40, 64).cuda(), torch.arange(rows, dtype=torch.int32, device="cuda") % 40
+    shape = aq.QkShape(heads_q=4, heads_k=2, head_dim=64, rot_dim=64, interleaved=0, eps=1e-6, n_positions=40)
+    sides = []
+    for i in range(2):
+        st, stream = aq.aq_stage_create(), torch.cuda.Stream()
+        set_type(aq, st, "bf16")
+        aq.aq_stage_configure(st, aq.AQ_STREAM, stream.cuda_stream)
+        outs = [torch.zeros_like(v) for v in (dh, dh, dh, x, wg, wu, dqk)] + [floats(64), floats(64)]
+        sides.append((st, stream, outs))
+    torch.cuda.synchronize()
+
+    def calls(st, o):
+        aq.aq_gated_ffn(st, x, hidden, wg, wu, hidden, rows, hidden, inner, 0, o[0], inner, o[1], o[2], inner)
+        aq.aq_gated_ffn_grad(st, dh, inner, x, hidden, wg, wu, hidden, o[1], o[2], inner, rows, hidden, inner, 0, o[3], hidden, o[4], o[5], hidden)
+        aq.aq_qk_norm_rope_grad(st, shape, rows, dqk, 384, dqk[:, 256:], 384, qk, 384, qk[:, 256:], 384, None, None, cs, pos, o[6], 384,
+                                o[6][:, 256:], 384, o[7], o[8])
+    calls(sides[0][0], sides[0][2])
+    torch.cuda.synchronize()
+    want = [v.clone() for v in sides[0][2]]
+    for _ in range(20):
+        for st, _, outs in sides:
+            calls(st, outs)
+    torch.cuda.synchronize()
+    for st, _, outs in sides:
+        assert aq.aq_stage_status(st) == 0
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b)
+        aq.aq_stage_destroy(st)
+
+
+def test_offsets_beyond_32_bits(aq, stage):
+    """Buffers of more than 2^31 elements: the last rows against the same rows alone."""
+    set_type(aq, stage, "bf16")
+    rows, ld = 40000, 60000                                         # 2.4e9 elements
+    big = torch.zeros((rows, ld), dtype=torch.bfloat16, device="cuda")
+    tail = torch.randn((64, 5003), generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").bfloat16()
+    big[-64:, :5003] = tail
+    targets = torch.full((rows,), 7, dtype=torch.int32, device="cuda")
+    lp, ent, lse = floats(rows), floats(rows), floats(rows)
+    aq.aq_token_logprobs(stage, big, rows, 5003, ld, targets, 1.0, 0, lp, ent, lse, None, None)
+    one, e1, l1 = floats(64), floats(64), floats(64)
+    aq.aq_token_logprobs(stage, tail, 64, 5003, 5003, targets, 1.0, 0, one, e1, l1, None, None)
+    torch.cuda.synchronize()
+    assert torch.allclose(lp[-64:], one, atol=2e-5) and torch.allclose(ent[-64:], e1, atol=4e-5)
+    d, d1 = torch.empty_like(tail), torch.empty_like(tail)
+    aq.aq_token_logprobs_grad(stage, big, rows, 5003, ld, targets, 1.0, lse, None, torch.ones_like(lp), None, big, ld)       # in place
+    aq.aq_token_logprobs_grad(stage, tail, 64, 5003, 5003, targets, 1.0, lse[-64:].clone(), None, torch.ones_like(one), None, d1, 5003)
+    torch.cuda.synchronize()
+    assert torch.equal(big[-64:, :5003], d1)
+    del d
+    # heads and the feed-forward product on the same buffer: 64 columns of rows that far apart
+    big[-64:, :256] = torch.randn((64, 256), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").bfloat16()
+    part = big[-64:, :256].clone()
+    cs, pos = table(40, 64).cuda(), torch.arange(rows, dtype=torch.int32, device="cuda") % 40
+    shape = aq.QkShape(heads_q=2, heads_k=1, head_dim=64, rot_dim=64, interleaved=0, eps=1e-6, n_positions=40)
+    w = torch.randn((72, 64), generator=torch.Generator(device="cuda").manual_seed(4), device="cuda").bfloat16()
+    h, h1 = (torch.empty((n, 72), dtype=torch.bfloat16, device="cuda") for n in (rows, 64))
+    aq.aq_gated_ffn(stage, big, ld, w, w, 64, rows, 64, 72, 0, h, 72, None, None, 72)
+    aq.aq_gated_ffn(stage, part, 256, w, w, 64, 64, 64, 72, 0, h1, 72, None, None, 72)
+    aq.aq_qk_norm_rope(stage, shape, rows, big, ld, big[:, 128:], ld, None, None, cs, pos, big, ld, big[:, 128:], ld)
+    aq.aq_qk_norm_rope(stage, shape, 64, part, 256, part[:, 128:], 256, None, None, cs, pos[-64:].clone(), part, 256, part[:, 128:], 256)
+    torch.cuda.synchronize()
+    assert torch.equal(h[-64:], h1) and torch.equal(big[-64:, :256], part)
+    assert aq.aq_stage_status(stage) == 0
 
 
 def test_refusals(aq, stage):
