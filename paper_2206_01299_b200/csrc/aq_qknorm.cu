@@ -5,11 +5,16 @@
 // (not rotated).  The gradient turns back with -sn and then, with n = x r and g = w dy,
 //   dx = r (g - n mean(g n)),   dw = sum over rows and heads of dy n.
 //
-// Bound by memory: 2 T per element forward, 3 T backward, and a position's factors once per token and tensor.  The lanes of a
-// head are the next power of two of its 16-byte pieces, so a warp holds 32 / lanes heads at a time (a pass) and every lane
-// keeps the same elements of all of them: their weights and factors are formed once, as a_e = w_e cos_e and
+// The lanes of a head are the next power of two of its 16-byte pieces, so a warp holds 32 / lanes heads at a time (a pass) and
+// every lane keeps the same elements of all of them: their weights and factors are formed once, as a_e = w_e cos_e and
 // b_e = w_partner sn_e, and a head costs o_e = r (a_e x_e + b_e x_partner).  Partners are exchanged as they were loaded, two
 // values a word.  A warp's loads are all issued before it waits for its token's position.
+//
+// Bound by memory in the first place, 2 T per element forward and 3 T backward and a position's factors once per token, with the
+// issue of instructions (about 15 per element) close behind.  Forward, 32768 tokens of 25 + 25 heads of 64: 77 us, 5.4 TB/s;
+// backward, 16384 tokens of 24 + 8 heads of 64: 52 us, 3.9 TB/s.  What did not help: two pieces a lane, which spares the exchange
+// but doubles the registers (92 us, 68 us); rings in shared memory filled by bulk copies (81 us, 72 us) or, backward, by
+// asynchronous copies (56 us); instructions on pairs of binary32 values.
 
 #include "aq_stage.h"
 #include "aq_stage_device.cuh"
