@@ -628,9 +628,16 @@ struct Maps {
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-// Cycles of a stage of a tile of n columns: its products take 2 n, and its operands, 16384 + 64 n bytes to each
-// multiprocessor, 64 bytes a cycle at most.
-long long stage_cycles(int n) { return 2 * n > 256 + n ? 2 * n : 256 + n; }
+// The cost of tiles, in cycles.  A stage's products take 2 n for n columns; its operands, 16384 + 64 n bytes to each
+// multiprocessor, take about 480 + n / 4.  Starting a tile costs about 1500, its epilogue 11 n, which hides behind the next
+// tile's stages.  The constants are those that order the times of 16 widths and depths of five backward calls best (509 to 3000
+// rows; what they choose is within 1.18 of the fastest, four times the fastest itself).
+long long stage_cycles(int n) { return 2 * n > 480 + n / 4 ? 2 * n : 480 + n / 4; }
+long long epilogue_cycles(int n) { return 11 * n; }
+long long tile_cycles(int stages, int n) {
+  const long long work = (long long)stages * stage_cycles(n), before = epilogue_cycles(n);
+  return (work > before ? work : before) + 1500;
+}
 
 // Pairs that are on the GPU at the same time: the parts of the chip with an odd number of multiprocessors hold one CTA less.
 // A grid with more would run its last pairs after all others had finished their share.
@@ -687,8 +694,8 @@ cudaError_t run(const FfnArgs& a, cudaStream_t s) {
   int best = 0;
   long long least = 0;
   for (int f = 128; f >= 32; f -= 32) {
-    // rounds of the grid, the last one's epilogue, and about 1500 cycles to fill and drain the pipeline
-    const long long tiles = (long long)m_tiles * ceil_div(a.inner, f), c = ((tiles + a.pairs - 1) / a.pairs) * kb * stage_cycles(2 * f) + 32 * f + 1500;
+    // rounds of the grid, and the last one's epilogue
+    const long long tiles = (long long)m_tiles * ceil_div(a.inner, f), c = ((tiles + a.pairs - 1) / a.pairs) * tile_cycles(kb, 2 * f) + epilogue_cycles(2 * f);
     if (!best || c < least) { best = f; least = c; }
   }
   p.cls[0] = {0, m_tiles, ceil_div(a.inner, best), 2 * best, 2 * best, 1, kb};
@@ -744,12 +751,9 @@ int classes_of(const Plan& plan, long long rows, int hidden, int inner, bool dx,
 }
 
 long long tiles_of(const TileClass& c) { return (long long)c.m_tiles * c.count * c.parts; }
-// of a tile: its stages and what starting the next one costs
-long long cycles_of(const TileClass& c, int columns) { return (long long)c.k_blocks * stage_cycles(columns) + 200; }
-
 // Widths and parts by an estimate of the longest load.  Parts of dx's depth, 2 * inner, serve few rows, whose dx is a
-// handful of very long tiles; joining them is another kernel of about 5000 cycles that moves 8 bytes a value and part, some
-// 3500 a cycle.
+// handful of very long tiles; joining them is another kernel of about 2200 cycles more that moves 8 bytes a value and part, some
+// 2800 a cycle.
 Plan plan_of(const FfnGradArgs& a) {
   Plan best;
   const int kb0 = 2 * ceil_div(a.inner, kDeep);
@@ -763,14 +767,14 @@ Plan plan_of(const FfnGradArgs& a) {
       const int count = classes_of(plan, a.rows, a.hidden, a.inner, a.dx != nullptr, a.dwg != nullptr, cls);
       long long work = 0, tiles = 0;
       for (int c = 0; c < count; ++c) {
-        work += (long long)cls[c].m_tiles * cls[c].parts * ((cls[c].count - 1) * cycles_of(cls[c], n) + cycles_of(cls[c], cls[c].last));
+        work += (long long)cls[c].m_tiles * cls[c].parts * ((cls[c].count - 1) * tile_cycles(cls[c].k_blocks, n) + tile_cycles(cls[c].k_blocks, cls[c].last));
         tiles += tiles_of(cls[c]);
       }
       // taken longest first, the pairs end within about half of a short tile of one another
-      const long long longest = cycles_of(cls[0], cls[0].count > 1 && n > cls[0].last ? n : cls[0].last);
-      plan.cycles = tiles <= a.pairs ? 0 : work / a.pairs + cycles_of(cls[count - 1], n) / 2;
+      const long long longest = tile_cycles(cls[0].k_blocks, cls[0].count > 1 && n > cls[0].last ? n : cls[0].last);
+      plan.cycles = tiles <= a.pairs ? 0 : work / a.pairs + tile_cycles(cls[count - 1].k_blocks, n) / 2;
       if (plan.cycles < longest) plan.cycles = longest;
-      plan.cycles += 16 * n + (parts > 1 ? 5000 + (long long)parts * a.rows * a.hidden * 8 / 3500 : 0);
+      plan.cycles += epilogue_cycles(n) + (parts > 1 ? 2200 + (long long)parts * a.rows * a.hidden * 8 / 2800 : 0);
       if (best.cycles < 0 || plan.cycles < best.cycles) best = plan;
     }
   }
