@@ -15,7 +15,7 @@
 // Bound by the tensor cores, and over longer stretches by the power limit: 8192 x 1600 x 6400 fp16 forward with g and u kept
 // 221 us (1520 TFLOP/s) after a pause and 295 us (1140) back to back, where the library's one product of the same size takes
 // 270; backward 603 and 724 us, of them about 80 for dg and du (memory), where the library's two products take 305 and 316 back to back.
-// A stage brings a multiprocessor 32 KB for 512 cycles of products, the 64 bytes a cycle that L2 delivers, so that smaller
+// A stage of a full tile brings a multiprocessor 32 KB for 512 cycles of products, about what L2 delivers, so that smaller
 // tiles are bound by that.  Waits that poll instead of sleeping cost the backward pass 11 % (695 against 622 us).
 
 #include <cuda.h>
