@@ -50,7 +50,8 @@ struct Lane {
   bool holds;
   int partner;                                // kPairsByShuffle: lane of the pairs' other members
   int half;
-  T* shared;                                  // kPairsByShared: 256 values of this warp
+  T* shared;                                  // kPairsByShared: 256 values of this warp, and where in them the partners of
+  int at[4];                                  // two neighbouring elements begin (half a rotation of an even number of elements)
 
   __device__ Lane(const QkArgs& a, T* sh) {
     lane = threadIdx.x & 31;
@@ -62,6 +63,10 @@ struct Lane {
     const int step = a.rot_dim / 16;          // pieces between the members of a pair
     partner = lane;
     if (MODE == kPairsByShuffle && piece < 2 * step) partner = lane + (piece < step ? step : -step);
+    if (MODE == kPairsByShared) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) at[j] = slot * W * 8 + partner_of(a, piece * 8 + 2 * j);
+    }
   }
   __device__ int partner_of(const QkArgs& a, int e) const {
     if (e >= a.rot_dim) return e;
@@ -118,8 +123,17 @@ struct Lane {
       __syncwarp();
       reinterpret_cast<uint4*>(shared)[lane] = v;
       __syncwarp();
+      if (half % 2 == 0) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) xp[j] = (float)shared[slot * W * 8 + partner_of(a, piece * 8 + j)];
+        for (int j = 0; j < 4; ++j) {
+          const float2 f = Num<T>::open(*reinterpret_cast<const uint32_t*>(shared + at[j]));
+          xp[2 * j] = f.x;
+          xp[2 * j + 1] = f.y;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) xp[j] = (float)shared[slot * W * 8 + partner_of(a, piece * 8 + j)];
+      }
     }
   }
 };
@@ -153,7 +167,7 @@ __device__ float inverse_root(float x) { float y; asm("rsqrt.approx.ftz.f32 %0, 
 
 // blockIdx.y: a batch of `per` passes of the queries' heads (the first batches_q) or the keys'
 template <typename T, int W, int MODE>
-__global__ void __launch_bounds__(kQkThreads, kCtas) qk_kernel(const QkArgs a, int batches_q, int per) {
+__global__ void __launch_bounds__(kQkThreads, MODE == kPairsByShared ? kCtas - 1 : kCtas) qk_kernel(const QkArgs a, int batches_q, int per) {
   __shared__ __align__(16) T exchange[MODE == kPairsByShared ? kQkWarps * 256 : 8];
   constexpr int H = 32 / W;
   const long long token = (long long)blockIdx.x * kQkWarps + threadIdx.x / 32;
