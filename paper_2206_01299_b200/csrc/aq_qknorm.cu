@@ -96,6 +96,20 @@ struct Lane {
       sn[0] = -s.x; sn[1] = s.x; sn[2] = -s.y; sn[3] = s.y; sn[4] = -s.z; sn[5] = s.z; sn[6] = -s.w; sn[7] = s.w;
       return;
     }
+    if (MODE == kPairsByShared && half % 2 == 0) {      // two consecutive pairs
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) {
+        const int e = e0 + j;
+        if (e >= a.rot_dim) break;
+        const bool second = e >= half;
+        const float2 c = __ldg(reinterpret_cast<const float2*>(table + (second ? e - half : e))), s = __ldg(reinterpret_cast<const float2*>(table + (second ? e : e + half)));
+        cs[j] = c.x;
+        cs[j + 1] = c.y;
+        sn[j] = second ? s.x : -s.x;
+        sn[j + 1] = second ? s.y : -s.y;
+      }
+      return;
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int e = e0 + j;
@@ -204,8 +218,19 @@ __global__ void __launch_bounds__(kQkThreads, MODE == kPairsByShared ? kCtas - 1
     } else if (MODE == kPairsByShuffle) {
       load_weights<T>(weights, l.partner & (W - 1), l.holds, wp);
     } else {
+      const T* const w0 = static_cast<const T*>(weights);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) wp[j] = l.holds ? (float)static_cast<const T*>(weights)[l.partner_of(a, l.piece * 8 + j)] : 1.0f;
+      for (int j = 0; j < 8; j += 2) {
+        const int e = l.piece * 8 + j, to = l.holds ? l.partner_of(a, e) : 0, to1 = l.holds ? l.partner_of(a, e + 1) : 0;
+        if (l.half % 2 == 0) {
+          const float2 f = Num<T>::open(__ldg(reinterpret_cast<const uint32_t*>(w0 + to)));
+          wp[j] = f.x;
+          wp[j + 1] = f.y;
+        } else {
+          wp[j] = (float)w0[to];
+          wp[j + 1] = (float)w0[to1];
+        }
+      }
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) { fa[j] *= w[j]; fb[j] *= wp[j]; }
