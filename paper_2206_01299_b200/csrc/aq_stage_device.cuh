@@ -56,10 +56,6 @@ __device__ bool barrier_wait(uint32_t bar, uint32_t parity, uint32_t* status) {
     if (barrier_try(bar, parity)) return true;
   return barrier_wait_long(bar, parity, status);
 }
-// `bytes` of this GPU's memory (16-byte aligned, a multiple of 16) into this CTA's shared memory, counted by a barrier
-__device__ void copy_in(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
-}
 // one lane waits for its warp
 __device__ bool warp_wait(int lane, uint32_t bar, uint32_t parity, uint32_t* status) {
   int ok = 1;
