@@ -393,7 +393,8 @@ typedef struct aq_stage aq_stage;
 
 /* On the current device; NULL on failure (aq_stage_last_error(NULL), aq_stage_last_error_code(NULL)). */
 aq_stage* aq_stage_create(void);
-/* Waits for the handle's stream, frees everything the handle owns.  NULL is allowed. */
+/* Waits for the handle's stream, frees everything the handle owns (graphs that captured its calls must not run afterwards).
+ * NULL is allowed. */
 void aq_stage_destroy(aq_stage* st);
 /* AQ_DTYPE (AQ_FP16, the default, AQ_BF16 or AQ_FP32; AQ_FP32 serves the token log probabilities only, the
  * other calls answer AQ_EUNSUPPORTED) or AQ_STREAM. */
@@ -457,7 +458,8 @@ int aq_gated_ffn(aq_stage* st, const void* x, int64_t ldx, const void* wg, const
  * dx T[rows][lddx] (out; may be null), dwg, dwu T[inner][lddw] (out; both or neither may be null).  dg and du
  * are rounded to T before the products (the tensor cores' operand type) and kept in the handle's workspace: 4 * rows * inner bytes,
  * and for few rows up to 256 MB for parts of dx.  It grows at the first call that needs more (that call synchronises the
- * stream and cannot be captured into a CUDA graph: AQ_EUNSUPPORTED).
+ * stream and cannot be captured into a CUDA graph: AQ_EUNSUPPORTED).  A captured graph keeps the workspace that it was captured
+ * with: the handle holds on to it beside a larger one until aq_stage_destroy, which the graph must not outlive.
  */
 int aq_gated_ffn_grad(aq_stage* st, const void* dh, int64_t lddh, const void* x, int64_t ldx, const void* wg, const void* wu,
                       int64_t ldw, const void* g, const void* u, int64_t ldgu, int64_t rows, int hidden, int inner, int act,

@@ -8,6 +8,12 @@
 #include <cstdio>
 #include <new>
 
+// A workspace that was outgrown while a captured graph may still hold its address.
+struct KeptBlock {
+  void* block;
+  KeptBlock* next;
+};
+
 struct aq_stage {
   int device = 0, sms = 0, pairs = 0;
   int dtype = AQ_FP16;
@@ -17,6 +23,8 @@ struct aq_stage {
   float* partials = nullptr;              // aq_qk_norm_rope_grad
   void* work = nullptr;                   // aq_gated_ffn_grad
   size_t work_bytes = 0;
+  bool work_captured = false;             // a stream capture has taken its address
+  KeptBlock* kept = nullptr;              // freed with the handle
   char err[256] = {0};
   int err_code = AQ_OK;
 };
@@ -55,19 +63,30 @@ struct DeviceGuard {
 
 int launched(aq_stage* st, cudaError_t e, const char* what) { return e == cudaSuccess ? AQ_OK : cuda_fail(st, e, what); }
 
-// Grows the workspace.  Work in flight may still use the old block, so the stream is drained first.
+// Makes the workspace at least that large.  A block whose address went into a captured graph is kept until the handle is destroyed,
+// for the graph may be replayed at any time; any other may still be used by work in flight, so the stream is drained before it is freed.
 int ensure_work(aq_stage* st, size_t bytes) {
-  if (st->work_bytes >= bytes) return AQ_OK;
   cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
   cudaError_t e = cudaStreamIsCapturing(st->stream, &capture);
   if (e != cudaSuccess) return cuda_fail(st, e, "cudaStreamIsCapturing");
+  if (st->work_bytes >= bytes) {
+    if (capture != cudaStreamCaptureStatusNone) st->work_captured = true;
+    return AQ_OK;
+  }
   if (capture != cudaStreamCaptureStatusNone)
     return fail(st, AQ_EUNSUPPORTED, "the workspace has to grow to %zu bytes, which a stream capture does not allow: run the call once before", bytes);
-  e = cudaStreamSynchronize(st->stream);
-  if (e != cudaSuccess) return cuda_fail(st, e, "cudaStreamSynchronize");
-  cudaFree(st->work);
+  if (st->work_captured) {
+    KeptBlock* const k = new (std::nothrow) KeptBlock{st->work, st->kept};
+    if (!k) return fail(st, AQ_ENOMEM, "host allocation failed");
+    st->kept = k;
+  } else {
+    e = cudaStreamSynchronize(st->stream);
+    if (e != cudaSuccess) return cuda_fail(st, e, "cudaStreamSynchronize");
+    cudaFree(st->work);
+  }
   st->work = nullptr;
   st->work_bytes = 0;
+  st->work_captured = false;
   e = cudaMalloc(&st->work, bytes);
   if (e != cudaSuccess) return cuda_fail(st, e, "workspace");
   st->work_bytes = bytes;
@@ -162,6 +181,12 @@ void aq_stage_destroy(aq_stage* st) {
   cudaFree(st->status);
   cudaFree(st->partials);
   cudaFree(st->work);
+  while (st->kept) {
+    KeptBlock* const k = st->kept;
+    st->kept = k->next;
+    cudaFree(k->block);
+    delete k;
+  }
   delete st;
 }
 
