@@ -492,7 +492,8 @@ int aq_qk_norm_rope(aq_stage* st, const aq_qk_shape* shape, int64_t rows, const 
 /*
  * Its gradient: dq, dk T (out, strides of their own; may be dq_out and dk_out themselves with the same strides) and dwq, dwk
  * float[head_dim] (out; summed over rows and heads; may be null) from dq_out, dk_out, the forward inputs
- * and the same tables.  A token with a position outside the table gets zeros and adds nothing to dwq and dwk.
+ * and the same tables.  A token with a position outside the table gets zeros and adds nothing to dwq and dwk, whatever its
+ * rows hold.  Elsewhere an infinite or NaN element makes elements of its own head NaN, and its own pair's columns of dwq or dwk.
  */
 int aq_qk_norm_rope_grad(aq_stage* st, const aq_qk_shape* shape, int64_t rows, const void* dq_out, int64_t dq_out_stride,
                          const void* dk_out, int64_t dk_out_stride, const void* q, int64_t q_stride, const void* k, int64_t k_stride,

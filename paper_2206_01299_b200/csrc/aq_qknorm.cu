@@ -328,10 +328,11 @@ __global__ void __launch_bounds__(kQkThreads, kGradCtas) qk_grad_kernel(const Qk
         }
         const bool mine = l.holds && at + (p + i) * step <= last;
         const float r = inverse_root(fmaf(sum_over_head<W>(l.holds ? ss : 0.0f), inv, a.eps));
-        const float mean = sum_over_head<W>(l.holds ? dot : 0.0f) * inv * r * r * r, rw = mine && position >= 0 ? r : 0.0f;
+        const float mean = sum_over_head<W>(l.holds ? dot : 0.0f) * inv * r * r * r;
+        const bool counts = mine && position >= 0;               // what does not may be NaN or infinite: left out, not times 0
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          dw[j] = fmaf(dy[j] * rw, x[j], dw[j]);
+          dw[j] = counts ? fmaf(dy[j] * r, x[j], dw[j]) : dw[j];
           dyp[j] = fmaf(dyp[j], r, -x[j] * mean);
         }
         if (mine) dst[at + (p + i) * step] = position >= 0 ? close8<T>(dyp) : make_uint4(0, 0, 0, 0);

@@ -88,3 +88,73 @@ def test_an_outgrown_workspace_that_no_graph_holds_is_freed(aq, stage):
         aq.aq_gated_ffn_grad(stage, g, inner, x, hidden, w, w, hidden, g, g, inner, i * 1024, hidden, inner, 0, None, 8, d[0], d[1], hidden)
     torch.cuda.synchronize()
     assert free - torch.cuda.mem_get_info()[0] < 1.5e9
+
+
+# ---- norm and rotation: what must not reach the weights' gradients --------------------------------------------------
+
+QK_WAYS = [  # rows, heads_q, heads_k, head_dim, rot, interleaved: each way to a pair's other member, heads that do and do not fill a warp
+    (40, 3, 2, 64, 64, False), (40, 5, 1, 64, 32, True), (40, 3, 3, 40, 40, False), (2500, 3, 1, 128, 64, False), (40, 7, 3, 24, 12, False)]
+
+
+def qk_grad_call(aq, st, shape, x, dy, nq, cs, positions, w):
+    """Outputs of the gradient call on [rows, (heads_q + heads_k) * head_dim] tensors, with the weights' sums."""
+    rows, ld = x.shape
+    out, dwq, dwk = torch.full_like(x, 5.0), floats(shape.head_dim), floats(shape.head_dim)
+    aq.aq_qk_norm_rope_grad(st, shape, rows, dy, ld, dy[:, nq:], ld, x, ld, x[:, nq:], ld, w, w, cs, positions, out, ld, out[:, nq:], ld, dwq, dwk)
+    torch.cuda.synchronize()
+    return out, dwq, dwk
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("rows,heads_q,heads_k,dh,rot,interleaved", QK_WAYS)
+def test_qk_gradient_tokens_outside_the_table_may_hold_anything(aq, stage, dtype, rows, heads_q, heads_k, dh, rot, interleaved):
+    """Padding is often uninitialised memory: its NaNs and infinities change no bit of anything."""
+    set_type(aq, stage, dtype)
+    t, nq, wide = forms.TYPES[dtype], heads_q * dh, (heads_q + heads_k) * dh
+    gen = torch.Generator().manual_seed(dh + rot)
+    x, dy = (torch.randn((rows, wide), generator=gen).to(t).cuda() for _ in range(2))
+    w = (1 + 0.3 * torch.randn(dh, generator=gen)).to(t).cuda()
+    positions = torch.randint(0, 40, (rows,), generator=gen, dtype=torch.int32)
+    off = torch.rand(rows, generator=gen) < 0.3
+    off[0], off[-1] = True, True
+    positions[off] = torch.where(torch.rand(int(off.sum()), generator=gen) < 0.5, -1, 40).int()
+    shape = aq.QkShape(heads_q=heads_q, heads_k=heads_k, head_dim=dh, rot_dim=rot, interleaved=int(interleaved), eps=1e-6, n_positions=40)
+    cs, positions, off = table(40, rot).cuda(), positions.cuda(), off.cuda()
+    want = qk_grad_call(aq, stage, shape, x, dy, nq, cs, positions, w)
+    assert aq.aq_stage_status(stage) == aq.AQ_ST_BAD_ID
+    assert all(bool(torch.isfinite(v).all()) for v in want)
+    n = int(off.sum())
+    junk = torch.tensor([math.nan, math.inf, -math.inf, 1.0])
+    for where in (x, dy):
+        kept = where.clone()
+        where[off] = junk[torch.randint(0, 4, (n, wide), generator=gen)].to(t).cuda()
+        got = qk_grad_call(aq, stage, shape, x, dy, nq, cs, positions, w)
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        if where is x:
+            where.copy_(kept)                                     # then in dy alone
+    assert aq.aq_stage_status(stage) == aq.AQ_ST_BAD_ID
+
+
+@pytest.mark.parametrize("rows,heads_q,heads_k,dh,rot,interleaved", QK_WAYS)
+@pytest.mark.parametrize("where", ["x", "dy"])
+def test_qk_gradient_an_infinity_stays_in_its_columns(aq, stage, rows, heads_q, heads_k, dh, rot, interleaved, where):
+    """One infinite element in the last head.  dw sums dy n over rows and heads, column by column: an infinite x_e makes n_e NaN and the
+    head's other n 0; an infinite dy_e reaches, turned back, its own column and that of the other member of its pair (neighbours,
+    where pairs are neighbours).  No other column, and no weight of the other tensor, may notice."""
+    set_type(aq, stage, "bf16")
+    nq, wide = heads_q * dh, (heads_q + heads_k) * dh
+    gen = torch.Generator().manual_seed(dh + rot)
+    x, dy = (torch.randn((rows, wide), generator=gen).bfloat16().cuda() for _ in range(2))
+    w = (1 + 0.3 * torch.randn(dh, generator=gen)).bfloat16().cuda()
+    positions = torch.randint(1, 40, (rows,), generator=gen, dtype=torch.int32).cuda()
+    shape = aq.QkShape(heads_q=heads_q, heads_k=heads_k, head_dim=dh, rot_dim=rot, interleaved=int(interleaved), eps=1e-6, n_positions=40)
+    for first, heads, which in ((0, heads_q, 1), (nq, heads_k, 2)):
+        for e in (dh - 1, dh - 8):
+            a, b = x.clone(), dy.clone()
+            (a if where == "x" else b)[rows // 2, first + (heads - 1) * dh + e] = math.inf
+            got = qk_grad_call(aq, stage, shape, a, b, nq, table(40, rot).cuda(), positions, w)
+            partner = e ^ 1 if interleaved else e if e >= rot else (e + rot // 2) % rot
+            touched = {e} if where == "x" else {e, partner}
+            assert bool(torch.isfinite(got[3 - which]).all())
+            assert set(torch.nonzero(~torch.isfinite(got[which])).flatten().tolist()) == touched
