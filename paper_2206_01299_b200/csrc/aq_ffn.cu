@@ -157,7 +157,7 @@ struct Products {
   float* partial;                             // dx in parts: float[parts][rows][cols], else null
   TileClass cls[kClasses];                    // the longest tiles first
   int tiles;                                  // of all classes
-  uint32_t* next;                             // tiles taken beyond each pair's first; 0 between launches
+  uint32_t* next;                             // tiles taken beyond each pair's first, pairs that take no more; both 0 between launches
   uint32_t format;
   uint32_t* status;
 };
@@ -346,7 +346,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
           if (!barrier_wait(tile_wanted, i & 1, p.status) || !barrier_wait(tile_read(slot), ((i >> 1) & 1) ^ 1, p.status)) break;
           barrier_expect(tile_sent(slot), 4);
           at = pairs + atomicAdd(p.next, 1u);
-          if (at == (unsigned)p.tiles + pairs - 1) *p.next = 0;      // the last one that any pair takes: for the next launch
           for (uint32_t r = 0; r < 2; ++r) send(in_cta(shared_address(&tile_ids[slot]), r), at, in_cta(tile_sent(slot), r));
         } else {
           barrier_expect(tile_sent(slot), 4);
@@ -356,6 +355,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
         }
         if (at >= (unsigned)p.tiles) break;
       }
+      // The last pair that has done with taking, however it came to that, leaves the counters as the next launch expects them.
+      __threadfence();                         // its takes come first
+      if (rank == 0 && atomicAdd(p.next + 1, 1u) == pairs - 1) { p.next[0] = 0; p.next[1] = 0; }
     }
   } else if (warp >= 4) {
     const int quarter = warp & 3, turn = (warp - 4) / 4;

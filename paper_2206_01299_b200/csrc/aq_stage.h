@@ -62,7 +62,7 @@ struct FfnArgs {
   void* h; long long ldh;
   void *g, *u; long long ldgu;            // may be null
   uint32_t* status;
-  uint32_t* next;                         // tiles taken; 0 between calls
+  uint32_t* next;                         // two counters of the CTA pairs; 0 between calls
   int pairs;                              // CTA pairs resident at a time
 };
 

@@ -158,3 +158,63 @@ def test_qk_gradient_an_infinity_stays_in_its_columns(aq, stage, rows, heads_q, 
             touched = {e} if where == "x" else {e, partner}
             assert bool(torch.isfinite(got[3 - which]).all())
             assert set(torch.nonzero(~torch.isfinite(got[which])).flatten().tolist()) == touched
+
+
+# ---- feed-forward: many tiles a pair ------------------------------------------------------------------------------
+
+def ffn_case(rows, hidden, inner, t, seed, pad=0):
+    """Operands of a call, its weights scaled to outputs near one; the 64-bit forms are evaluated on the GPU."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    put = lambda r, c, s=1.0: Guarded(r, c, t, pad).put(s * torch.randn((r, c), generator=gen, device="cuda"))  # noqa: E731
+    return put(rows, hidden), put(inner, hidden, hidden ** -0.5), put(inner, hidden, hidden ** -0.5)
+
+
+def call_ffn(aq, st, x, wg, wu, name, out):
+    rows, hidden = x.view.shape
+    aq.aq_gated_ffn(st, x.view, x.ld, wg.view, wu.view, wg.ld, rows, hidden, wg.view.shape[0], act_key(aq, name), *out)
+
+
+def forward_tiles(rows, inner):
+    return -(-rows // 256) * -(-inner // 128)                      # at least: a tile has 256 rows and up to 128 outputs
+
+
+def backward_tiles(rows, hidden, inner):
+    return (-(-rows // 256) + 2 * -(-inner // 256)) * -(-hidden // 256)     # at least: 256 x up to 256, dx whole
+
+
+def pairs_at_most():
+    return torch.cuda.get_device_properties(0).multi_processor_count // 2
+
+
+def test_gated_ffn_after_a_call_that_gave_up(aq, stage):
+    """A kernel whose wait ran out may leave its tile counter anywhere.  The counter is put there by hand (nothing else that is safe
+    makes a wait run out): the call that meets it is lost, the ones after it are whole again."""
+    import ctypes
+
+    class Head(ctypes.Structure):                                  # what the handle begins with
+        _fields_ = [("device", ctypes.c_int), ("sms", ctypes.c_int), ("pairs", ctypes.c_int), ("dtype", ctypes.c_int), ("stream", ctypes.c_void_p),
+                    ("status", ctypes.c_void_p), ("ticket", ctypes.c_void_p), ("next", ctypes.c_void_p)]
+    head = Head.from_address(stage)
+    assert head.sms == torch.cuda.get_device_properties(0).multi_processor_count and 0 < head.pairs <= head.sms // 2
+    assert head.ticket == head.status + 64 and head.next == head.status + 128
+    counter = torch.as_tensor(type("Word", (), {"__cuda_array_interface__": dict(shape=(1,), typestr="<i4", data=(head.next, False), version=3)})(), device="cuda")
+    rows, hidden, inner = 2100, 64, 2056                           # 9 x 17 tiles
+    assert forward_tiles(rows, inner) > head.pairs
+    x, wg, wu = ffn_case(rows, hidden, inner, torch.float16, 1)
+    h = torch.zeros((rows, inner), dtype=torch.float16, device="cuda")
+    out = (h, inner, None, None, inner)
+    call_ffn(aq, stage, x, wg, wu, "silu", out)
+    torch.cuda.synchronize()
+    want = h.clone()
+    assert counter.item() == 0
+    tiles = forward_tiles(rows, inner)
+    for left in (1, tiles - head.pairs, tiles - head.pairs + 3, tiles - 1, tiles, tiles + 1000):
+        counter.fill_(left)
+        torch.cuda.synchronize()
+        call_ffn(aq, stage, x, wg, wu, "silu", out)
+        torch.cuda.synchronize()
+        assert counter.item() == 0, left
+        h.zero_()
+        call_ffn(aq, stage, x, wg, wu, "silu", out)
+        torch.cuda.synchronize()
+        assert torch.equal(h, want) and counter.item() == 0, left
