@@ -258,22 +258,43 @@ def aq_import_sample(h, sample_id, m_host, seen):
 
 
 # ---- stage operators: buffers are named with their row strides, so a tensor may be a slice whose rows are contiguous.  A small
-# call takes a few microseconds on the GPU, so these wrappers do as little as they can.
+# call takes a few microseconds on the GPU, so these wrappers do as little as they can: a tensor's element type, place and
+# layout are checked (an int address is taken as it is), sizes and alignments by the library.
 
-def _row(x):
-    """Address of a tensor whose rows (last dimension) are contiguous, of an int address, or None."""
+_stage_types = {}        # handle: element type of its operands
+_i32 = _f32 = None       # torch.int32, torch.float32 once there is a handle
+
+
+def _row(x, t):
+    """Address of a CUDA tensor of type t whose rows (last dimension) are contiguous, of an int address, or None."""
     if x is None or type(x) is int:
         return x
-    assert x.is_contiguous() or x.stride(-1) == 1 or x.shape[-1] == 1, "rows must be contiguous"
-    return x.data_ptr()
+    if x.dtype is t and x.is_cuda and (x.is_contiguous() or x.stride(-1) == 1 or x.shape[-1] == 1):
+        return x.data_ptr()
+    _unfit(x, t, "contiguous rows")
 
 
-def _whole(x):
-    """Address of a contiguous tensor, an int address, or None."""
+def _whole(x, t):
+    """Address of a contiguous CUDA tensor of type t, an int address, or None."""
     if x is None or type(x) is int:
         return x
-    assert x.is_contiguous(), "tensor must be contiguous"
-    return x.data_ptr()
+    if x.dtype is t and x.is_cuda and x.is_contiguous():
+        return x.data_ptr()
+    _unfit(x, t, "contiguous elements")
+
+
+def _unfit(x, t, layout):
+    raise AssertionError(f"needs a CUDA tensor of {t} with {layout}, got {x.dtype} on {x.device} with strides {x.stride()}")
+
+
+def _stage_type(st, value):
+    global _i32, _f32
+    try:
+        import torch
+    except ImportError:  # then every operand is an address
+        return
+    _i32, _f32 = torch.int32, torch.float32
+    _stage_types[st] = {AQ_FP16: torch.float16, AQ_BF16: torch.bfloat16, AQ_FP32: torch.float32}[value]
 
 
 def _stage_error(st, rc):
@@ -284,16 +305,22 @@ def aq_stage_create():
     st = lib().aq_stage_create()
     if not st:
         raise AqError(aq_stage_last_error_code(None), aq_stage_last_error(None))
+    _stage_type(st, AQ_FP16)
     return st
 
 
 def aq_stage_destroy(st):
+    _stage_types.pop(st, None)
     lib().aq_stage_destroy(st)
 
 
 def aq_stage_configure(st, key, value):
     rc = lib().aq_stage_configure(st, key, value)
-    return rc and _stage_error(st, rc)
+    if rc:
+        _stage_error(st, rc)
+    if key == AQ_DTYPE:
+        _stage_type(st, value)
+    return rc
 
 
 def aq_stage_status(st):
@@ -311,39 +338,47 @@ def aq_stage_last_error_code(st):
 
 
 def aq_token_logprobs(st, logits, rows, vocab, ld, targets, scale, top_k, logprob, entropy, lse, top_ids, top_logprobs):
-    rc = (_lib or lib()).aq_token_logprobs(st, _row(logits), rows, vocab, ld, _whole(targets), scale, top_k, _whole(logprob),
-                                           _whole(entropy), _whole(lse), _whole(top_ids), _whole(top_logprobs))
+    rc = (_lib or lib()).aq_token_logprobs(st, _row(logits, _stage_types.get(st)), rows, vocab, ld, _whole(targets, _i32), scale, top_k,
+                                           _whole(logprob, _f32), _whole(entropy, _f32), _whole(lse, _f32), _whole(top_ids, _i32),
+                                           _whole(top_logprobs, _f32))
     return rc and _stage_error(st, rc)
 
 
 def aq_token_logprobs_grad(st, logits, rows, vocab, ld, targets, scale, lse, entropy, d_logprob, d_entropy, d_logits, ld_d):
-    rc = (_lib or lib()).aq_token_logprobs_grad(st, _row(logits), rows, vocab, ld, _whole(targets), scale, _whole(lse), _whole(entropy),
-                                                _whole(d_logprob), _whole(d_entropy), _row(d_logits), ld_d)
+    t = _stage_types.get(st)
+    rc = (_lib or lib()).aq_token_logprobs_grad(st, _row(logits, t), rows, vocab, ld, _whole(targets, _i32), scale, _whole(lse, _f32),
+                                                _whole(entropy, _f32), _whole(d_logprob, _f32), _whole(d_entropy, _f32), _row(d_logits, t), ld_d)
     return rc and _stage_error(st, rc)
 
 
 def aq_gated_ffn(st, x, ldx, wg, wu, ldw, rows, hidden, inner, act, h, ldh, g, u, ldgu):
-    rc = (_lib or lib()).aq_gated_ffn(st, _row(x), ldx, _row(wg), _row(wu), ldw, rows, hidden, inner, act, _row(h), ldh, _row(g),
-                                      _row(u), ldgu)
+    t = _stage_types.get(st)
+    rc = (_lib or lib()).aq_gated_ffn(st, _row(x, t), ldx, _row(wg, t), _row(wu, t), ldw, rows, hidden, inner, act, _row(h, t), ldh,
+                                      _row(g, t), _row(u, t), ldgu)
     return rc and _stage_error(st, rc)
 
 
 def aq_gated_ffn_grad(st, dh, lddh, x, ldx, wg, wu, ldw, g, u, ldgu, rows, hidden, inner, act, dx, lddx, dwg, dwu, lddw):
-    rc = (_lib or lib()).aq_gated_ffn_grad(st, _row(dh), lddh, _row(x), ldx, _row(wg), _row(wu), ldw, _row(g), _row(u), ldgu, rows,
-                                           hidden, inner, act, _row(dx), lddx, _row(dwg), _row(dwu), lddw)
+    t = _stage_types.get(st)
+    rc = (_lib or lib()).aq_gated_ffn_grad(st, _row(dh, t), lddh, _row(x, t), ldx, _row(wg, t), _row(wu, t), ldw, _row(g, t), _row(u, t),
+                                           ldgu, rows, hidden, inner, act, _row(dx, t), lddx, _row(dwg, t), _row(dwu, t), lddw)
     return rc and _stage_error(st, rc)
 
 
 def aq_qk_norm_rope(st, shape, rows, q, q_stride, k, k_stride, wq, wk, cos_sin, positions, q_out, q_out_stride, k_out, k_out_stride):
     """shape: a QkShape."""
-    rc = (_lib or lib()).aq_qk_norm_rope(st, C.addressof(shape), rows, _row(q), q_stride, _row(k), k_stride, _whole(wq), _whole(wk),
-                                         _whole(cos_sin), _whole(positions), _row(q_out), q_out_stride, _row(k_out), k_out_stride)
+    t = _stage_types.get(st)
+    rc = (_lib or lib()).aq_qk_norm_rope(st, C.addressof(shape), rows, _row(q, t), q_stride, _row(k, t), k_stride, _whole(wq, t),
+                                         _whole(wk, t), _whole(cos_sin, _f32), _whole(positions, _i32), _row(q_out, t), q_out_stride,
+                                         _row(k_out, t), k_out_stride)
     return rc and _stage_error(st, rc)
 
 
 def aq_qk_norm_rope_grad(st, shape, rows, dq_out, dq_out_stride, dk_out, dk_out_stride, q, q_stride, k, k_stride, wq, wk, cos_sin,
                          positions, dq, dq_stride, dk, dk_stride, dwq, dwk):
-    rc = (_lib or lib()).aq_qk_norm_rope_grad(st, C.addressof(shape), rows, _row(dq_out), dq_out_stride, _row(dk_out), dk_out_stride,
-                                              _row(q), q_stride, _row(k), k_stride, _whole(wq), _whole(wk), _whole(cos_sin),
-                                              _whole(positions), _row(dq), dq_stride, _row(dk), dk_stride, _whole(dwq), _whole(dwk))
+    t = _stage_types.get(st)
+    rc = (_lib or lib()).aq_qk_norm_rope_grad(st, C.addressof(shape), rows, _row(dq_out, t), dq_out_stride, _row(dk_out, t), dk_out_stride,
+                                              _row(q, t), q_stride, _row(k, t), k_stride, _whole(wq, t), _whole(wk, t),
+                                              _whole(cos_sin, _f32), _whole(positions, _i32), _row(dq, t), dq_stride, _row(dk, t),
+                                              dk_stride, _whole(dwq, _f32), _whole(dwk, _f32))
     return rc and _stage_error(st, rc)
