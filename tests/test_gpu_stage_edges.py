@@ -218,3 +218,111 @@ def test_gated_ffn_after_a_call_that_gave_up(aq, stage):
         call_ffn(aq, stage, x, wg, wu, "silu", out)
         torch.cuda.synchronize()
         assert torch.equal(h, want) and counter.item() == 0, left
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("rows,hidden,inner,pad", [(2100, 840, 2600, 8), (4000, 64, 1000, 0), (33, 72, 24008, 0), (1025, 200, 5000, 8)])
+def test_gated_ffn_of_many_tiles(aq, stage, dtype, rows, hidden, inner, pad):
+    """More tiles than the GPU holds pairs: every pair takes several, from the counter, with both halves of its tensor memory."""
+    assert forward_tiles(rows, inner) > pairs_at_most()
+    set_type(aq, stage, dtype)
+    t, u = forms.TYPES[dtype], forms.UNIT[dtype]
+    for name in ("silu", "gelu", "gelu_tanh"):
+        x, wg, wu = ffn_case(rows, hidden, inner, t, rows + hidden, pad)
+        h, g, up = Guarded(rows, inner, t, pad), Guarded(rows, inner, t, pad + 8), Guarded(rows, inner, t, pad + 8)
+        call_ffn(aq, stage, x, wg, wu, name, (h.view, h.ld, g.view, up.view, g.ld))
+        torch.cuda.synchronize()
+        for b in (h, g, up, x, wg, wu):
+            b.check()
+        x64, g64, u64 = x.view.double(), wg.view.double(), wu.view.double()
+        h_want, g_want, u_want = forms.ffn(x64, g64, u64, name)
+        e = 4 * math.sqrt(hidden) * 2 * E                          # as in test_gated_ffn
+        mg, mu = x64.abs() @ g64.abs().T, x64.abs() @ u64.abs().T
+        near(g.view, g_want, u * g_want.abs() + e * mg + forms.TINY[dtype])
+        near(up.view, u_want, u * u_want.abs() + e * mu + forms.TINY[dtype])
+        near(h.view, h_want, u * h_want.abs() + forms.TINY[dtype] + 1.13 * e * (mg * u_want.abs() + mu * g_want.abs()) + 16 * E * (g_want * u_want).abs())
+    assert aq.aq_stage_status(stage) == 0
+
+
+def near(got, want, tol):
+    """within(), on the GPU."""
+    off = (got.double() - want).abs()
+    assert bool((off <= tol).all()), float((off / tol).max())
+
+
+MANY_TILES = [  # several rounds of tiles: with a narrow last column of tiles (1400, 840), a widened one (264, 392), dx in parts (the last three)
+    (2100, 1400, 5000, 0), (2100, 840, 2600, 8), (300, 2048, 8192, 0), (1000, 264, 9000, 8), (1500, 392, 4104, 0)]
+
+
+def ffn_grad_case(rows, hidden, inner, t, seed, pad=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    put = lambda r, c, s=1.0: Guarded(r, c, t, pad).put(s * torch.randn((r, c), generator=gen, device="cuda"))  # noqa: E731
+    return [put(rows, inner), put(rows, hidden), put(inner, hidden, hidden ** -0.5), put(inner, hidden, hidden ** -0.5), put(rows, inner), put(rows, inner)]
+
+
+def call_ffn_grad(aq, st, ops, name, dx, dwg, dwu):
+    dh, x, wg, wu, g, u = ops
+    rows, hidden = x.view.shape
+    aq.aq_gated_ffn_grad(st, dh.view, dh.ld, x.view, x.ld, wg.view, wu.view, wg.ld, g.view, u.view, g.ld, rows, hidden, wg.view.shape[0],
+                         act_key(aq, name), dx.view if dx else None, dx.ld if dx else 8, dwg.view if dwg else None, dwu.view if dwu else None, dwg.ld if dwg else 8)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("rows,hidden,inner,pad", MANY_TILES)
+def test_gated_ffn_gradient_of_many_tiles(aq, stage, dtype, rows, hidden, inner, pad):
+    """Every element of dx and of the weights' gradients, all three outputs at once and apart."""
+    assert backward_tiles(rows, hidden, inner) > pairs_at_most()
+    set_type(aq, stage, dtype)
+    t, u, tiny = forms.TYPES[dtype], forms.UNIT[dtype], forms.TINY[dtype]
+    name = ("silu", "gelu", "gelu_tanh")[(rows + hidden) % 3]
+    ops = ffn_grad_case(rows, hidden, inner, t, rows + inner, pad)
+    dh, x, wg, wu, g, up = (b.view.double() for b in ops)
+    dg, du, dx, dwg, dwu = forms.ffn_grad(dh, x, wg, wu, g, up, name)
+    eg = u * dg.abs() + tiny + 16 * E * (dh * up).abs() * (1 + g.abs())               # as in test_gated_ffn_gradient
+    eu = u * du.abs() + tiny + 16 * E * (dh * g).abs()
+    em, er = 4 * math.sqrt(2 * inner) * 2 * E, 4 * math.sqrt(rows) * 2 * E
+    dx_tol = u * dx.abs() + tiny + eg @ wg.abs() + eu @ wu.abs() + em * (dg.abs() @ wg.abs() + du.abs() @ wu.abs())
+    wg_tol = u * dwg.abs() + tiny + eg.T @ x.abs() + er * (dg.abs().T @ x.abs())
+    wu_tol = u * dwu.abs() + tiny + eu.T @ x.abs() + er * (du.abs().T @ x.abs())
+    for want_dx, want_dw in ((True, True), (True, False), (False, True)):
+        o = [Guarded(r, hidden, t, pad + 8) for r in (rows, inner, inner)]
+        call_ffn_grad(aq, stage, ops, name, o[0] if want_dx else None, o[1] if want_dw else None, o[2] if want_dw else None)
+        torch.cuda.synchronize()
+        for b in ops + o:
+            b.check()
+        if want_dx:
+            near(o[0].view, dx, dx_tol)
+        if want_dw:
+            near(o[1].view, dwg, wg_tol)
+            near(o[2].view, dwu, wu_tol)
+    assert aq.aq_stage_status(stage) == 0
+
+
+def test_two_handles_with_many_tiles_each(aq):
+    """Calls of several rounds of tiles on two handles and streams side by side: each takes its tiles from its own counter."""
+    rows, hidden, inner = 1500, 392, 4104
+    ops = ffn_grad_case(rows, hidden, inner, torch.bfloat16, 3)
+    assert backward_tiles(rows, hidden, inner) > pairs_at_most() and forward_tiles(rows, inner) > pairs_at_most()
+    sides = []
+    for _ in range(2):
+        st, stream = aq.aq_stage_create(), torch.cuda.Stream()
+        set_type(aq, st, "bf16")
+        aq.aq_stage_configure(st, aq.AQ_STREAM, stream.cuda_stream)
+        sides.append((st, [Guarded(rows, inner, torch.bfloat16)] + [Guarded(r, hidden, torch.bfloat16) for r in (rows, inner, inner)]))
+    torch.cuda.synchronize()
+
+    def calls(st, o):
+        call_ffn(aq, st, ops[1], ops[2], ops[3], "gelu", (o[0].view, o[0].ld, None, None, o[0].ld))
+        call_ffn_grad(aq, st, ops, "gelu", *o[1:])
+    calls(*sides[0])
+    torch.cuda.synchronize()
+    want = [b.flat.clone() for b in sides[0][1]]
+    for _ in range(10):
+        for side in sides:
+            calls(*side)
+    torch.cuda.synchronize()
+    for st, o in sides:
+        assert aq.aq_stage_status(st) == 0
+        for b, w in zip(o, want):
+            assert torch.equal(b.flat, w)
+        aq.aq_stage_destroy(st)
