@@ -39,7 +39,9 @@ template <> struct Operand<__nv_bfloat16> {
 };
 
 // Phi(-|g|), the normal distribution's tail: e^(-g^2/2) times a polynomial in t = 1 / (1 + 0.375 |g| / sqrt(2)), fitted to
-// erfc(x) e^(x^2) / 2 over x = 0..12 by reweighted least squares (relative error 2.5e-8; 4e-7 as evaluated here).
+// erfc(x) e^(x^2) / 2 over x = 0..12 by reweighted least squares.  The fit is good to 4.5e-8; as evaluated here, in binary32, what
+// counts is the rounding of the exponent: relative error 4.8e-7 up to |g| = 2, 1.5e-6 up to 5, 2.8e-6 up to 8, 7.6e-6 up
+// to 13, far below one rounding of the 16-bit outputs (4.9e-4 or 3.9e-3) everywhere.
 // Against erfcf: the forward kernel's epilogue at 256 x 128 outputs a tile 15000 cycles with erfcf.
 __device__ float normal_tail(float g) {
   const float x = fabsf(g), t = __fdividef(1.0f, fmaf(x, 0.2651650429f, 1.0f));

@@ -326,3 +326,59 @@ def test_two_handles_with_many_tiles_each(aq):
         for b, w in zip(o, want):
             assert torch.equal(b.flat, w)
         aq.aq_stage_destroy(st)
+
+
+# ---- the activations over their whole range ----------------------------------------------------------------------------
+
+ACT_RANGE = torch.cat([torch.linspace(-14, 14, 1601), torch.linspace(-100, 100, 401), torch.tensor([-0.0, 1e-4, -1e-4, 1e4, -1e4])])
+
+
+def exponent_of(name, g):
+    """The largest exponent that the form of an activation at g raises e to."""
+    return {"silu": g.abs(), "gelu": 0.5 * g * g, "gelu_tanh": 1.6 * g.abs() * (1 + 0.0448 * g * g)}[name]
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("name", ["silu", "gelu", "gelu_tanh"])
+def test_activations_relative_to_their_own_size(aq, stage, dtype, name):
+    """g and u = 1 through weights that pass them on, so that h = act(g), du = act(g) and dg = act'(g).
+
+    Relative to the value: one rounding of the type; the exponent y of e^y is formed in up to four roundings (a product or two, and
+    times log2 e), which cost 4 E |y|, and the rest (polynomial, reciprocal, products) 16 E.  For the derivative, whose two
+    terms cancel near its zero, relative to the sum of their magnitudes.  Below: e^-y beyond 2^126 counts as infinite, so
+    sigmoids under 2^-125 may be 0, which g (in the derivative, g y') magnifies."""
+    set_type(aq, stage, dtype)
+    t, u = forms.TYPES[dtype], forms.UNIT[dtype]
+    v = ACT_RANGE.to(t)
+    n = v.numel()
+    g = v.double()
+    y = math.sqrt(8 / math.pi) * (g + 0.044715 * g ** 3)
+    x = torch.zeros((n, 16), dtype=t)
+    x[:, 0], x[:, 8] = v, 1.0
+    wg, wu = torch.zeros((8, 16), dtype=t), torch.zeros((8, 16), dtype=t)
+    wg[:, 0], wu[:, 8] = 1.0, 1.0
+    few = torch.empty((16, 8), dtype=t, device="cuda")             # the kernel for few rows, too
+    h, gg, uu = (torch.empty((n, 8), dtype=t, device="cuda") for _ in range(3))
+    args = (16, wg.cuda(), wu.cuda(), 16)
+    aq.aq_gated_ffn(stage, x.cuda(), *args, n, 16, 8, act_key(aq, name), h, 8, gg, uu, 8)
+    aq.aq_gated_ffn(stage, x[:1600:100].contiguous().cuda(), *args, 16, 16, 8, act_key(aq, name), few, 8, None, None, 8)
+    # sigma or Phi, never as one minus something, and what multiplies g in the derivative
+    over, bend = {"silu": lambda: (torch.sigmoid(g), torch.sigmoid(g) * torch.sigmoid(-g)),
+                  "gelu": lambda: (0.5 * torch.erfc(-g / math.sqrt(2.0)), torch.exp(-0.5 * g * g) / math.sqrt(2 * math.pi)),
+                  "gelu_tanh": lambda: (torch.sigmoid(y), torch.sigmoid(y) * torch.sigmoid(-y) * math.sqrt(8 / math.pi) * (1 + 3 * 0.044715 * g * g))}[name]()
+    value, slope = g * over, over + g * bend
+    rough = 16 * E + 4 * E * exponent_of(name, g)
+    floor = forms.TINY[dtype] + 2.0 ** -125 * (1 + g.abs())
+    tol = (u * value.abs() + rough.clamp(max=1.0) * value.abs() + floor)[:, None].expand(n, 8)
+    within(h, value[:, None].expand(n, 8), tol)
+    within(few, value[:1600:100, None].expand(16, 8), tol[:1600:100])
+    # dx = dg wg + du wu with wg, wu the two halves of an identity, dh = u = 1
+    one = torch.ones((n, 8), dtype=t, device="cuda")
+    wg, wu, zero = torch.zeros((8, 16), dtype=t), torch.zeros((8, 16), dtype=t), torch.zeros((8, 16), dtype=t, device="cuda")
+    wg[:, :8], wu[:, 8:] = torch.eye(8), torch.eye(8)
+    dx = torch.empty((n, 16), dtype=t, device="cuda")
+    aq.aq_gated_ffn_grad(stage, one, 8, x.cuda(), 16, wg.cuda(), wu.cuda(), 16, gg, one, 8, n, 16, 8, act_key(aq, name), dx, 16, None, None, 16)
+    size, steep = over + (g * bend).abs(), 1.6 * (1 + 0.135 * g * g) if name == "gelu_tanh" else torch.ones_like(g)
+    slope_tol = u * slope.abs() + rough.clamp(max=1.0) * size + forms.TINY[dtype] + 2.0 ** -125 * (1 + (g * steep).abs())
+    within(dx[:, :8], slope[:, None].expand(n, 8), slope_tol[:, None].expand(n, 8))
+    within(dx[:, 8:], value[:, None].expand(n, 8), tol)
