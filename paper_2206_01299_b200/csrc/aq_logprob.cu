@@ -40,6 +40,7 @@ constexpr float kUnset = -1e6f;               // reference before the first larg
 constexpr float kGone = -1e4f;                // exponents below give exactly 0; also keeps 0 * -infinity out of t
 constexpr float kClear = 200.0f;              // exponentials this far below the largest are 0 in binary32 sums
 constexpr float kFar = 1e6f;                  // largest |y| of a row's maximum that the sums take in their stride: its rounding is 1/32 there
+constexpr float kHuge = 1e38f;                // exponents beyond are about to overflow
 constexpr float kSlack = 8.0f;                // how far a value may exceed the reference before it is moved: 2^8 is
                                               // nothing to a binary32 sum, and the move leaves the loop's common path
 
@@ -352,11 +353,14 @@ __device__ void join_lanes(Sums& a) {
 }
 
 // Whether the sums of a pass do not stand: logits so large that rounding the reference already moves it by whole units, or so
-// low (all of them masked, perhaps) that raising the masked ones to kLow would show.
+// low (all of them masked, perhaps) that raising the masked ones to kLow would show, or a scale so large that they overflow.
 template <typename T> __device__ bool far(float top, float s, float c) {
   if (top == -CUDART_INF_F && s == 0.0f) return false;         // nothing but -infinity
-  return fabsf(top) * c > kFar || (Pack<T>::kLow > -CUDART_INF_F && (top - Pack<T>::kLow) * c < kClear);
+  const float above = (top - Pack<T>::kLow) * c;
+  return fabsf(top) * c > kFar || (Pack<T>::kLow > -CUDART_INF_F && (above < kClear || above > kHuge));
 }
+// c; a scale near the end of binary32 would make it infinite
+__device__ float base2(float scale) { return fminf(scale * kLog2e, 3.4e38f); }
 
 // Calls f with every logit of a row; the whole CTA, `part` being all of the row.
 template <typename T, typename F> __device__ void each_logit(const Part<T>& part, F f) {
@@ -383,7 +387,7 @@ template <typename T, typename F> __device__ void each_logit(const Part<T>& part
 template <typename T>
 __device__ void far_row(RowShared& sh, const Part<T>& part, float scale) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const float c = scale * kLog2e;
+  const float c = base2(scale);
   float top = -CUDART_INF_F, s = 0.0f, t = 0.0f;
   each_logit(part, [&](float x) { top = fmaxf(top, x); });
   top = warp_max(top);
@@ -438,7 +442,7 @@ __global__ void __launch_bounds__(kRowThreads, kRanks > 1 ? 1 : kRowCtas) logpro
   const long long row = blockIdx.x / kRanks;
   const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
   const Part<T> part(x, (unsigned)a.vocab, rank, kRanks);
-  const float c = a.scale * kLog2e;
+  const float c = base2(a.scale);
   if constexpr (kRanks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
 
   Sums2 sums;
@@ -597,7 +601,7 @@ __global__ void __launch_bounds__(kRowThreads) logprob_short_kernel(const Logpro
     }
     if (edge) f(edge_x, edge_id);
   };
-  const float c = a.scale * kLog2e;
+  const float c = base2(a.scale);
   float top = -CUDART_INF_F, s = 0.0f, t = 0.0f;
   each([&](float e, unsigned) { top = fmaxf(top, e); });
   top = warp_max(top);
@@ -664,7 +668,7 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
   const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
   T* const out = static_cast<T*>(a.d_logits) + row * a.ld_d;
   const unsigned vocab = (unsigned)a.vocab;
-  const float c = a.scale * kLog2e;
+  const float c = base2(a.scale);
   // c's own rounding matters to binary32 outputs only
   const float c_lo = fmaf(a.scale, kLog2eRest, fmaf(a.scale, kLog2e, -c));
   const float lse = a.lse[row], entropy = a.d_entropy ? a.entropy[row] : 0.0f;
@@ -682,10 +686,11 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
     for (unsigned i = i0 + tid; i < i1; i += LANES) out[i] = Pack<T>::round(0.0f);
     return;
   }
-  const float ref = lse * kLog2e;
-  if (!(fabsf(lse) <= kFarLse) || Pack<T>::kLow * c - ref > -kClear) {
+  const float ref = lse * kLog2e, low = Pack<T>::kLow * c - ref;
+  if (!(fabsf(lse) <= kFarLse) || low > -kClear || (Pack<T>::kLow > -CUDART_INF_F && low < -kHuge)) {
     // the first piece's CTA does the whole row: the logits are so large that lse has no digits left for ln p (or so low or little
-    // scaled that raising the masked ones would show), and the row's own sum is formed again, relative to its largest logit
+    // scaled that raising the masked ones would show, or scaled so much that they overflow), and the row's own sum is formed again,
+    // relative to its largest logit
     if (piece) return;
     __shared__ float part[kRowWarps];
     float top = -CUDART_INF_F;

@@ -382,3 +382,30 @@ def test_activations_relative_to_their_own_size(aq, stage, dtype, name):
     slope_tol = u * slope.abs() + rough.clamp(max=1.0) * size + forms.TINY[dtype] + 2.0 ** -125 * (1 + (g * steep).abs())
     within(dx[:, :8], slope[:, None].expand(n, 8), slope_tol[:, None].expand(n, 8))
     within(dx[:, 8:], value[:, None].expand(n, 8), tol)
+
+
+# ---- log probabilities far from zero, and with extreme scales -----------------------------------------------------------
+
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("rows,vocab", [(3, 700), (2, 9001), (90, 9001)])
+@pytest.mark.parametrize("scale", [1e34, 3e38])
+def test_logprobs_with_a_very_large_scale(aq, stage, dtype, rows, vocab, scale):
+    """1 / temperature near the end of binary32: nothing but the largest logits is left, whatever is masked."""
+    set_type(aq, stage, dtype)
+    x = torch.zeros((rows, vocab))
+    x[:, ::3] = -math.inf
+    x[:, 1::3] = -2.0
+    x[1] = torch.where(torch.arange(vocab) < 5, 0.0, -math.inf)
+    x = x.to(forms.TYPES[dtype])
+    targets = torch.full((rows,), 2, dtype=torch.int32)
+    buf, out = Guarded(rows, vocab, forms.TYPES[dtype]).put(x), Guarded(rows, vocab, forms.TYPES[dtype])
+    got = run_logprobs(aq, stage, buf, targets, scale, 4)
+    check_logprobs(x.double(), targets, scale, 4, got)
+    gl = torch.full((rows,), 1 / scale)
+    run_logprobs_grad(aq, stage, buf, out, targets.cuda(), scale, got[2].float().cuda(), got[1].float().cuda(), gl.cuda(), gl.cuda())
+    s32, l32 = (torch.tensor(v, dtype=torch.float32).double().item() for v in (scale, 1 / scale))
+    for r in (0, 1, rows - 1):
+        want = forms.logprobs_grad(x[r].double(), 2, s32, l32, l32)
+        within(out.view[r], want, forms.UNIT[dtype] * want.abs() + forms.TINY[dtype] + 1e-4 * want.abs() + 1e-5)
