@@ -690,7 +690,8 @@ __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const Logprob
   if (!(fabsf(lse) <= kFarLse) || low > -kClear || (Pack<T>::kLow > -CUDART_INF_F && low < -kHuge)) {
     // the first piece's CTA does the whole row: the logits are so large that lse has no digits left for ln p (or so low or little
     // scaled that raising the masked ones would show, or scaled so much that they overflow), and the row's own sum is formed again,
-    // relative to its largest logit
+    // relative to its largest logit.  Three passes by one CTA: 4096 x 50264 bf16 rows 156 us with one in a hundred of them so,
+    // 190 us with one in ten, 476 us with all (120 us with none; binary32, twice the bytes, 820 us with all).
     if (piece) return;
     __shared__ float part[kRowWarps];
     float top = -CUDART_INF_F;

@@ -409,3 +409,43 @@ def test_logprobs_with_a_very_large_scale(aq, stage, dtype, rows, vocab, scale):
     for r in (0, 1, rows - 1):
         want = forms.logprobs_grad(x[r].double(), 2, s32, l32, l32)
         within(out.view[r], want, forms.UNIT[dtype] * want.abs() + forms.TINY[dtype] + 1e-4 * want.abs() + 1e-5)
+
+
+@pytest.mark.parametrize("dtype,offset,scale", [("fp16", 7000.0, 1.0), ("fp16", -30000.0, 0.25), ("bf16", 20000.0, 0.25), ("fp32", 5000.0, 1.0), ("fp32", -1e6, 1.0),
+                                                ("fp32", 1e30, 2.0 ** -75)])
+@pytest.mark.parametrize("rows,vocab", [(3, 700), (2, 30011)])
+def test_logprobs_gradient_of_far_rows(aq, stage, dtype, offset, scale, rows, vocab):
+    """Rows whose logits lie far from zero, where lse has no digits left for ln p, with a distribution under the offset: steps of
+    the type there (0.5 at least), some masked; beside a row that is near zero.
+
+    The gradient forms the row's sum again relative to its largest logit, so p is good to the sum's 2e-5 and 4 E of the distance;
+    only the entropy, an input, and the output's rounding come on top."""
+    set_type(aq, stage, dtype)
+    t = forms.TYPES[dtype]
+    gen = torch.Generator().manual_seed(vocab)
+    step = 2.0 ** (math.floor(math.log2(abs(offset))) - {"fp16": 10, "bf16": 7, "fp32": 23}[dtype])
+    unit = max(step, 0.5)
+    x = offset - unit * torch.randint(0, 7, (rows, vocab), generator=gen, dtype=F64)
+    x[torch.rand((rows, vocab), generator=gen) < 0.1] = -math.inf
+    x[-1] = 3 * torch.randn(vocab, generator=gen, dtype=F64)
+    x[:, vocab // 3] = torch.where(torch.isfinite(x[:, vocab // 3]), x[:, vocab // 3], offset)
+    x = x.to(t)
+    targets = torch.full((rows,), vocab // 3, dtype=torch.int32)
+    s32 = torch.tensor(scale, dtype=torch.float32).double().item()
+    assert abs(x[0].double().max().item() * s32) > 4096
+    buf, out = Guarded(rows, vocab, t, 3, 1).put(x), Guarded(rows, vocab, t, 3, 1)
+    lp, h, lse, _, _ = run_logprobs(aq, stage, buf, targets, scale, 0)
+    gl, gh = torch.randn(rows, generator=gen), torch.randn(rows, generator=gen)
+    run_logprobs_grad(aq, stage, buf, out, targets.cuda(), scale, lse.float().cuda(), h.float().cuda(), gl.cuda(), gh.cuda())
+    out.check()
+    for r in range(rows):
+        z = x[r].double() * s32
+        want = forms.logprobs_grad(x[r].double(), int(targets[r]), s32, gl[r].item(), gh[r].item())
+        p = torch.softmax(z, 0)
+        below = torch.where(p > 0, torch.log_softmax(z, 0), torch.zeros_like(z))
+        hh = -(p * below).sum()
+        size = s32 * p * (abs(gl[r].item()) + abs(gh[r].item()) * (below.abs() + hh))
+        near_zero = 2 * E * (z[p > 0].abs().max() + abs(lse[r].item())) if abs(lse[r].item()) < 4096 else 0.0      # lse's own digits
+        size[int(targets[r])] += s32 * abs(gl[r].item())
+        tol = forms.UNIT[dtype] * want.abs() + forms.TINY[dtype] + size * (6e-5 + E * (8 + 4 * below.abs()) + near_zero) + s32 * 4e-5 * abs(gh[r].item()) * p
+        within(out.view[r], want, tol)
