@@ -601,7 +601,8 @@ using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, 
                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 cudaError_t encoder(EncodeTiled* out) {
-  static EncodeTiled fn = nullptr;            // the same address for every thread that finds it
+  static std::atomic<EncodeTiled> known{nullptr};          // the same address for every thread that finds it
+  EncodeTiled fn = known.load(std::memory_order_relaxed);
   if (!fn) {
     void* p = nullptr;
     cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
@@ -609,6 +610,7 @@ cudaError_t encoder(EncodeTiled* out) {
     if (e != cudaSuccess) return e;
     if (found != cudaDriverEntryPointSuccess || !p) return cudaErrorNotSupported;
     fn = reinterpret_cast<EncodeTiled>(p);
+    known.store(fn, std::memory_order_relaxed);
   }
   *out = fn;
   return cudaSuccess;

@@ -386,8 +386,6 @@ def test_activations_relative_to_their_own_size(aq, stage, dtype, name):
 
 # ---- log probabilities far from zero, and with extreme scales -----------------------------------------------------------
 
-
-
 @pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
 @pytest.mark.parametrize("rows,vocab", [(3, 700), (2, 9001), (90, 9001)])
 @pytest.mark.parametrize("scale", [1e34, 3e38])
@@ -449,3 +447,46 @@ def test_logprobs_gradient_of_far_rows(aq, stage, dtype, offset, scale, rows, vo
         size[int(targets[r])] += s32 * abs(gl[r].item())
         tol = forms.UNIT[dtype] * want.abs() + forms.TINY[dtype] + size * (6e-5 + E * (8 + 4 * below.abs()) + near_zero) + s32 * 4e-5 * abs(gh[r].item()) * p
         within(out.view[r], want, tol)
+
+
+# ---- several host threads ---------------------------------------------------------------------------------------------------
+
+def test_host_threads_with_a_handle_each():
+    """Four threads make their handles and call side by side, in a process of its own so that their first calls are the library's first."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import threading, torch
+import paper_2206_01299_b200 as aq
+rows, hidden, inner = 300, 136, 520
+g = torch.Generator(device="cuda").manual_seed(1)
+x, wg, wu, dh = (torch.randn(s, generator=g, device="cuda").half() for s in ((rows, hidden), (inner, hidden), (inner, hidden), (rows, inner)))
+torch.cuda.synchronize()
+outs, errors, ready = [None] * 4, [], threading.Barrier(4)
+def work(i):
+    try:
+        st, stream = aq.aq_stage_create(), torch.cuda.Stream()
+        aq.aq_stage_configure(st, aq.AQ_STREAM, stream.cuda_stream)
+        with torch.cuda.stream(stream):
+            h, g, u = (torch.empty_like(dh) for _ in range(3))
+            d = [torch.empty_like(v) for v in (x, wg, wu)]
+        stream.synchronize()
+        ready.wait()
+        for _ in range(10):
+            aq.aq_gated_ffn(st, x, hidden, wg, wu, hidden, rows, hidden, inner, aq.AQ_ACT_GELU, h, inner, g, u, inner)
+            aq.aq_gated_ffn_grad(st, dh, inner, x, hidden, wg, wu, hidden, g, u, inner, rows, hidden, inner, aq.AQ_ACT_GELU, d[0], hidden, d[1], d[2], hidden)
+        assert aq.aq_stage_status(st) == 0
+        aq.aq_stage_destroy(st)
+        outs[i] = [h, g, u] + d
+    except Exception as e:
+        errors.append(e)
+threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+[t.start() for t in threads]
+[t.join() for t in threads]
+assert not errors, errors
+assert all(torch.equal(a, b) for o in outs[1:] for a, b in zip(o, outs[0])) and torch.isfinite(outs[0][0]).all()
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
