@@ -122,8 +122,8 @@ enum {
                             prefetched for it; that sample is skipped */
   AQ_ST_BAD_PTR = 16,    /* a list-form call found a null or misaligned pointer in one of its arrays; nothing
                             is read or written for that sample */
-  AQ_ST_STALLED = 32     /* stage handles: a kernel gave up on a wait that should have ended (every wait in a kernel
-                            is bounded); the outputs of that call are not valid */
+  AQ_ST_STALLED = 32     /* stage handles: a kernel gave up on a wait that should have ended (its waits for copies, products and
+                            tiles end after four seconds); the outputs of that call are not valid */
 };
 
 /*
@@ -456,7 +456,8 @@ int aq_gated_ffn(aq_stage* st, const void* x, int64_t ldx, const void* wg, const
  *   dg = dh * u * act'(g),  du = dh * act(g),
  *   dx = dg wg + du wu,  dwg = dg^T x,  dwu = du^T x
  * dx T[rows][lddx] (out; may be null), dwg, dwu T[inner][lddw] (out; both or neither may be null).  dg and du
- * are rounded to T before the products (the tensor cores' operand type) and kept in the handle's workspace: 4 * rows * inner bytes,
+ * are rounded to T before the products (the tensor cores' operand type), so that in fp16 a |dg| or |du| above 65504 is infinite and
+ * one below 6e-8 is 0, whatever the products would have made of it: scale the loss for that.  They are kept in the handle's workspace: 4 * rows * inner bytes,
  * and for few rows up to 256 MB for parts of dx.  It grows at the first call that needs more (that call synchronises the
  * stream and cannot be captured into a CUDA graph: AQ_EUNSUPPORTED).  A captured graph keeps the workspace that it was captured
  * with: the handle holds on to it beside a larger one until aq_stage_destroy, which the graph must not outlive.

@@ -13,8 +13,8 @@
 //   dW        A = dg (du) read across its rows (M-major), B = x N-major: the sum runs over the tokens
 //
 // Bound by the tensor cores, and over longer stretches by the power limit: 8192 x 1600 x 6400 fp16 forward with g and u kept
-// 221 us (1520 TFLOP/s) after a pause and 295 us (1140) back to back, where the library's one product of the same size takes
-// 270; backward 603 and 724 us, of them about 80 for dg and du (memory), where the library's two products take 305 and 316 back to back.
+// 221 us (1520 TFLOP/s) after a pause and 286 to 302 us (1110 to 1170) back to back, where the library's one product of the same
+// size takes 270; backward 603 and 698 to 736 us, of them about 80 for dg and du (memory), where the library's two products take 305 and 316 back to back.
 // A stage of a full tile brings a multiprocessor 32 KB for 512 cycles of products, about what L2 delivers, so that smaller
 // tiles are bound by that.  Waits that poll instead of sleeping cost the backward pass 11 % (695 against 622 us).
 
@@ -444,7 +444,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFfnThreads, 1) prod
   if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tensor), "r"(kColumns) : "memory");
 }
 
-// dg and du to the workspace, eight elements per thread
+// dg and du to the workspace, eight elements per thread.  Rounded to T, what the tensor cores take: two 16-bit parts of each would be
+// twice the products.  The one rounding more takes the relative error of dx and dW from 2.1e-4 to 2.9e-4 (fp16) and from 1.7e-3
+// to 2.4e-3 (bf16).
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256) ffn_dgu_kernel(const FfnGradArgs a) {
   next_may_launch();

@@ -9,8 +9,8 @@
 // costs no digits.
 //
 // Three limits lie close together: memory (8192 x 50304 bf16: 126 us), one exponential a logit (91 us) and the issue of
-// instructions (about 80 us); the pass takes 168 us, 4.9 TB/s.  The gradient reads and writes each logit once: 4096 x 50257
-// bf16 137 us, 6.0 TB/s.  What did not help the pass: loads one step ahead (180 us), rows streamed through a ring in shared
+// instructions (about 80 us); the pass takes 164 to 179 us, 4.6 to 5.0 TB/s (2048 rows under a profiler: issue slots 0.68,
+// exponentials 0.55, DRAM 0.54).  The gradient reads and writes each logit once: 4096 x 50257 bf16 134 to 140 us, 5.9 to 6.1 TB/s.  What did not help the pass: loads one step ahead (180 us), rows streamed through a ring in shared
 // memory by CTAs that stay, instructions on pairs of binary32 values, 128 threads to a row.
 
 #include <cooperative_groups.h>

@@ -11,8 +11,8 @@
 // values a word.  A warp's loads are all issued before it waits for its token's position.
 //
 // Bound by memory in the first place, 2 T per element forward and 3 T backward and a position's factors once per token, with the
-// issue of instructions (about 15 per element) close behind.  Forward, 32768 tokens of 25 + 25 heads of 64: 77 us, 5.4 TB/s;
-// backward, 16384 tokens of 24 + 8 heads of 64: 52 us, 3.9 TB/s.  What did not help: two pieces a lane, which spares the exchange
+// issue of instructions (about 15 per element) close behind.  Forward, 32768 tokens of 25 + 25 heads of 64: 77 to 82 us, 5.1 to
+// 5.4 TB/s (issue slots 0.73 under a profiler); backward, 16384 tokens of 24 + 8 heads of 64: 50.5 us, 4.0 TB/s (issue slots 0.62, 16 warps).  What did not help: two pieces a lane, which spares the exchange
 // but doubles the registers (92 us, 68 us); rings in shared memory filled by bulk copies (81 us, 72 us) or, backward, by
 // asynchronous copies (56 us); instructions on pairs of binary32 values.
 
