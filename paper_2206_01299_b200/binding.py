@@ -261,7 +261,7 @@ def aq_import_sample(h, sample_id, m_host, seen):
 # call takes a few microseconds on the GPU, so these wrappers do as little as they can: a tensor's element type, place and
 # layout are checked (an int address is taken as it is), sizes and alignments by the library.
 
-_stage_types = {}        # handle: element type of its operands
+_stage_types = {}        # handle: element type of its operands; none for one that was not made here, whose operands' types go unchecked
 _i32 = _f32 = None       # torch.int32, torch.float32 once there is a handle
 
 
@@ -269,7 +269,7 @@ def _row(x, t):
     """Address of a CUDA tensor of type t whose rows (last dimension) are contiguous, of an int address, or None."""
     if x is None or type(x) is int:
         return x
-    if x.dtype is t and x.is_cuda and (x.is_contiguous() or x.stride(-1) == 1 or x.shape[-1] == 1):
+    if (x.dtype is t or t is None) and x.is_cuda and (x.is_contiguous() or x.stride(-1) == 1 or x.shape[-1] == 1):
         return x.data_ptr()
     _unfit(x, t, "contiguous rows")
 
@@ -278,7 +278,7 @@ def _whole(x, t):
     """Address of a contiguous CUDA tensor of type t, an int address, or None."""
     if x is None or type(x) is int:
         return x
-    if x.dtype is t and x.is_cuda and x.is_contiguous():
+    if (x.dtype is t or t is None) and x.is_cuda and x.is_contiguous():
         return x.data_ptr()
     _unfit(x, t, "contiguous elements")
 

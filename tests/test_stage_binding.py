@@ -91,3 +91,12 @@ def test_a_handle_starts_with_fp16_and_forgets_its_type(stage):
     aq.aq_gated_ffn(again, *arguments(CALLS["aq_gated_ffn"], torch.float16))
     with pytest.raises(AssertionError):
         aq.aq_gated_ffn(again, *arguments(CALLS["aq_gated_ffn"], torch.bfloat16))
+
+
+def test_a_handle_made_past_the_wrappers_takes_any_type_but_no_cpu_tensor(stage):
+    _, recorder = stage
+    good = arguments(CALLS["aq_gated_ffn"], torch.bfloat16)
+    aq.aq_gated_ffn(77, *good)
+    assert recorder.calls[-1] == "aq_gated_ffn"
+    with pytest.raises(AssertionError):
+        aq.aq_gated_ffn(77, torch.zeros((8, 8), dtype=torch.bfloat16), *good[1:])
