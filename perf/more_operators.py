@@ -12,10 +12,9 @@ true); `exact` gives the same outputs in binary64 from the definitions.
 
 The moments in 8 bits: m in e4m3, v in e5m2, each block of 256 elements of a tensor with a power of two as its scale,
 the smallest that keeps the block's largest magnitude in range.  v moves by a thousandth of its value per step, far
-less than half a step of any 8-bit format, so roundings are dithered: element i of a tensor at step t goes up where
-its place between two neighbours and a 16-bit threshold add up to one or more.  Thresholds are the two halves of
-i * WEYL_PLACE + t * WEYL_STEP mod 2^32: over the steps they visit every part of the interval equally often.  A v
-that is not zero does not become zero.
+less than half a step of any 8-bit format, so roundings are random, by 16-bit numbers that element i of a tensor has at
+step t: the value goes up where its place between two neighbours and the number add up to one or more.  The numbers are
+the halves of a hash of i and t (`_random`).  A v that is not zero does not become zero.
 """
 import math
 
@@ -27,8 +26,7 @@ T = {"fp16": torch.float16, "bf16": torch.bfloat16, "fp32": torch.float32}
 SIZE = {"fp16": 2, "bf16": 2, "fp32": 4}
 EPS_NORM, EPS_ADAM, BETA1, BETA2 = 1e-5, 1e-8, 0.9, 0.999
 BLOCK = 256
-# upper half: the fractions of the square root of 3 and of the golden ratio, for v; lower half: of the square roots of 5 and 2, for m
-WEYL_PLACE, WEYL_STEP = 0xBB673C6F, 0x9E376A09
+ROOT3, GOLDEN = 0xBB67AE85, 0x9E3779B9      # the fractions of the square root of 3 and of the golden ratio, times 2^32
 
 
 # ---- cases ------------------------------------------------------------------------------------------------
@@ -247,9 +245,15 @@ def _plain_clip(s):
     return _outputs(s, "norm", "factor", "step")
 
 
-def _thresholds(n, step):
-    """16-bit thresholds of m and v."""
-    u = (torch.arange(n, device="cuda") * WEYL_PLACE + step * WEYL_STEP) & 0xFFFFFFFF
+def _random(n, step):
+    """16-bit numbers for m and v; all arithmetic mod 2^32."""
+    k = (step * GOLDEN) & 0xFFFFFFFF
+    k = ((k ^ (k >> 16)) * ROOT3) & 0xFFFFFFFF
+    k = ((k ^ (k >> 15)) * GOLDEN) & 0xFFFFFFFF
+    k = k ^ (k >> 16)
+    u = ((torch.arange(n, device="cuda") + k) * ROOT3) & 0xFFFFFFFF
+    u = ((u ^ (u >> 15)) * GOLDEN) & 0xFFFFFFFF
+    u = u ^ (u >> 16)
     return (u & 0xFFFF).int(), (u >> 16).int()
 
 
@@ -258,7 +262,7 @@ def _blocks(x):
     return torch.nn.functional.pad(x, (0, -x.numel() % BLOCK)).view(-1, BLOCK)
 
 
-def _encode(x, thresholds, mantissa, bias, top):
+def _encode(x, random, mantissa, bias, top):
     """(codes, scales) of x >= 0 in the format with so many mantissa bits; `top`: its largest exponent."""
     drop = 23 - mantissa
     # 1.75 * 2^top is the largest value of either format: 1.75 and less of an octave stay in it
@@ -266,13 +270,13 @@ def _encode(x, thresholds, mantissa, bias, top):
     k = (((largest + (1 << 21) - 1) >> 23) - 127 - top).clamp(min=-126)
     # scaled so that the format's exponents are binary32's smallest, its subnormal numbers among them
     y = (_blocks(x) * ((127 - k) << 23).view(torch.float32)[:, None]).flatten()[:x.numel()] * 2.0 ** (bias - 127)
-    return (y.view(torch.int32) + (thresholds << (drop - 16))) >> drop, ((127 + k) << 23).view(torch.float32)
+    return (y.view(torch.int32) + (random << (drop - 16))) >> drop, ((127 + k) << 23).view(torch.float32)
 
 
 def _store(s, place, m, v, step):
     """A tensor's moments into the case's buffers."""
     at, n, block, blocks, _ = place
-    um, uv = _thresholds(n, step)
+    um, uv = _random(n, step)
     code, s["m_scale"][block:block + blocks] = _encode(m.abs(), um, 3, 7, 8)
     code = code | ((m.view(torch.int32) >> 31) & 0x80)
     s["m"][at:at + n].view(torch.uint8).copy_(code)
@@ -410,7 +414,7 @@ def work(case):
 
 # ---- the definitions in 64 bits ---------------------------------------------------------------------------
 
-def _round(x, thresholds, mantissa, lowest, top):
+def _round(x, random, mantissa, lowest, top):
     """Values of x >= 0 in blocks' scaled 8-bit format, and the scales: magnitudes and steps by exponents, no bit patterns."""
     rows = _blocks(x)
     largest = rows.amax(1)
@@ -419,7 +423,7 @@ def _round(x, thresholds, mantissa, lowest, top):
     scale = torch.pow(2.0, k.double())
     z = rows / scale[:, None]
     step = torch.pow(2.0, (torch.frexp(z)[1] - 1).clamp(min=lowest).double() - mantissa)
-    up = _blocks(thresholds).double() / 65536
+    up = _blocks(random).double() / 65536
     z = (torch.floor(z / step + up) * step).clamp(max=1.75 * 2.0 ** top)
     return z.flatten()[:x.numel()], scale
 
@@ -441,7 +445,7 @@ def _exact_adamw_tensor(s, place, out):
     if c["bits"] == 32:
         out["m"][here], out["v"][here] = m, v
         return
-    um, uv = _thresholds(n, s["step"])
+    um, uv = _random(n, s["step"])
     z, out["m_scale"][block:block + blocks] = _round(m.abs(), um, 3, -6, 8)
     out["m"][here] = torch.where(m < 0, -z, z)
     z, out["v_scale"][block:block + blocks] = _round(v, uv, 2, -14, 15)
