@@ -379,7 +379,8 @@ int aq_import_sample(aq_handle* h, int64_t sample_id, const void* m_host, uint8_
  * A stage decodes an activation, runs its layers, and encodes the result; on the way back it quantizes
  * the gradient of the activation.  Three operators of those layers, each with its gradient, that a stage
  * of a language model needs next to the codec: the norm and rotation of query and key heads, the gated
- * feed-forward product, and the last stage's loss.
+ * feed-forward product, and the last stage's loss.  Further below: the layer norm of the residual stream with its
+ * gradient, and what ends a macro-batch, the norm of all gradients and the optimizer's step.
  *
  * They run on a stage handle, which holds an element type, a stream, a status word and workspaces, and
  * no model state.  Rules as for the codec's handles: calls enqueue on the handle's stream and return;
@@ -396,8 +397,8 @@ aq_stage* aq_stage_create(void);
 /* Waits for the handle's stream, frees everything the handle owns (graphs that captured its calls must not run afterwards).
  * NULL is allowed. */
 void aq_stage_destroy(aq_stage* st);
-/* AQ_DTYPE (AQ_FP16, the default, AQ_BF16 or AQ_FP32; AQ_FP32 serves the token log probabilities only, the
- * other calls answer AQ_EUNSUPPORTED) or AQ_STREAM. */
+/* AQ_DTYPE (AQ_FP16, the default, AQ_BF16 or AQ_FP32; AQ_FP32 does not serve aq_gated_ffn,
+ * aq_qk_norm_rope and their gradients, which answer AQ_EUNSUPPORTED) or AQ_STREAM. */
 int aq_stage_configure(aq_stage* st, int key, int64_t value);
 /* Synchronises the stream, returns the sticky AQ_ST_* bits in *bits_host (host) and clears them. */
 int aq_stage_status(aq_stage* st, uint32_t* bits_host);
@@ -500,6 +501,84 @@ int aq_qk_norm_rope_grad(aq_stage* st, const aq_qk_shape* shape, int64_t rows, c
                          const void* dk_out, int64_t dk_out_stride, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                          const void* wq, const void* wk, const float* cos_sin, const int32_t* positions,
                          void* dq, int64_t dq_stride, void* dk, int64_t dk_stride, float* dwq, float* dwk);
+
+/*
+ * Layer norm of every row, with the residual's addition in the same pass:
+ *   s = x + residual,  mean = mean(s),  rstd = 1 / sqrt(mean((s - mean)^2) + eps),  y = (s - mean) * rstd * w + b
+ * x, residual T[rows][ldx, ldr], first `hidden` of a row (in; residual may be null: s = x); w, b T[hidden] or null for ones and
+ * zeros; sum T[rows][lds] (out; may be null, and has to be without a residual); y T[rows][ldy] (out); mean, rstd float[rows] (out;
+ * may be null): what aq_layer_norm_grad needs, with s.  s is rounded to T, as it is stored, before the norm.  y may be x
+ * or residual, and sum may be the other of the two or residual, where their row strides are equal.  hidden in 1..2^20, rows >= 0, element
+ * alignment; rows of whole 16-byte pieces on 16-byte boundaries are the fast ones.  A row with a NaN or an infinity has NaN in mean, rstd and y or
+ * parts of them, and touches no other row; with eps 0 so has a row of equal values.
+ */
+int aq_layer_norm(aq_stage* st, const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* w, const void* b, float eps,
+                  int64_t rows, int hidden, void* sum, int64_t lds, void* y, int64_t ldy, float* mean, float* rstd);
+
+/*
+ * Its gradient.  With n = (s - mean) * rstd and g = dy * w:
+ *   dx = rstd * (g - mean(g) - n * mean(g * n)) + dsum,  dw = sum over rows of dy * n,  db = sum over rows of dy
+ * dy T[rows][lddy] (in); dsum T[rows][ldds] (in; may be null): the gradient that reaches s past the norm, along the residual
+ * stream; s (the stored sum, or x without a residual), mean, rstd as aq_layer_norm left them.  dx T[rows][lddx] (out; may be null) is
+ * the gradient of x and of residual alike; it may be dy, dsum or s, where the row strides are equal.  dw, db float[hidden] (out; each may be null).
+ * Sums of dw and db are kept in the handle's workspace, which grows as aq_gated_ffn_grad says.
+ */
+int aq_layer_norm_grad(aq_stage* st, const void* dy, int64_t lddy, const void* dsum, int64_t ldds, const void* s, int64_t lds, const void* w,
+                       const float* mean, const float* rstd, int64_t rows, int hidden, void* dx, int64_t lddx, float* dw, float* db);
+
+/*
+ * One tensor of aq_adamw or aq_grad_norm (which reads grad, numel and grad_dtype only).  The array is host memory and is
+ * read before the call returns; its addresses are device addresses.  Tensors are contiguous, may be empty, and may not overlap (a tensor
+ * that two layers share is listed once).  Element alignment; 16-byte alignment of all addresses (8-byte of 8-bit moments) is faster.
+ */
+typedef struct {
+  void* param;            /* T[numel] (in/out; with a master: out) */
+  float* master;          /* [numel] binary32 copy that the step works on (in/out), or null; null with AQ_FP32 */
+  const void* grad;       /* [numel] */
+  void *m, *v;            /* [numel] moments (in/out): float, or e4m3 codes of m and e5m2 codes of v; zeros before the first step */
+  float *m_scale, *v_scale; /* float[ceil(numel / 256)] (in/out) with 8-bit moments: what a block's codes are multiplied by */
+  int64_t numel;
+  float weight_decay;     /* >= 0 */
+  int32_t grad_dtype;     /* the handle's element type, or AQ_FP32 */
+} aq_adam_tensor;
+
+/*
+ * The 2-norm of all tensors' gradients together, and the factor that unscales and clips them, without a read on the host:
+ *   norm = inv_scale * sqrt(sum g^2),  factor = inv_scale * min(1, max_norm / (norm + 1e-6))
+ * inv_scale: 1 / the scale of the loss; max_norm 0 or infinity: no clipping.  norm, factor float[1], step int64[1] (out, device; each may
+ * be null).  A norm that is not finite (an infinity or NaN in a gradient, or one whose square exceeds binary32, above 1.8e19) makes factor NaN, with which
+ * aq_adamw leaves everything as it is; otherwise *step, the number of the optimizer's step, is advanced by one.  Squares
+ * below 1e-45 count as nothing.  n >= 0; more than 400 tensors take a launch for every 400.
+ */
+int aq_grad_norm(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, double inv_scale, double max_norm, float* norm, float* factor, int64_t* step);
+
+/* Settings of aq_adamw. */
+typedef struct {
+  double lr, beta1, beta2;   /* betas in [0, 1) */
+  double eps;                /* 1e-30..1e30 */
+  int64_t step;              /* 1 for the first step */
+  int32_t state_bits;        /* 32 or 8 */
+} aq_adamw_config;
+
+/*
+ * One AdamW step over all tensors:
+ *   g = factor * grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p - lr weight_decay p - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
+ * p is the master where there is one, and param its value rounded to T; otherwise param.  factor float[1], d_lr float[1],
+ * d_step int64[1] (in, device; each may be null): the gradients' factor (1 without), and the learning rate and step in the settings'
+ * place, which a captured graph reads anew at every replay (a step below 1 counts as 1).  A factor that is not finite leaves every
+ * tensor as it is.
+ * Moments in 8 bits: a block of 256 elements has a power of two as its scale, the smallest that keeps its largest magnitude in
+ * the format's range (e4m3 up to 448, e5m2 up to 57344).  p goes by the new m and v as they are before they are stored.  Stored, a value becomes one of its two
+ * neighbours in the format, the upper with the probability of its place between them: when that place, in 65536ths, and a random
+ * number reach 65536.  The numbers of element i of its tensor are the lower (m) and upper (v) 16 bits of u, in arithmetic mod 2^32 with
+ * A = 0xBB67AE85 and B = 0x9E3779B9:  k = step * B;  k = (k ^ k >> 16) * A;  k = (k ^ k >> 15) * B;  k = k ^ k >> 16;
+ * u = (i + k) * A;  u = (u ^ u >> 15) * B;  u = u ^ u >> 16.  A v above zero does not become zero.  m and v are computed with a rounding of
+ * every product and sum, so that the codes are reproducible elsewhere.  A gradient that is not finite, where no factor holds the step
+ * back, makes its element NaN, and with 8-bit moments its whole block from the next step on.
+ */
+int aq_adamw(aq_stage* st, const aq_adamw_config* config, const aq_adam_tensor* tensors, int64_t n, const float* factor, const float* d_lr,
+             const int64_t* d_step);
 
 #ifdef __cplusplus
 }

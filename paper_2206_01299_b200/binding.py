@@ -29,7 +29,19 @@ class QkShape(C.Structure):
                 ("interleaved", C.c_int32), ("eps", C.c_float), ("n_positions", C.c_int64)]
 
 
-_P, _I, _L, _F = C.c_void_p, C.c_int, C.c_int64, C.c_float
+class AdamTensor(C.Structure):
+    """aq_adam_tensor: one tensor of aq_adamw or aq_grad_norm; aq_adam_table makes an array of them."""
+    _fields_ = [("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("numel", C.c_int64), ("weight_decay", C.c_float), ("grad_dtype", C.c_int32)]
+
+
+class AdamwConfig(C.Structure):
+    """aq_adamw_config: the settings of aq_adamw."""
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64),
+                ("state_bits", C.c_int32)]
+
+
+_P, _I, _L, _F, _D = C.c_void_p, C.c_int, C.c_int64, C.c_float, C.c_double
 
 # name -> (restype, argtypes); the load test checks these against the header
 SIGNATURES = {
@@ -74,6 +86,10 @@ SIGNATURES = {
     "aq_gated_ffn_grad": (_I, [_P, _P, _L, _P, _L, _P, _P, _L, _P, _P, _L, _L, _I, _I, _I, _P, _L, _P, _P, _L]),
     "aq_qk_norm_rope": (_I, [_P, _P, _L, _P, _L, _P, _L, _P, _P, _P, _P, _P, _L, _P, _L]),
     "aq_qk_norm_rope_grad": (_I, [_P, _P, _L, _P, _L, _P, _L, _P, _L, _P, _L, _P, _P, _P, _P, _P, _L, _P, _L, _P, _P]),
+    "aq_layer_norm": (_I, [_P, _P, _L, _P, _L, _P, _P, _F, _L, _I, _P, _L, _P, _L, _P, _P]),
+    "aq_layer_norm_grad": (_I, [_P, _P, _L, _P, _L, _P, _L, _P, _P, _P, _L, _I, _P, _L, _P, _P]),
+    "aq_grad_norm": (_I, [_P, _P, _L, _D, _D, _P, _P, _P]),
+    "aq_adamw": (_I, [_P, _P, _P, _L, _P, _P, _P]),
 }
 
 _lib = None
@@ -262,7 +278,7 @@ def aq_import_sample(h, sample_id, m_host, seen):
 # layout are checked (an int address is taken as it is), sizes and alignments by the library.
 
 _stage_types = {}        # handle: element type of its operands; none for one that was not made here, whose operands' types go unchecked
-_i32 = _f32 = None       # torch.int32, torch.float32 once there is a handle
+_i32 = _f32 = _i64 = None  # torch.int32, torch.float32, torch.int64 once there is a handle
 
 
 def _row(x, t):
@@ -288,12 +304,12 @@ def _unfit(x, t, layout):
 
 
 def _stage_type(st, value):
-    global _i32, _f32
+    global _i32, _f32, _i64
     try:
         import torch
     except ImportError:  # then every operand is an address
         return
-    _i32, _f32 = torch.int32, torch.float32
+    _i32, _f32, _i64 = torch.int32, torch.float32, torch.int64
     _stage_types[st] = {AQ_FP16: torch.float16, AQ_BF16: torch.bfloat16, AQ_FP32: torch.float32}[value]
 
 
@@ -381,4 +397,73 @@ def aq_qk_norm_rope_grad(st, shape, rows, dq_out, dq_out_stride, dk_out, dk_out_
                                               _row(q, t), q_stride, _row(k, t), k_stride, _whole(wq, t), _whole(wk, t),
                                               _whole(cos_sin, _f32), _whole(positions, _i32), _row(dq, t), dq_stride, _row(dk, t),
                                               dk_stride, _whole(dwq, _f32), _whole(dwk, _f32))
+    return rc and _stage_error(st, rc)
+
+
+def aq_layer_norm(st, x, ldx, residual, ldr, w, b, eps, rows, hidden, sum, lds, y, ldy, mean, rstd):
+    t = _stage_types.get(st)
+    rc = (_lib or lib()).aq_layer_norm(st, _row(x, t), ldx, _row(residual, t), ldr, _whole(w, t), _whole(b, t), eps, rows, hidden,
+                                       _row(sum, t), lds, _row(y, t), ldy, _whole(mean, _f32), _whole(rstd, _f32))
+    return rc and _stage_error(st, rc)
+
+
+def aq_layer_norm_grad(st, dy, lddy, dsum, ldds, s, lds, w, mean, rstd, rows, hidden, dx, lddx, dw, db):
+    t = _stage_types.get(st)
+    rc = (_lib or lib()).aq_layer_norm_grad(st, _row(dy, t), lddy, _row(dsum, t), ldds, _row(s, t), lds, _whole(w, t), _whole(mean, _f32),
+                                            _whole(rstd, _f32), rows, hidden, _row(dx, t), lddx, _whole(dw, _f32), _whole(db, _f32))
+    return rc and _stage_error(st, rc)
+
+
+def aq_adam_table(st, grads, params=None, masters=None, m=None, v=None, m_scale=None, v_scale=None, weight_decay=0.0):
+    """Array of AdamTensor for aq_adamw, or for aq_grad_norm where nothing but the gradients is given.
+
+    Every argument is a list with one contiguous CUDA tensor (or None, for a tensor without that part) for each of the
+    tensors; weight_decay is a number for all of them or a list.  Moments in 8 bits are torch.float8_e4m3fn (m) and torch.float8_e5m2 (v) or
+    their bytes as torch.uint8, with m_scale and v_scale.  The array holds addresses: it can be kept for as long as the
+    tensors keep their places, and does not keep them alive.  Lay it out anew where gradients are allocated in every step.
+    """
+    import torch
+    t, n = _stage_types.get(st), len(grads)
+    narrow = m_scale is not None
+    kinds = {"m": (torch.float8_e4m3fn, torch.uint8) if narrow else (torch.float32,), "v": (torch.float8_e5m2, torch.uint8) if narrow else (torch.float32,),
+             "param": (t,), "grad": (t, torch.float32), "master": (torch.float32,), "m_scale": (torch.float32,), "v_scale": (torch.float32,)}
+    codes = {torch.float16: AQ_FP16, torch.bfloat16: AQ_BF16, torch.float32: AQ_FP32}
+    columns = {"grad": grads, "param": params, "master": masters, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale}
+    decay = [weight_decay] * n if isinstance(weight_decay, (int, float)) else weight_decay
+    assert len(decay) == n and all(c is None or len(c) == n for c in columns.values()), "lists of different lengths"
+    table = (AdamTensor * n)()
+    written = []
+    for i, row in enumerate(table):
+        row.numel, row.weight_decay, row.grad_dtype = grads[i].numel(), decay[i], codes[grads[i].dtype]
+        for name, column in columns.items():
+            x = None if column is None else column[i]
+            if x is None:
+                continue
+            assert t is None or x.dtype in kinds[name], f"{name} of tensor {i} is {x.dtype}"
+            size = -(-row.numel // 256) if name.endswith("scale") else row.numel
+            assert x.numel() == size, f"{name} of tensor {i} has {x.numel()} elements, not {size}"
+            setattr(row, name, _whole(x, x.dtype))
+            if name != "grad" and size:
+                written.append((x.data_ptr(), x.data_ptr() + x.numel() * x.element_size()))
+    written.sort()
+    assert all(a[1] <= b[0] for a, b in zip(written, written[1:])), "two tensors overlap: one that layers share is listed once"
+    return table
+
+
+def _table(tensors, n):
+    """An array of at least n AdamTensor, or an int address."""
+    if type(tensors) is not int and tensors is not None:
+        assert n <= len(tensors) and tensors._type_ is AdamTensor, "needs an array of AdamTensor with n of them"
+    return tensors
+
+
+def aq_grad_norm(st, tensors, n, inv_scale, max_norm, norm, factor, step):
+    """tensors: an array of AdamTensor, or its address."""
+    rc = (_lib or lib()).aq_grad_norm(st, _table(tensors, n), n, inv_scale, max_norm, _whole(norm, _f32), _whole(factor, _f32), _whole(step, _i64))
+    return rc and _stage_error(st, rc)
+
+
+def aq_adamw(st, config, tensors, n, factor, d_lr, d_step):
+    """config: an AdamwConfig; tensors: an array of AdamTensor, or its address."""
+    rc = (_lib or lib()).aq_adamw(st, C.addressof(config), _table(tensors, n), n, _whole(factor, _f32), _whole(d_lr, _f32), _whole(d_step, _i64))
     return rc and _stage_error(st, rc)

@@ -6,7 +6,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 CODEC_SOURCES = [os.path.join(CSRC, f) for f in ("aq_api.cu", "aq_kernels.cu", "aq_lowbit.cu", "aq_anygroup.cu", "aq_noalloc.cu")]
-STAGE_SOURCES = [os.path.join(CSRC, f) for f in ("aq_stage_api.cu", "aq_logprob.cu", "aq_qknorm.cu", "aq_ffn.cu")]
+STAGE_SOURCES = [os.path.join(CSRC, f) for f in ("aq_stage_api.cu", "aq_logprob.cu", "aq_qknorm.cu", "aq_ffn.cu",
+                                                       "aq_layernorm.cu", "aq_adamw.cu")]
 SOURCES = CODEC_SOURCES + STAGE_SOURCES
 HEADERS = [os.path.join(CSRC, "aq_internal.h"), os.path.join(CSRC, "aq_device.cuh"), os.path.join(CSRC, "aq_stage.h"), os.path.join(CSRC, "aq_stage_device.cuh"),
            os.path.join(os.path.dirname(HERE), "include", "aq_b200.h")]

@@ -1,5 +1,5 @@
 // Launch-layer interface between the stage handle's C ABI (aq_stage_api.cu) and its kernels
-// (aq_logprob.cu, aq_qknorm.cu, aq_ffn.cu).
+// (aq_logprob.cu, aq_qknorm.cu, aq_ffn.cu, aq_layernorm.cu, aq_adamw.cu).
 #pragma once
 
 #include <cuda_runtime.h>
@@ -81,6 +81,69 @@ struct FfnGradArgs {
   int sms, pairs;
 };
 
+struct LayerNormArgs {
+  const void* x; long long ldx;
+  const void* residual; long long ldr;    // may be null
+  const void *w, *b;                      // may be null
+  float eps;
+  long long rows; int hidden;
+  void* sum; long long lds;               // may be null
+  void* y; long long ldy;
+  float *mean, *rstd;                     // may be null
+  bool whole;                             // rows are whole 16-byte pieces, all on 16-byte boundaries
+  int sms;
+};
+
+struct LayerNormGradArgs {
+  const void* dy; long long lddy;
+  const void* dsum; long long ldds;       // may be null
+  const void* s; long long lds;
+  const void* w;                          // may be null
+  const float *mean, *rstd;
+  long long rows; int hidden;
+  void* dx; long long lddx;               // may be null
+  float *dw, *db;                         // may be null
+  float* partials;                        // workspace, layer_norm_grad_parts(a) x [2][hidden]: sums of dw, db
+  bool whole;
+  int sms;
+};
+
+// One tensor of a step, as the kernels read it.
+struct AdamPart {
+  void* param;
+  float* master;                          // may be null
+  const void* grad;
+  void *m, *v;
+  float *m_scale, *v_scale;               // 8-bit moments only
+  long long numel;
+  float decay;
+  uint32_t flags;                         // kPartWide, kPartGradF32
+};
+constexpr uint32_t kPartWide = 1;         // everything on a 16-byte boundary, 8-bit moments on an 8-byte one
+constexpr uint32_t kPartGradF32 = 2;      // the gradient is binary32 beside 16-bit parameters
+constexpr int kAdamTable = 400;           // tensors of a launch: 72 bytes each and 8 of a running count, of 32764 bytes of arguments
+constexpr int kAdamChunk = 2048;          // elements of a tensor that a CTA takes at a time: a block of 256 to a warp
+
+struct AdamScalars {
+  float beta1, rest1, beta2, rest2;       // rest: 1 - beta
+  float eps, lr, c1, c2;                  // c: 1 - beta^step
+  double beta1_exact, beta2_exact;
+  uint32_t step;                          // mod 2^32
+  const float* factor;                    // may be null
+  const float* d_lr;                      // may be null
+  const int64_t* d_step;                  // may be null
+};
+
+struct NormScalars {
+  double* partials;                       // a CTA's sum each, kNormCtas; behind them the sum of the launches before
+  uint32_t* ticket;                       // CTAs that have written theirs; 0 between calls
+  bool first, last;                       // of the launches of a call
+  double inv_scale, max_norm;             // max_norm: infinite for none
+  float *norm, *factor;                   // may be null
+  int64_t* step;                          // may be null
+};
+constexpr int kNormCtas = 2048;
+
 cudaError_t launch_logprob(int dtype, const LogprobArgs& a, cudaStream_t s);
 cudaError_t launch_logprob_grad(int dtype, const LogprobGradArgs& a, cudaStream_t s);
 cudaError_t launch_qk(int dtype, const QkArgs& a, cudaStream_t s);
@@ -90,5 +153,12 @@ cudaError_t ffn_resident_pairs(int* pairs);       // of the current device
 long long ffn_grad_partial_bytes(const FfnGradArgs& a);
 cudaError_t launch_ffn(int dtype, const FfnArgs& a, cudaStream_t s);
 cudaError_t launch_ffn_grad(int dtype, const FfnGradArgs& a, cudaStream_t s);
+cudaError_t launch_layer_norm(int dtype, const LayerNormArgs& a, cudaStream_t s);
+// sums of dw and db that a call keeps in `partials`; goes by the sizes, `whole`, sms and the type
+long long layer_norm_grad_parts(int dtype, const LayerNormGradArgs& a);
+cudaError_t launch_layer_norm_grad(int dtype, const LayerNormGradArgs& a, cudaStream_t s);
+// `parts`: 0..kAdamTable tensors, none of them empty; they travel in the launch's arguments
+cudaError_t launch_adamw(int dtype, int state_bits, const AdamPart* parts, int n, const AdamScalars& a, int sms, cudaStream_t s);
+cudaError_t launch_grad_norm(int dtype, const AdamPart* parts, int n, const NormScalars& a, int sms, cudaStream_t s);
 
 }  // namespace aq

@@ -20,8 +20,8 @@ struct aq_stage {
   cudaStream_t stream = nullptr;
   uint32_t* status = nullptr;
   uint32_t *ticket = nullptr, *next = nullptr;   // in the status word's allocation
-  float* partials = nullptr;              // aq_qk_norm_rope_grad
-  void* work = nullptr;                   // aq_gated_ffn_grad
+  float* partials = nullptr;              // aq_qk_norm_rope_grad, aq_grad_norm
+  void* work = nullptr;                   // aq_gated_ffn_grad, aq_layer_norm_grad
   size_t work_bytes = 0;
   bool work_captured = false;             // a stream capture has taken its address
   KeptBlock* kept = nullptr;              // freed with the handle
@@ -142,6 +142,66 @@ aq::QkArgs qk_args(aq_stage* st, const aq_qk_shape* sh, int64_t rows, const void
   a.wq = wq; a.wk = wk; a.cos_sin = cos_sin; a.positions = positions;
   a.partials = st->partials; a.ticket = st->ticket; a.status = st->status; a.sms = st->sms;
   return a;
+}
+
+unsigned size_of(int dtype) { return dtype == AQ_FP32 ? 4 : 2; }
+
+// A T[..][hidden] operand of the layer norm: element alignment and any stride do; `whole` stays true for 16-byte pieces.
+int check_norm_rows(aq_stage* st, const char* who, const char* name, const void* p, int64_t ld, int64_t hidden, bool* whole) {
+  const unsigned size = size_of(st->dtype);
+  if (!p || misaligned(p, size)) return fail(st, AQ_EINVAL, "%s: %s is null or misaligned", who, name);
+  if (ld < hidden || ld > (1ll << 38)) return fail(st, AQ_EINVAL, "%s: the row stride of %s must be at least %lld", who, name, (long long)hidden);
+  if (misaligned(p, 16) || ld % (16 / size)) *whole = false;
+  return AQ_OK;
+}
+
+int check_norm(aq_stage* st, const char* who, int64_t rows, int hidden, const void* w, const void* b, bool* whole) {
+  if (rows < 0 || rows > 0x7fffffffll) return fail(st, AQ_EINVAL, "%s: rows must be in 0..2^31-1", who);
+  if (hidden < 1 || hidden > (1 << 20)) return fail(st, AQ_EINVAL, "%s: hidden must be in 1..2^20 (got %d)", who, hidden);
+  const unsigned size = size_of(st->dtype);
+  if (misaligned(w, size) || misaligned(b, size)) return fail(st, AQ_EINVAL, "%s: w or b is misaligned", who);
+  *whole = hidden % (16 / size) == 0 && !misaligned(w, 16) && !misaligned(b, 16);
+  return AQ_OK;
+}
+
+// Two operands in one place have to have the same rows.
+int check_in_place(aq_stage* st, const char* who, const void* out, int64_t ld_out, const void* in, int64_t ld_in) {
+  if (out && out == in && ld_out != ld_in) return fail(st, AQ_EINVAL, "%s: in place, the row strides must be equal", who);
+  return AQ_OK;
+}
+
+int check_adam_tensor(aq_stage* st, const char* who, int64_t i, const aq_adam_tensor& t) {
+  if (t.numel < 0 || t.numel > (1ll << 40)) return fail(st, AQ_EINVAL, "%s: tensor %lld: numel must be in 0..2^40", who, (long long)i);
+  if (t.grad_dtype != st->dtype && t.grad_dtype != AQ_FP32) return fail(st, AQ_EINVAL, "%s: tensor %lld: grad_dtype must be the handle's element type or AQ_FP32", who, (long long)i);
+  if (t.numel && (!t.grad || misaligned(t.grad, size_of(t.grad_dtype)))) return fail(st, AQ_EINVAL, "%s: tensor %lld: grad is null or misaligned", who, (long long)i);
+  return AQ_OK;
+}
+
+int check_adam_state(aq_stage* st, const char* who, int64_t i, const aq_adam_tensor& t, int bits) {
+  if (!(t.weight_decay >= 0.0f) || !std::isfinite(t.weight_decay)) return fail(st, AQ_EINVAL, "%s: tensor %lld: weight_decay must be finite and not negative", who, (long long)i);
+  if (!t.numel) return AQ_OK;
+  if (!t.param || misaligned(t.param, size_of(st->dtype))) return fail(st, AQ_EINVAL, "%s: tensor %lld: param is null or misaligned", who, (long long)i);
+  if (t.master && st->dtype == AQ_FP32) return fail(st, AQ_EINVAL, "%s: tensor %lld: binary32 parameters have no master copy", who, (long long)i);
+  if (misaligned(t.master, 4)) return fail(st, AQ_EINVAL, "%s: tensor %lld: master is misaligned", who, (long long)i);
+  if (!t.m || !t.v || (bits == 32 && (misaligned(t.m, 4) || misaligned(t.v, 4)))) return fail(st, AQ_EINVAL, "%s: tensor %lld: m or v is null or misaligned", who, (long long)i);
+  if (bits == 8 && (!t.m_scale || !t.v_scale || misaligned(t.m_scale, 4) || misaligned(t.v_scale, 4)))
+    return fail(st, AQ_EINVAL, "%s: tensor %lld: m_scale or v_scale is null or misaligned", who, (long long)i);
+  return AQ_OK;
+}
+
+// Tensors [*i, ...) that are not empty, at most kAdamTable of them; bits 0: gradients only.
+int gather_parts(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, int bits, int64_t* i, aq::AdamPart* parts) {
+  int have = 0;
+  for (; *i < n && have < aq::kAdamTable; ++*i) {
+    const aq_adam_tensor& t = tensors[*i];
+    if (!t.numel) continue;
+    bool wide = !misaligned(t.grad, 16);
+    if (bits) wide = wide && !misaligned(t.param, 16) && !misaligned(t.master, 16) && !misaligned(t.m, bits == 8 ? 8 : 16) && !misaligned(t.v, bits == 8 ? 8 : 16);
+    const bool f32 = t.grad_dtype == AQ_FP32 && st->dtype != AQ_FP32;
+    parts[have++] = aq::AdamPart{t.param, t.master, t.grad, t.m, t.v, t.m_scale, t.v_scale, (long long)t.numel, t.weight_decay,
+                                 (wide ? aq::kPartWide : 0u) | (f32 ? aq::kPartGradF32 : 0u)};
+  }
+  return have;
 }
 
 #define AQ_TRY(expr) do { const int rc_ = (expr); if (rc_ != AQ_OK) return rc_; } while (0)
@@ -374,6 +434,117 @@ int aq_qk_norm_rope_grad(aq_stage* st, const aq_qk_shape* shape, int64_t rows, c
   a.q_out = dq; a.q_out_stride = dq_stride; a.k_out = dk; a.k_out_stride = dk_stride;
   a.dwq = dwq; a.dwk = dwk;
   return launched(st, aq::launch_qk_grad(st->dtype, a, st->stream), who);
+}
+
+int aq_layer_norm(aq_stage* st, const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* w, const void* b, float eps,
+                  int64_t rows, int hidden, void* sum, int64_t lds, void* y, int64_t ldy, float* mean, float* rstd) {
+  if (!st) return AQ_EINVAL;
+  const char* who = "aq_layer_norm";
+  bool whole;
+  AQ_TRY(check_norm(st, who, rows, hidden, w, b, &whole));
+  if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(st, AQ_EINVAL, "%s: eps must be finite and not negative", who);
+  if (misaligned(mean, 4) || misaligned(rstd, 4)) return fail(st, AQ_EINVAL, "%s: mean or rstd is misaligned", who);
+  if (sum && !residual) return fail(st, AQ_EINVAL, "%s: sum without residual", who);
+  if (rows == 0) return AQ_OK;
+  AQ_TRY(check_norm_rows(st, who, "x", x, ldx, hidden, &whole));
+  AQ_TRY(check_norm_rows(st, who, "y", y, ldy, hidden, &whole));
+  if (residual) AQ_TRY(check_norm_rows(st, who, "residual", residual, ldr, hidden, &whole));
+  if (sum) AQ_TRY(check_norm_rows(st, who, "sum", sum, lds, hidden, &whole));
+  if (sum && sum == y) return fail(st, AQ_EINVAL, "%s: sum and y are two outputs", who);
+  AQ_TRY(check_in_place(st, who, y, ldy, x, ldx));
+  AQ_TRY(check_in_place(st, who, y, ldy, residual, ldr));
+  AQ_TRY(check_in_place(st, who, sum, lds, x, ldx));
+  AQ_TRY(check_in_place(st, who, sum, lds, residual, ldr));
+  DeviceGuard guard(st->device);
+  const aq::LayerNormArgs a{x, ldx, residual, ldr, w, b, eps, rows, hidden, sum, lds, y, ldy, mean, rstd, whole, st->sms};
+  return launched(st, aq::launch_layer_norm(st->dtype, a, st->stream), who);
+}
+
+int aq_layer_norm_grad(aq_stage* st, const void* dy, int64_t lddy, const void* dsum, int64_t ldds, const void* s, int64_t lds, const void* w,
+                       const float* mean, const float* rstd, int64_t rows, int hidden, void* dx, int64_t lddx, float* dw, float* db) {
+  if (!st) return AQ_EINVAL;
+  const char* who = "aq_layer_norm_grad";
+  bool whole;
+  AQ_TRY(check_norm(st, who, rows, hidden, w, nullptr, &whole));
+  if (misaligned(dw, 4) || misaligned(db, 4)) return fail(st, AQ_EINVAL, "%s: dw or db is misaligned", who);
+  DeviceGuard guard(st->device);
+  if (rows == 0) {                                           // no token: the weights' gradients are sums of nothing
+    for (float* p : {dw, db}) {
+      if (!p) continue;
+      const cudaError_t e = cudaMemsetAsync(p, 0, sizeof(float) * (size_t)hidden, st->stream);
+      if (e != cudaSuccess) return cuda_fail(st, e, who);
+    }
+    return AQ_OK;
+  }
+  AQ_TRY(check_norm_rows(st, who, "dy", dy, lddy, hidden, &whole));
+  AQ_TRY(check_norm_rows(st, who, "s", s, lds, hidden, &whole));
+  if (dsum) AQ_TRY(check_norm_rows(st, who, "dsum", dsum, ldds, hidden, &whole));
+  if (dx) AQ_TRY(check_norm_rows(st, who, "dx", dx, lddx, hidden, &whole));
+  AQ_TRY(check_in_place(st, who, dx, lddx, dy, lddy));
+  AQ_TRY(check_in_place(st, who, dx, lddx, dsum, ldds));
+  AQ_TRY(check_in_place(st, who, dx, lddx, s, lds));
+  if (!mean || !rstd || misaligned(mean, 4) || misaligned(rstd, 4)) return fail(st, AQ_EINVAL, "%s: mean or rstd is null or misaligned", who);
+  if (!dx && !dw && !db) return AQ_OK;
+  aq::LayerNormGradArgs a{dy, lddy, dsum, ldds, s, lds, w, mean, rstd, rows, hidden, dx, lddx, dw, db, nullptr, whole, st->sms};
+  if (dw || db) AQ_TRY(ensure_work(st, (size_t)aq::layer_norm_grad_parts(st->dtype, a) * 2 * (size_t)hidden * sizeof(float)));
+  a.partials = static_cast<float*>(st->work);
+  return launched(st, aq::launch_layer_norm_grad(st->dtype, a, st->stream), who);
+}
+
+int aq_grad_norm(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, double inv_scale, double max_norm, float* norm, float* factor, int64_t* step) {
+  if (!st) return AQ_EINVAL;
+  const char* who = "aq_grad_norm";
+  if (n < 0 || (n && !tensors)) return fail(st, AQ_EINVAL, "%s: tensors is null, or n is negative", who);
+  if (!(inv_scale > 0.0) || !std::isfinite(inv_scale)) return fail(st, AQ_EINVAL, "%s: inv_scale must be positive and finite", who);
+  if (!(max_norm >= 0.0)) return fail(st, AQ_EINVAL, "%s: max_norm must not be negative or NaN", who);
+  if (misaligned(norm, 4) || misaligned(factor, 4) || misaligned(step, 8)) return fail(st, AQ_EINVAL, "%s: misaligned pointer", who);
+  for (int64_t i = 0; i < n; ++i) AQ_TRY(check_adam_tensor(st, who, i, tensors[i]));
+  DeviceGuard guard(st->device);
+  aq::NormScalars a{reinterpret_cast<double*>(st->partials), st->ticket, true, false, inv_scale, max_norm > 0.0 ? max_norm : INFINITY, norm, factor, step};
+  aq::AdamPart parts[aq::kAdamTable];
+  for (int64_t i = 0; !a.last; a.first = false) {
+    const int have = gather_parts(st, tensors, n, 0, &i, parts);
+    a.last = i >= n;
+    AQ_TRY(launched(st, aq::launch_grad_norm(st->dtype, parts, have, a, st->sms, st->stream), who));
+  }
+  return AQ_OK;
+}
+
+int aq_adamw(aq_stage* st, const aq_adamw_config* config, const aq_adam_tensor* tensors, int64_t n, const float* factor, const float* d_lr,
+             const int64_t* d_step) {
+  if (!st) return AQ_EINVAL;
+  const char* who = "aq_adamw";
+  if (!config) return fail(st, AQ_EINVAL, "%s: null config", who);
+  if (n < 0 || (n && !tensors)) return fail(st, AQ_EINVAL, "%s: tensors is null, or n is negative", who);
+  if (config->state_bits != 32 && config->state_bits != 8) return fail(st, AQ_EINVAL, "%s: state_bits must be 32 or 8 (got %d)", who, config->state_bits);
+  if (!(config->beta1 >= 0.0 && config->beta1 < 1.0 && config->beta2 >= 0.0 && config->beta2 < 1.0)) return fail(st, AQ_EINVAL, "%s: beta1 and beta2 must be in [0, 1)", who);
+  if (!(config->eps >= 1e-30) || !(config->eps < 1e30)) return fail(st, AQ_EINVAL, "%s: eps must be in 1e-30..1e30", who);
+  if (!d_lr && !std::isfinite((float)config->lr)) return fail(st, AQ_EINVAL, "%s: lr must be finite", who);
+  if (!d_step && config->step < 1) return fail(st, AQ_EINVAL, "%s: step counts from 1", who);
+  if (misaligned(factor, 4) || misaligned(d_lr, 4) || misaligned(d_step, 8)) return fail(st, AQ_EINVAL, "%s: misaligned pointer", who);
+  for (int64_t i = 0; i < n; ++i) {
+    AQ_TRY(check_adam_tensor(st, who, i, tensors[i]));
+    AQ_TRY(check_adam_state(st, who, i, tensors[i], config->state_bits));
+  }
+  DeviceGuard guard(st->device);
+  aq::AdamScalars a{};
+  a.beta1 = (float)config->beta1; a.rest1 = (float)(1.0 - config->beta1);
+  a.beta2 = (float)config->beta2; a.rest2 = (float)(1.0 - config->beta2);
+  a.beta1_exact = config->beta1; a.beta2_exact = config->beta2;
+  a.eps = (float)config->eps;
+  a.factor = factor; a.d_lr = d_lr; a.d_step = d_step;
+  if (!d_lr) a.lr = (float)config->lr;
+  if (!d_step) {
+    a.step = (uint32_t)config->step;
+    a.c1 = (float)(1.0 - std::pow(config->beta1, (double)config->step));
+    a.c2 = (float)(1.0 - std::pow(config->beta2, (double)config->step));
+  }
+  aq::AdamPart parts[aq::kAdamTable];
+  for (int64_t i = 0; i < n;) {
+    const int have = gather_parts(st, tensors, n, config->state_bits, &i, parts);
+    AQ_TRY(launched(st, aq::launch_adamw(st->dtype, config->state_bits, parts, have, a, st->sms, st->stream), who));
+  }
+  return AQ_OK;
 }
 
 }  // extern "C"

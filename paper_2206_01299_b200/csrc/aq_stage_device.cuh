@@ -65,10 +65,10 @@ __device__ bool warp_wait(int lane, uint32_t bar, uint32_t parity, uint32_t* sta
 
 // A launch that may be placed while the stream's previous kernel drains (the kernels wait for its results themselves).
 template <typename... Params, typename... Args>
-cudaError_t launch(void (*kernel)(Params...), dim3 ctas, unsigned threads, size_t shared, cudaStream_t s, Args... args) {
+cudaError_t launch(void (*kernel)(Params...), dim3 ctas, dim3 threads, size_t shared, cudaStream_t s, Args... args) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = ctas;
-  cfg.blockDim = dim3(threads);
+  cfg.blockDim = threads;
   cfg.dynamicSmemBytes = shared;
   cfg.stream = s;
   cudaLaunchAttribute attr{};
