@@ -529,7 +529,7 @@ int aq_layer_norm_grad(aq_stage* st, const void* dy, int64_t lddy, const void* d
 /*
  * One tensor of aq_adamw or aq_grad_norm (which reads grad, numel and grad_dtype only).  The array is host memory and is
  * read before the call returns; its addresses are device addresses.  Tensors are contiguous, may be empty, and may not overlap (a tensor
- * that two layers share is listed once).  Element alignment; 16-byte alignment of all addresses (8-byte of 8-bit moments) is faster.
+ * that two layers share is listed once).  Element alignment; addresses that are multiples of eight elements are faster.
  */
 typedef struct {
   void* param;            /* T[numel] (in/out; with a master: out) */
@@ -555,7 +555,7 @@ int aq_grad_norm(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, double 
 /* Settings of aq_adamw. */
 typedef struct {
   double lr, beta1, beta2;   /* betas in [0, 1) */
-  double eps;                /* 1e-30..1e30 */
+  double eps;                /* 1e-12..1e30 */
   int64_t step;              /* 1 for the first step */
   int32_t state_bits;        /* 32 or 8 */
 } aq_adamw_config;

@@ -21,122 +21,143 @@
 #include "aq_stage.h"
 #include "aq_stage_device.cuh"
 
+#include <type_traits>
+
 namespace aq {
 namespace {
 
 constexpr int kAdamThreads = 256, kAdamWarps = kAdamThreads / 32;
-constexpr int kAdamCtas = 4, kNormCtasPerSm = 8;
+constexpr int kAdamCtas = 2, kNormCtasPerSm = 8;    // CTAs on a multiprocessor
 constexpr uint32_t kRoot3 = 0xBB67AE85u, kGolden = 0x9E3779B9u;   // fractions of the square root of 3 and of the golden ratio, times 2^32
 
 template <int N> struct Table {
   AdamPart part[N];
-  long long first[N + 1];                     // chunks of the tensors before this one
+  int first[N + 1];                           // units of the tensors before this one
   int n;
+  uint32_t unit;                              // elements that a warp takes at a time, blocks of 256
 };
 
-// Eight values of a lane.  Wide: neighbours, by 16-byte accesses; otherwise every 32nd element.
-template <typename T> struct Eight {
-  static __device__ void load(const T* p, float* f) {
-    const uint4 v = __ldcs(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { const float2 a = Num<T>::open(w[i]); f[2 * i] = a.x; f[2 * i + 1] = a.y; }
+// ---- eight elements of a lane: neighbours by one access of up to 32 bytes (`wide`), otherwise every 32nd element -------------
+
+template <typename T> struct Eight {            // 16-bit types: two to a word
+  static constexpr int W = 4;
+  static __device__ void load(const T* p, uint32_t* w) {
+    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
   }
-  static __device__ void store(T* p, const float* f) {
-    __stcs(reinterpret_cast<uint4*>(p), make_uint4(Num<T>::close(f[0], f[1]), Num<T>::close(f[2], f[3]), Num<T>::close(f[4], f[5]), Num<T>::close(f[6], f[7])));
+  static __device__ void store(T* p, const uint32_t* w) {
+    asm volatile("st.global.L1::no_allocate.v4.b32 [%4], {%0, %1, %2, %3};" ::"r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "l"(p) : "memory");
   }
-  static __device__ float one(T x) { return (float)x; }
-  static __device__ T back(float x) { return Num<T>::one(x); }
+  static __device__ void load_one(const T* p, int j, uint32_t* w) { w[j / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p) << (16 * (j & 1)); }
+  static __device__ void store_one(T* p, int j, const uint32_t* w) { *reinterpret_cast<uint16_t*>(p) = (uint16_t)(w[j / 2] >> (16 * (j & 1))); }
+  static __device__ float2 open(const uint32_t* w, int i) { return Num<T>::open(w[i]); }
+  static __device__ void close(uint32_t* w, int i, float2 f) { w[i] = Num<T>::close(f.x, f.y); }
 };
 template <> struct Eight<float> {
-  static __device__ void load(const float* p, float* f) {
-    const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  static constexpr int W = 8;
+  static __device__ void load(const float* p, uint32_t* w) {
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
   }
-  static __device__ void store(float* p, const float* f) {
-    __stcs(reinterpret_cast<float4*>(p), make_float4(f[0], f[1], f[2], f[3]));
-    __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(f[4], f[5], f[6], f[7]));
+  static __device__ void store(float* p, const uint32_t* w) {
+    asm volatile("st.global.L1::no_allocate.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                 ::"r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(p) : "memory");
   }
-  static __device__ float one(float x) { return x; }
-  static __device__ float back(float x) { return x; }
+  static __device__ void load_one(const float* p, int j, uint32_t* w) { w[j] = __float_as_uint(*p); }
+  static __device__ void store_one(float* p, int j, const uint32_t* w) { *p = __uint_as_float(w[j]); }
+  static __device__ float2 open(const uint32_t* w, int i) { return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1])); }
+  static __device__ void close(uint32_t* w, int i, float2 f) { w[2 * i] = __float_as_uint(f.x); w[2 * i + 1] = __float_as_uint(f.y); }
+};
+template <> struct Eight<uint8_t> {             // codes: four to a word
+  static constexpr int W = 2;
+  static __device__ void load(const uint8_t* p, uint32_t* w) { asm volatile("ld.global.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p)); }
+  static __device__ void store(uint8_t* p, const uint32_t* w) { asm volatile("st.global.L1::no_allocate.v2.b32 [%2], {%0, %1};" ::"r"(w[0]), "r"(w[1]), "l"(p) : "memory"); }
+  static __device__ void load_one(const uint8_t* p, int j, uint32_t* w) { w[j / 4] |= (uint32_t)*p << (8 * (j & 3)); }
+  static __device__ void store_one(uint8_t* p, int j, const uint32_t* w) { *p = (uint8_t)(w[j / 4] >> (8 * (j & 3))); }
 };
 
-// Which elements of a tensor a lane has: `wide` ones are all there.
+// Which elements of a tensor a lane has.
 struct Lane8 {
-  bool wide;
-  long long at;                               // of the first
-  long long numel;
-  __device__ long long place(int j) const { return wide ? at + j : at + 32 * j; }
-  __device__ bool has(int j) const { return wide || at + 32 * j < numel; }
+  bool wide;                                    // all eight are there
+  uint32_t at, numel;                           // the first one
+  __device__ bool has(int j) const { return at + 32 * j < numel; }
 };
-
-template <typename T> __device__ void take(const Lane8& l, const void* from, float* f) {
+template <typename T> __device__ void take(const Lane8& l, const void* from, uint32_t* w) {
   const T* const p = static_cast<const T*>(from) + l.at;
   if (l.wide) {
-    Eight<T>::load(p, f);
+    Eight<T>::load(p, w);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = l.has(j) ? Eight<T>::one(p[32 * j]) : 0.0f;
+    for (int i = 0; i < Eight<T>::W; ++i) w[i] = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (l.has(j)) Eight<T>::load_one(p + 32 * j, j, w);
   }
 }
-template <typename T> __device__ void put(const Lane8& l, void* to, const float* f) {
+template <typename T> __device__ void put(const Lane8& l, void* to, const uint32_t* w) {
   T* const p = static_cast<T*>(to) + l.at;
   if (l.wide) {
-    Eight<T>::store(p, f);
+    Eight<T>::store(p, w);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (l.has(j)) p[32 * j] = Eight<T>::back(f[j]);
+      if (l.has(j)) Eight<T>::store_one(p + 32 * j, j, w);
   }
 }
-__device__ uint2 take_codes(const Lane8& l, const void* from) {
-  const uint8_t* const p = static_cast<const uint8_t*>(from) + l.at;
-  if (l.wide) return __ldcs(reinterpret_cast<const uint2*>(p));
-  uint32_t c[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) c[j] = l.has(j) ? p[32 * j] : 0;
-  return make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
+
+// ---- copies to shared memory that a warp waits for later ------------------------------------------------------
+
+__device__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+__device__ void copy8(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory"); }
+__device__ void copy4(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory"); }
+__device__ void copy32(uint32_t to, const void* from) { copy16(to, from); copy16(to + 16, static_cast<const char*>(from) + 16); }
+template <typename T> __device__ void copy_eight(uint32_t to, const void* from) { if (sizeof(T) == 4) copy32(to, from); else copy16(to, from); }
+__device__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ void shared8(uint32_t from, uint32_t* w) { asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(from) : "memory"); }
+__device__ void shared16(uint32_t from, uint32_t* w) { asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from) : "memory"); }
+__device__ void shared32(uint32_t from, uint32_t* w) { shared16(from, w); shared16(from + 16, w + 4); }
+template <typename T> __device__ void shared_eight(uint32_t from, uint32_t* w) { if constexpr (sizeof(T) == 4) shared32(from, w); else shared16(from, w); }
+
+// ---- arithmetic on pairs: one instruction for two, each rounded as a single one is ---------------------------------------
+
+__device__ float2 both(float x) { return make_float2(x, x); }
+__device__ float2 mul2(float2 a, float2 b) {
+  float2 c;
+  asm("{.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmul.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;}" : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
 }
-__device__ void put_codes(const Lane8& l, void* to, const uint32_t* c) {
-  uint8_t* const p = static_cast<uint8_t*>(to) + l.at;
-  if (l.wide) {
-    __stcs(reinterpret_cast<uint2*>(p), make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (l.has(j)) p[32 * j] = (uint8_t)c[j];
-  }
+__device__ float2 fma2(float2 a, float2 b, float2 d) {
+  float2 c;
+  asm("{.reg .b64 x, y, z, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 w, {%6, %7};\nfma.rn.f32x2 z, x, y, w;\nmov.b64 {%0, %1}, z;}"
+      : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(d.x), "f"(d.y));
+  return c;
 }
+// a + b, where both may be products that have been rounded: a packed product and sum become one fused operation in the assembler, rounding
+// modes or not, and a factor of one that it does not know keeps them apart
+__device__ float2 sum2(float2 a, float2 b, float one) { return fma2(a, both(one), b); }
+// the largest magnitude; NaN if there is one
+__device__ float largest3(float a, float b, float c) { float d; asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
+__device__ uint32_t largest_of_warp(float x) { return __reduce_max_sync(0xffffffffu, __float_as_uint(x) & 0x7fffffffu); }
+// m / (root + eps); both approximations are within 2^-22, and a root below 1e-19 may come out as zero beside eps
+__device__ float approximate_root(float x) { float y; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ float approximate_inverse(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// ---- moments in 8 bits ---------------------------------------------------------------------------------------
 
 __device__ float2 half_pair(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
-// values of eight codes, before the scale; every one is a binary16 number
-__device__ void open_e4m3(uint2 c, float* f) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint16_t two = (uint16_t)((i < 2 ? c.x : c.y) >> (16 * (i & 1)));
-    uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(two));
-    const float2 a = half_pair(h);
-    f[2 * i] = a.x;
-    f[2 * i + 1] = a.y;
-  }
+// values of codes 2i, 2i + 1 before the scale; every one is a binary16 number
+__device__ float2 open_e4m3(const uint32_t* c, int i) {
+  const uint16_t two = (uint16_t)(c[i / 2] >> (16 * (i & 1)));
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(two));
+  return half_pair(h);
 }
-__device__ void open_e5m2(uint2 c, float* f) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {               // e5m2 is the upper byte of a binary16
-    const uint32_t two = (i < 2 ? c.x : c.y) >> (16 * (i & 1));
-    const float2 a = half_pair((two & 0xffu) << 8 | (two & 0xff00u) << 16);
-    f[2 * i] = a.x;
-    f[2 * i + 1] = a.y;
-  }
-}
+__device__ float2 open_e5m2(const uint32_t* c, int i) { return half_pair(__byte_perm(c[i / 2], 0, i & 1 ? 0x3424 : 0x1404)); }   // the upper byte of a binary16
 
-// A block's scale 2^k from its largest magnitude, given as the bits of the binary32; top: the format's largest exponent.
-// The formats end at 1.75 * 2^top, so a magnitude above 1.75 of its octave counts to the next one.  Infinities and NaN: NaN.
-__device__ int scale_exponent(uint32_t largest, int top) { return max((int)((largest + 0x1fffffu) >> 23) - 127 - top, -126); }
-__device__ float power_of_two(int k) { return __uint_as_float((uint32_t)(127 + k) << 23); }
-
-struct Clock { float step_size, root_c2, lr; uint32_t key; };
+// The exponent of a block's scale, 127 added to it, from the bits of its largest magnitude; top: the format's largest exponent.  The formats
+// end at 1.75 * 2^top, so a magnitude above 1.75 of its octave counts to the next one.  At least 1: a binary32 of full precision.
+__device__ int scale_exponent(uint32_t largest, int top) { return max((int)((largest + 0x1fffffu) >> 23) - top, 1); }
+__device__ float power_of_two(int e) { return __uint_as_float((uint32_t)e << 23); }
 
 // The random bits of an element at a step: for m the lower half, for v the upper.
 __device__ uint32_t step_key(uint32_t step) {
@@ -145,11 +166,55 @@ __device__ uint32_t step_key(uint32_t step) {
   k = (k ^ (k >> 15)) * kGolden;
   return k ^ (k >> 16);
 }
-__device__ uint32_t random_bits(uint32_t place, uint32_t key) {
-  uint32_t u = (place + key) * kRoot3;
-  u = (u ^ (u >> 15)) * kGolden;
+__device__ uint32_t random_bits(uint32_t scrambled) {           // of (element + key) * kRoot3
+  const uint32_t u = (scrambled ^ (scrambled >> 15)) * kGolden;
   return u ^ (u >> 16);
 }
+// Codes of m[8] and v[8].  A moment is scaled so that the format's exponents are binary32's smallest, subnormal numbers among them; the
+// format's last bit is then bit 20 or 21, the random number is added below it, and the bits above are the code.
+__device__ __forceinline__ void store_codes(const float2* m, const float2* v, int em, int ev, uint32_t place, uint32_t stride, uint32_t key, uint32_t* cm, uint32_t* cv) {
+  float2 ym[4], yv[4];
+  const float im = power_of_two(254 - em), iv = power_of_two(254 - ev);
+  if (em <= 127 + 29 && ev <= 127 + 37) {                       // times 2^-120 and 2^-112 they still are binary32 numbers
+    const float2 jm = both(im * 0x1p-120f), jv = both(iv * 0x1p-112f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { ym[i] = mul2(m[i], jm); yv[i] = mul2(v[i], jv); }
+  } else {                                                      // moments of 1e11 and more
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      ym[i] = mul2(mul2(m[i], both(im)), both(0x1p-120f));
+      yv[i] = mul2(mul2(v[i], both(iv)), both(0x1p-112f));
+    }
+  }
+  uint32_t tm[8], tv[8], least = 0xffffffffu;
+  const uint32_t scrambled = (place + key) * kRoot3;
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    const uint32_t u = random_bits(scrambled + (uint32_t)j * (stride * kRoot3)), w = random_bits(scrambled + (uint32_t)(j + 1) * (stride * kRoot3));
+    tm[j] = __float_as_uint(ym[j / 2].x) + (u & 0xffffu) * 16;  // the sign stays in bit 31
+    tm[j + 1] = __float_as_uint(ym[j / 2].y) + (w & 0xffffu) * 16;
+    tv[j] = __float_as_uint(yv[j / 2].x) + (u >> 16) * 32;
+    tv[j + 1] = __float_as_uint(yv[j / 2].y) + (w >> 16) * 32;
+    least = __vimin3_u32(least, tv[j], tv[j + 1]);
+  }
+  if (least < 1u << 21) {                                       // a v above zero does not become zero
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if ((j & 1 ? v[j / 2].y : v[j / 2].x) > 0.0f) tv[j] = max(tv[j], 1u << 21);
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t* const t = tm + 4 * i;                       // upper halves of two: sign, four zeros, seven bits of the code, four below
+    const uint32_t a = __byte_perm(t[0], t[1], 0x7632), b = __byte_perm(t[2], t[3], 0x7632);
+    cm[i] = __byte_perm((a >> 4 & 0x7f7f7f7fu) | (a >> 8 & 0x80808080u), (b >> 4 & 0x7f7f7f7fu) | (b >> 8 & 0x80808080u), 0x6420);
+    const uint32_t* const s = tv + 4 * i;                       // three zeros, eight bits, five below
+    cv[i] = __byte_perm(__byte_perm(s[0], s[1], 0x7632) >> 5, __byte_perm(s[2], s[3], 0x7632) >> 5, 0x6420);
+  }
+}
+
+// ---- the step ------------------------------------------------------------------------------------------------
+
+struct Clock { float step_size, root_c2, lr; uint32_t key; };
 
 __device__ double power(double base, uint64_t n) {
   double p = 1.0;
@@ -160,106 +225,231 @@ __device__ double power(double base, uint64_t n) {
   return p;
 }
 
-template <typename T, int BITS, int N>
+// What a lane has read of its eight elements.  MIXED: some tensor has a binary32 gradient or a master beside 16-bit parameters.
+template <typename T, int BITS, bool MIXED> struct Read {
+  static constexpr int W = MIXED ? 8 : Eight<T>::W, S = BITS == 32 ? 8 : 2;
+  uint32_t g[W], p[W], m[S], v[S];
+  float sm, sv;
+};
+// ... and what becomes of them
+template <typename T, int BITS> struct Written {
+  uint32_t master[8], p[Eight<T>::W], m[BITS == 32 ? 8 : 2], v[BITS == 32 ? 8 : 2];
+  float sm, sv;
+};
+
+struct Settings { float factor, beta1, rest1, beta2, rest2, one, eps, step_size, root_c2, decay; uint32_t key; };
+
+// Eight elements of a lane, a block's 256 of a warp; place, stride: of the lane's elements in their tensor.
+template <typename T, int BITS, bool MIXED>
+__device__ __forceinline__ void update(const Settings& a, const Read<T, BITS, MIXED>& r, bool grad32, bool master, uint32_t place, uint32_t stride, Written<T, BITS>& o) {
+  float2 m[4], v[4];
+  float largest_m = 0.0f, largest_v = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 g = mul2(MIXED && grad32 ? Eight<float>::open(r.g, i) : Eight<T>::open(r.g, i), both(a.factor));
+    if (BITS == 32) {
+      m[i] = Eight<float>::open(r.m, i);
+      v[i] = Eight<float>::open(r.v, i);
+    } else {
+      m[i] = mul2(open_e4m3(r.m, i), both(r.sm));
+      v[i] = mul2(open_e5m2(r.v, i), both(r.sv));
+    }
+    m[i] = sum2(mul2(m[i], both(a.beta1)), mul2(g, both(a.rest1)), a.one);
+    v[i] = sum2(mul2(v[i], both(a.beta2)), mul2(mul2(g, g), both(a.rest2)), a.one);
+    if (BITS == 8) {
+      largest_m = largest3(largest_m, m[i].x, m[i].y);
+      largest_v = largest3(largest_v, v[i].x, v[i].y);
+    }
+    float2 root = make_float2(approximate_root(v[i].x), approximate_root(v[i].y));
+    root = fma2(root, both(a.root_c2), both(a.eps));
+    const float2 move = mul2(m[i], make_float2(approximate_inverse(root.x), approximate_inverse(root.y)));
+    float2 p = MIXED && master ? Eight<float>::open(r.p, i) : Eight<T>::open(r.p, i);
+    p = fma2(both(-a.step_size), move, fma2(both(-a.decay), p, p));
+    if (MIXED) Eight<float>::close(o.master, i, p);
+    Eight<T>::close(o.p, i, p);
+    if (BITS == 32) {
+      Eight<float>::close(o.m, i, m[i]);
+      Eight<float>::close(o.v, i, v[i]);
+    }
+  }
+  if (BITS == 8) {
+    const uint32_t bits_m = largest_of_warp(largest_m), bits_v = largest_of_warp(largest_v);
+    const int em = scale_exponent(bits_m, 8), ev = scale_exponent(bits_v, 15);
+    store_codes(m, v, em, ev, place, stride, a.key, o.m, o.v);
+    const float nan = __int_as_float(0x7fc00000);               // a block with an infinity or NaN is NaN from here on
+    o.sm = bits_m < 0x7f800000u ? power_of_two(em) : nan;
+    o.sv = bits_v < 0x7f800000u ? power_of_two(ev) : nan;
+  }
+}
+
+// The tensor that has unit c, from t on.
+template <int N> __device__ int tensor_of(const Table<N>& table, int c, int t) {
+  if (c < table.first[t + 1]) return t;
+  for (int hi = table.n; hi - t > 1;) {
+    const int mid = (t + hi) / 2;
+    if (table.first[mid] <= c) t = mid; else hi = mid;
+  }
+  return t;
+}
+
+// A warp's walk over the blocks of its units.
+template <int N> struct Walk {
+  int c, t, step;
+  uint32_t at, left;                          // of the block: its first element in its tensor; blocks of the unit, this one among them
+  __device__ Walk(const Table<N>& table, int first, int step) : c(first), t(0), step(step), at(0), left(0) { find(table); }
+  __device__ bool here(const Table<N>& table) const { return c < table.first[table.n]; }
+  __device__ void find(const Table<N>& table) {
+    if (!here(table)) return;
+    t = tensor_of(table, c, t);
+    at = (uint32_t)(c - table.first[t]) * table.unit;
+    left = min(table.unit, table.part[t].numel - at + 255) / 256;
+  }
+  __device__ void next(const Table<N>& table, uint32_t blocks) {
+    at += 256 * blocks;
+    left -= blocks;
+    if (left) return;
+    c += step;
+    find(table);
+  }
+};
+
+// Shared memory of the 8-bit moments: every warp has two slots for a piece of P blocks each.  A block's gradients, parameters,
+// codes of m and of v; behind the blocks their scales in pairs.
+template <typename T, bool MIXED> struct Ring {
+  static constexpr int kValues = 256 * (MIXED ? 4 : (int)sizeof(T)), P = kValues == 512 ? 4 : 1;
+  static constexpr int kParam = kValues, kM = 2 * kValues, kV = kM + 256, kBlock = kV + 256, kScales = P * kBlock, kSlot = kScales + (P * 8 + 15) / 16 * 16;
+  static constexpr int kBytes = kAdamWarps * 2 * kSlot;
+  static_assert(kSlot % 16 == 0, "copies start on 16-byte boundaries");
+};
+
+template <typename T, int BITS, bool MIXED, int N>
 __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __grid_constant__ Table<N> table, const __grid_constant__ AdamScalars a) {
+  using State = typename std::conditional<BITS == 32, float, uint8_t>::type;
+  using Rg = Ring<T, MIXED>;
+  constexpr uint32_t P = Rg::P;
+  extern __shared__ __align__(16) uint8_t rings[];
   __shared__ Clock shared_clock;
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  uint32_t here = shared_address(rings) + warp * 2 * Rg::kSlot, there = here + Rg::kSlot;
   next_may_launch();
   wait_for_previous();
-  const float factor = a.factor ? __ldg(a.factor) : 1.0f;
-  if (!(fabsf(factor) < __int_as_float(0x7f800000))) return;   // a step that is to be left out
+  Settings set{a.factor ? __ldg(a.factor) : 1.0f, a.beta1, a.rest1, a.beta2, a.rest2, a.one, a.eps, 0, 0, 0, 0};
+  if (!(fabsf(set.factor) < __int_as_float(0x7f800000))) return;   // a step that is to be left out
+
+  // of a piece's blocks those that are whole and of aligned tensors
+  auto wide_blocks = [&](const Walk<N>& k) {
+    const AdamPart& part = table.part[k.t];
+    return part.flags & kPartWide ? min(min(k.left, P), (part.numel - k.at) / 256) : 0u;
+  };
+  auto ask = [&](const Walk<N>& k, uint32_t to) {
+    const AdamPart& part = table.part[k.t];
+    const uint32_t blocks = wide_blocks(k), e = k.at + lane * 8;
+    const bool grad32 = MIXED && (part.flags & kPartGradF32), master = MIXED && part.master;
+    const char* const g = static_cast<const char*>(part.grad) + (size_t)e * (grad32 ? 4 : sizeof(T));
+    const char* const p = master ? reinterpret_cast<const char*>(part.master + e) : reinterpret_cast<const char*>(static_cast<T*>(part.param) + e);
+    const uint8_t *const m = static_cast<uint8_t*>(part.m) + e, *const v = static_cast<uint8_t*>(part.v) + e;
+#pragma unroll
+    for (uint32_t i = 0; i < P; ++i) {
+      if (i >= blocks) break;
+      const uint32_t block = to + i * Rg::kBlock;
+      if (grad32) copy32(block + lane * 32, g + i * 1024); else copy_eight<T>(block + lane * 8 * sizeof(T), g + i * 256 * sizeof(T));
+      if (master) copy32(block + Rg::kParam + lane * 32, p + i * 1024); else copy_eight<T>(block + Rg::kParam + lane * 8 * sizeof(T), p + i * 256 * sizeof(T));
+      copy8(block + Rg::kM + lane * 8, m + i * 256);
+      copy8(block + Rg::kV + lane * 8, v + i * 256);
+    }
+    if ((lane & 15) < blocks) copy4(to + Rg::kScales + (lane & 15) * 8 + (lane >> 4) * 4, (lane & 16 ? part.v_scale : part.m_scale) + k.at / 256 + (lane & 15));
+  };
+  Walk<N> k(table, blockIdx.x * kAdamWarps + warp, gridDim.x * kAdamWarps), ahead = k;
+  if (BITS == 8) {
+    if (ahead.here(table)) {
+      ask(ahead, here);
+      ahead.next(table, min(ahead.left, P));
+    }
+    copies_end();
+  }
+
   if (threadIdx.x == 0) {
     const float lr = a.d_lr ? __ldg(a.d_lr) : a.lr;
     float c1 = a.c1, c2 = a.c2;
     uint32_t step = a.step;
     if (a.d_step) {
-      const int64_t t = max(__ldg(reinterpret_cast<const long long*>(a.d_step)), 1ll);
-      step = (uint32_t)t;
-      c1 = (float)(1.0 - power(a.beta1_exact, (uint64_t)t));
-      c2 = (float)(1.0 - power(a.beta2_exact, (uint64_t)t));
+      const int64_t n = max(__ldg(reinterpret_cast<const long long*>(a.d_step)), 1ll);
+      step = (uint32_t)n;
+      c1 = (float)(1.0 - power(a.beta1_exact, (uint64_t)n));
+      c2 = (float)(1.0 - power(a.beta2_exact, (uint64_t)n));
     }
     shared_clock = Clock{lr / c1, sqrtf(1.0f / c2), lr, step_key(step)};
   }
   __syncthreads();
-  const Clock clock = shared_clock;
+  set.step_size = shared_clock.step_size;
+  set.root_c2 = shared_clock.root_c2;
+  set.key = shared_clock.key;
+  const float lr = shared_clock.lr;
 
-  const long long chunks = table.first[table.n];
-  long long c = chunks * blockIdx.x / gridDim.x;
-  const long long end = chunks * (blockIdx.x + 1) / gridDim.x;
-  int t = 0;
-  for (int hi = table.n; hi - t > 1;) {       // the tensor that has chunk c
-    const int mid = (t + hi) / 2;
-    if (table.first[mid] <= c) t = mid; else hi = mid;
-  }
-  for (; c < end; ++c) {
-    while (table.first[t + 1] <= c) ++t;
-    const AdamPart& part = table.part[t];
-    const long long base = (c - table.first[t]) * kAdamChunk + warp * 256;
-    if (base >= part.numel) continue;
-    Lane8 l;
-    l.numel = part.numel;
-    l.wide = (part.flags & kPartWide) && base + 256 <= part.numel;
-    l.at = base + (l.wide ? lane * 8 : lane);
-    float g[8], p[8], m[8], v[8];
-    uint2 cm, cv;
-    float sm = 0.0f, sv = 0.0f;
-    const long long block = base / 256;
-    if (part.flags & kPartGradF32) take<float>(l, part.grad, g); else take<T>(l, part.grad, g);
-    if (part.master) take<float>(l, part.master, p); else take<T>(l, part.param, p);
-    if (BITS == 32) {
-      take<float>(l, part.m, m);
-      take<float>(l, part.v, v);
-    } else {
-      cm = take_codes(l, part.m);
-      cv = take_codes(l, part.v);
-      sm = part.m_scale[block];
-      sv = part.v_scale[block];
-      open_e4m3(cm, m);
-      open_e5m2(cv, v);
+  float unit_sm = 0.0f, unit_sv = 0.0f;                         // lane i: scales of the unit's block i
+  int in_unit = 0;
+#pragma unroll 1
+  while (k.here(table)) {
+    const AdamPart& part = table.part[k.t];
+    const bool grad32 = MIXED && (part.flags & kPartGradF32), master = MIXED && part.master;
+    const uint32_t blocks = min(k.left, P), wide = wide_blocks(k);
+    set.decay = lr * part.decay;
+    if (BITS == 8) {                                            // the next piece goes where the whole warp has read the last one
+      copies_wait<0>();
+      __syncwarp();
+      if (ahead.here(table)) {
+        ask(ahead, there);
+        ahead.next(table, min(ahead.left, P));
+      }
+      copies_end();
     }
-    uint32_t largest_m = 0, largest_v = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (BITS == 8) { m[j] = __fmul_rn(m[j], sm); v[j] = __fmul_rn(v[j], sv); }
-      const float gj = __fmul_rn(g[j], factor);
-      m[j] = __fadd_rn(__fmul_rn(m[j], a.beta1), __fmul_rn(gj, a.rest1));
-      v[j] = __fadd_rn(__fmul_rn(v[j], a.beta2), __fmul_rn(__fmul_rn(gj, gj), a.rest2));
+#pragma unroll 1
+    for (uint32_t i = 0; i < blocks; ++i) {
+      const uint32_t at = k.at + i * 256;
+      const Lane8 l{i < wide, at + (i < wide ? lane * 8 : lane), part.numel};
+      Read<T, BITS, MIXED> r;
+      if (BITS == 8 && i < wide) {
+        const uint32_t block = here + i * Rg::kBlock;
+        if (grad32) shared32(block + lane * 32, r.g); else shared_eight<T>(block + lane * 8 * sizeof(T), r.g);
+        if (master) shared32(block + Rg::kParam + lane * 32, r.p); else shared_eight<T>(block + Rg::kParam + lane * 8 * sizeof(T), r.p);
+        shared8(block + Rg::kM + lane * 8, r.m);
+        shared8(block + Rg::kV + lane * 8, r.v);
+        uint32_t scales[2];
+        shared8(here + Rg::kScales + i * 8, scales);
+        r.sm = __uint_as_float(scales[0]);
+        r.sv = __uint_as_float(scales[1]);
+      } else {
+        if (grad32) take<float>(l, part.grad, r.g); else take<T>(l, part.grad, r.g);
+        if (master) take<float>(l, part.master, r.p); else take<T>(l, part.param, r.p);
+        take<State>(l, part.m, r.m);
+        take<State>(l, part.v, r.v);
+        if (BITS == 8) { r.sm = part.m_scale[at / 256]; r.sv = part.v_scale[at / 256]; }
+      }
+      Written<T, BITS> o;
+      update<T, BITS, MIXED>(set, r, grad32, master, part.place + l.at, l.wide ? 1 : 32, o);
+      if (master) put<float>(l, part.master, o.master);
+      put<T>(l, part.param, o.p);
+      put<State>(l, part.m, o.m);
+      put<State>(l, part.v, o.v);
       if (BITS == 8) {
-        largest_m = max(largest_m, __float_as_uint(m[j]) & 0x7fffffffu);
-        largest_v = max(largest_v, __float_as_uint(v[j]) & 0x7fffffffu);
-      }
-      float root;
-      asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v[j]));
-      const float update = __fdividef(m[j], fmaf(root, clock.root_c2, a.eps));
-      p[j] -= fmaf(clock.step_size, update, clock.lr * part.decay * p[j]);
-    }
-    if (part.master) put<float>(l, part.master, p);
-    put<T>(l, part.param, p);
-    if (BITS == 32) {
-      put<float>(l, part.m, m);
-      put<float>(l, part.v, v);
-    } else {
-      largest_m = __reduce_max_sync(0xffffffffu, largest_m);
-      largest_v = __reduce_max_sync(0xffffffffu, largest_v);
-      const int km = scale_exponent(largest_m, 8), kv = scale_exponent(largest_v, 15);
-      const float im = power_of_two(-km), iv = power_of_two(-kv);
-      uint32_t em[8], ev[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t u = random_bits((uint32_t)l.place(j), clock.key);
-        // scaled so that the formats' exponents are binary32's smallest, subnormal numbers among them
-        const float ym = __fmul_rn(__fmul_rn(fabsf(m[j]), im), 0x1p-120f), yv = __fmul_rn(__fmul_rn(v[j], iv), 0x1p-112f);
-        em[j] = min((__float_as_uint(ym) + ((u & 0xffffu) << 4)) >> 20, 0x7eu) | (__float_as_uint(m[j]) >> 24 & 0x80u);
-        ev[j] = max(min((__float_as_uint(yv) + ((u >> 16) << 5)) >> 21, 0x7bu), v[j] > 0.0f ? 1u : 0u);
-      }
-      put_codes(l, part.m, em);
-      put_codes(l, part.v, ev);
-      if (lane == 0) {
-        const float nan = __int_as_float(0x7fc00000);
-        part.m_scale[block] = largest_m < 0x7f800000u ? power_of_two(km) : nan;
-        part.v_scale[block] = largest_v < 0x7f800000u ? power_of_two(kv) : nan;
+        if (lane == in_unit) { unit_sm = o.sm; unit_sv = o.sv; }
+        ++in_unit;
       }
     }
+    if (BITS == 8) {                                            // the scales of a unit leave together: pieces of a sector cost as much as whole ones
+      if (k.left == blocks) {
+        if (lane < in_unit) {
+          const uint32_t block = k.at / 256 + blocks - in_unit + lane;
+          part.m_scale[block] = unit_sm;
+          part.v_scale[block] = unit_sv;
+        }
+        in_unit = 0;
+      }
+      const uint32_t other = here;
+      here = there;
+      there = other;
+    }
+    k.next(table, blocks);
   }
 }
 
@@ -273,29 +463,20 @@ __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(const __grid_co
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   next_may_launch();
   wait_for_previous();
-  const long long chunks = table.first[table.n];
-  long long c = chunks * blockIdx.x / gridDim.x;
-  const long long end = chunks * (blockIdx.x + 1) / gridDim.x;
-  int t = 0;
-  for (int hi = table.n; hi - t > 1;) {
-    const int mid = (t + hi) / 2;
-    if (table.first[mid] <= c) t = mid; else hi = mid;
-  }
   double sum = 0.0;
 #pragma unroll 1
-  for (; c < end; ++c) {
-    while (table.first[t + 1] <= c) ++t;
-    const AdamPart& part = table.part[t];
-    const long long base = (c - table.first[t]) * kAdamChunk + warp * 256;
-    if (base >= part.numel) continue;
-    Lane8 l;
-    l.numel = part.numel;
-    l.wide = (part.flags & kPartWide) && base + 256 <= part.numel;
-    l.at = base + (l.wide ? lane * 8 : lane);
-    float g[8], s = 0.0f;
-    if (part.flags & kPartGradF32) take<float>(l, part.grad, g); else take<T>(l, part.grad, g);
+  for (Walk<N> k(table, blockIdx.x * kAdamWarps + warp, gridDim.x * kAdamWarps); k.here(table); k.next(table, 1)) {
+    const AdamPart& part = table.part[k.t];
+    const bool wide = (part.flags & kPartWide) && k.at + 256 <= part.numel, grad32 = part.flags & kPartGradF32;
+    const Lane8 l{wide, k.at + (wide ? lane * 8 : lane), part.numel};
+    uint32_t w[8];
+    if (grad32) take<float>(l, part.grad, w); else take<T>(l, part.grad, w);
+    float s = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s = fmaf(g[j], g[j], s);
+    for (int i = 0; i < 4; ++i) {
+      const float2 g = grad32 ? Eight<float>::open(w, i) : Eight<T>::open(w, i);
+      s = fmaf(g.x, g.x, fmaf(g.y, g.y, s));
+    }
     sum += (double)s;
   }
   auto join = [&](double x) {                 // the CTA's sum, for thread 0
@@ -334,38 +515,60 @@ __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(const __grid_co
   if (a.step && fine) ++*a.step;
 }
 
-template <int N> void fill(Table<N>& table, const AdamPart* parts, int n) {
-  long long chunks = 0;
+// Units of `unit` elements; how many there are.
+template <int N> int fill(Table<N>& table, const AdamPart* parts, int n, uint32_t unit) {
+  int units = 0;
   for (int i = 0; i < n; ++i) {
     table.part[i] = parts[i];
-    table.first[i] = chunks;
-    chunks += (parts[i].numel + kAdamChunk - 1) / kAdamChunk;
+    table.first[i] = units;
+    units += (int)((parts[i].numel + unit - 1) / unit);
   }
-  for (int i = n; i <= N; ++i) table.first[i] = chunks;
+  for (int i = n; i <= N; ++i) table.first[i] = units;
   table.n = n;
+  table.unit = unit;
+  return units;
 }
 
 template <int N, typename Kernel, typename Scalars>
-cudaError_t start(Kernel kernel, const AdamPart* parts, int n, const Scalars& a, long long ctas, cudaStream_t s) {
+cudaError_t start(Kernel kernel, const AdamPart* parts, int n, const Scalars& a, int ctas, size_t shared, cudaStream_t s) {
   Table<N> table;
-  fill(table, parts, n);
-  const long long chunks = table.first[n];
-  const unsigned grid = (unsigned)(chunks < 1 ? 1 : chunks < ctas ? chunks : ctas);
-  return launch(kernel, dim3(grid), kAdamThreads, 0, s, table, a);
+  // the longest units, up to eight blocks (whose scales fill a sector), with which every warp has eight
+  long long blocks = 0;
+  for (int i = 0; i < n; ++i) blocks += (parts[i].numel + 255) / 256;
+  uint32_t unit = 2048;
+  while (unit > 256 && blocks * 256 < 8ll * unit * ctas * kAdamWarps) unit /= 2;
+  const int units = fill(table, parts, n, unit), want = (units + kAdamWarps - 1) / kAdamWarps;
+  return launch(kernel, dim3((unsigned)(want < 1 ? 1 : want < ctas ? want : ctas)), kAdamThreads, shared, s, table, a);
 }
 
 // Most calls of few tensors are short: a small table spares them 30 KB of arguments.
 constexpr int kSmallTable = 24;
 
+template <typename T, int BITS, bool MIXED, int N> cudaError_t run_table(const AdamPart* parts, int n, const AdamScalars& a, int sms, cudaStream_t s) {
+  constexpr int kBytes = BITS == 8 ? Ring<T, MIXED>::kBytes : 0;
+  const auto kernel = adamw_kernel<T, BITS, MIXED, N>;
+  if (kBytes > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (e != cudaSuccess) return e;
+  }
+  return start<N>(kernel, parts, n, a, kAdamCtas * sms, kBytes, s);
+}
+template <typename T, int BITS, bool MIXED> cudaError_t run_mixed(const AdamPart* parts, int n, const AdamScalars& a, int sms, cudaStream_t s) {
+  if (n <= kSmallTable) return run_table<T, BITS, MIXED, kSmallTable>(parts, n, a, sms, s);
+  return run_table<T, BITS, MIXED, kAdamTable>(parts, n, a, sms, s);
+}
 template <typename T, int BITS> cudaError_t run_adamw(const AdamPart* parts, int n, const AdamScalars& a, int sms, cudaStream_t s) {
-  if (n <= kSmallTable) return start<kSmallTable>(adamw_kernel<T, BITS, kSmallTable>, parts, n, a, (long long)kAdamCtas * sms, s);
-  return start<kAdamTable>(adamw_kernel<T, BITS, kAdamTable>, parts, n, a, (long long)kAdamCtas * sms, s);
+  bool mixed = false;
+  for (int i = 0; i < n; ++i) mixed = mixed || parts[i].master || (parts[i].flags & kPartGradF32);
+  if constexpr (!std::is_same<T, float>::value)
+    if (mixed) return run_mixed<T, BITS, true>(parts, n, a, sms, s);
+  return run_mixed<T, BITS, false>(parts, n, a, sms, s);
 }
 
 template <typename T> cudaError_t run_norm(const AdamPart* parts, int n, const NormScalars& a, int sms, cudaStream_t s) {
-  const long long most = (long long)kNormCtasPerSm * sms < kNormCtas ? (long long)kNormCtasPerSm * sms : kNormCtas;
-  if (n <= kSmallTable) return start<kSmallTable>(grad_norm_kernel<T, kSmallTable>, parts, n, a, most, s);
-  return start<kAdamTable>(grad_norm_kernel<T, kAdamTable>, parts, n, a, most, s);
+  const int most = kNormCtasPerSm * sms < kNormCtas ? kNormCtasPerSm * sms : kNormCtas;
+  if (n <= kSmallTable) return start<kSmallTable>(grad_norm_kernel<T, kSmallTable>, parts, n, a, most, 0, s);
+  return start<kAdamTable>(grad_norm_kernel<T, kAdamTable>, parts, n, a, most, 0, s);
 }
 
 }  // namespace

@@ -108,24 +108,25 @@ struct LayerNormGradArgs {
   int sms;
 };
 
-// One tensor of a step, as the kernels read it.
+// A tensor of a step, or a part of a long one, as the kernels read it.
 struct AdamPart {
   void* param;
   float* master;                          // may be null
   const void* grad;
   void *m, *v;
   float *m_scale, *v_scale;               // 8-bit moments only
-  long long numel;
+  uint32_t numel;                         // at most kPartMost: longer tensors come in several
+  uint32_t place;                         // index of its first element in its tensor, mod 2^32
   float decay;
   uint32_t flags;                         // kPartWide, kPartGradF32
 };
-constexpr uint32_t kPartWide = 1;         // everything on a 16-byte boundary, 8-bit moments on an 8-byte one
+constexpr uint32_t kPartMost = 1u << 30;
+constexpr uint32_t kPartWide = 1;         // every address is a multiple of eight elements
 constexpr uint32_t kPartGradF32 = 2;      // the gradient is binary32 beside 16-bit parameters
 constexpr int kAdamTable = 400;           // tensors of a launch: 72 bytes each and 8 of a running count, of 32764 bytes of arguments
-constexpr int kAdamChunk = 2048;          // elements of a tensor that a CTA takes at a time: a block of 256 to a warp
 
 struct AdamScalars {
-  float beta1, rest1, beta2, rest2;       // rest: 1 - beta
+  float beta1, rest1, beta2, rest2, one;  // rest: 1 - beta; one: 1
   float eps, lr, c1, c2;                  // c: 1 - beta^step
   double beta1_exact, beta2_exact;
   uint32_t step;                          // mod 2^32

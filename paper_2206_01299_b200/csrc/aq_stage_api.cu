@@ -189,17 +189,35 @@ int check_adam_state(aq_stage* st, const char* who, int64_t i, const aq_adam_ten
   return AQ_OK;
 }
 
-// Tensors [*i, ...) that are not empty, at most kAdamTable of them; bits 0: gradients only.
-int gather_parts(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, int bits, int64_t* i, aq::AdamPart* parts) {
+// The next tensors that are not empty, from element *from of tensor *i on, in parts of at most kPartMost elements, at most kAdamTable of
+// them; bits 0: gradients only.
+int gather_parts(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, int bits, int64_t* i, int64_t* from, aq::AdamPart* parts) {
   int have = 0;
-  for (; *i < n && have < aq::kAdamTable; ++*i) {
+  for (; *i < n; ++*i, *from = 0) {
     const aq_adam_tensor& t = tensors[*i];
-    if (!t.numel) continue;
-    bool wide = !misaligned(t.grad, 16);
-    if (bits) wide = wide && !misaligned(t.param, 16) && !misaligned(t.master, 16) && !misaligned(t.m, bits == 8 ? 8 : 16) && !misaligned(t.v, bits == 8 ? 8 : 16);
+    const int size = (int)size_of(st->dtype), grad_size = (int)size_of(t.grad_dtype), state_size = bits == 8 ? 1 : 4;
+    bool wide = !misaligned(t.grad, 8 * grad_size);
+    if (bits) wide = wide && !misaligned(t.param, 8 * size) && !misaligned(t.master, 32) && !misaligned(t.m, 8 * state_size) && !misaligned(t.v, 8 * state_size);
     const bool f32 = t.grad_dtype == AQ_FP32 && st->dtype != AQ_FP32;
-    parts[have++] = aq::AdamPart{t.param, t.master, t.grad, t.m, t.v, t.m_scale, t.v_scale, (long long)t.numel, t.weight_decay,
-                                 (wide ? aq::kPartWide : 0u) | (f32 ? aq::kPartGradF32 : 0u)};
+    for (; *from < t.numel; *from += aq::kPartMost) {
+      if (have == aq::kAdamTable) return have;
+      const int64_t e = *from, left = t.numel - e;
+      auto at = [e](const void* p, int bytes) { return p ? const_cast<char*>(static_cast<const char*>(p)) + e * bytes : nullptr; };
+      aq::AdamPart& p = parts[have++];
+      p = aq::AdamPart{};
+      p.grad = at(t.grad, grad_size);
+      if (bits) {
+        p.param = at(t.param, size);
+        p.master = t.master ? t.master + e : nullptr;
+        p.m = at(t.m, state_size);
+        p.v = at(t.v, state_size);
+        if (bits == 8) { p.m_scale = t.m_scale + e / 256; p.v_scale = t.v_scale + e / 256; }
+        p.decay = t.weight_decay;
+      }
+      p.numel = (uint32_t)(left < aq::kPartMost ? left : aq::kPartMost);
+      p.place = (uint32_t)e;
+      p.flags = (wide ? aq::kPartWide : 0u) | (f32 ? aq::kPartGradF32 : 0u);
+    }
   }
   return have;
 }
@@ -502,8 +520,8 @@ int aq_grad_norm(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, double 
   DeviceGuard guard(st->device);
   aq::NormScalars a{reinterpret_cast<double*>(st->partials), st->ticket, true, false, inv_scale, max_norm > 0.0 ? max_norm : INFINITY, norm, factor, step};
   aq::AdamPart parts[aq::kAdamTable];
-  for (int64_t i = 0; !a.last; a.first = false) {
-    const int have = gather_parts(st, tensors, n, 0, &i, parts);
+  for (int64_t i = 0, from = 0; !a.last; a.first = false) {
+    const int have = gather_parts(st, tensors, n, 0, &i, &from, parts);
     a.last = i >= n;
     AQ_TRY(launched(st, aq::launch_grad_norm(st->dtype, parts, have, a, st->sms, st->stream), who));
   }
@@ -518,7 +536,7 @@ int aq_adamw(aq_stage* st, const aq_adamw_config* config, const aq_adam_tensor* 
   if (n < 0 || (n && !tensors)) return fail(st, AQ_EINVAL, "%s: tensors is null, or n is negative", who);
   if (config->state_bits != 32 && config->state_bits != 8) return fail(st, AQ_EINVAL, "%s: state_bits must be 32 or 8 (got %d)", who, config->state_bits);
   if (!(config->beta1 >= 0.0 && config->beta1 < 1.0 && config->beta2 >= 0.0 && config->beta2 < 1.0)) return fail(st, AQ_EINVAL, "%s: beta1 and beta2 must be in [0, 1)", who);
-  if (!(config->eps >= 1e-30) || !(config->eps < 1e30)) return fail(st, AQ_EINVAL, "%s: eps must be in 1e-30..1e30", who);
+  if (!(config->eps >= 1e-12) || !(config->eps < 1e30)) return fail(st, AQ_EINVAL, "%s: eps must be in 1e-12..1e30", who);
   if (!d_lr && !std::isfinite((float)config->lr)) return fail(st, AQ_EINVAL, "%s: lr must be finite", who);
   if (!d_step && config->step < 1) return fail(st, AQ_EINVAL, "%s: step counts from 1", who);
   if (misaligned(factor, 4) || misaligned(d_lr, 4) || misaligned(d_step, 8)) return fail(st, AQ_EINVAL, "%s: misaligned pointer", who);
@@ -530,6 +548,7 @@ int aq_adamw(aq_stage* st, const aq_adamw_config* config, const aq_adam_tensor* 
   aq::AdamScalars a{};
   a.beta1 = (float)config->beta1; a.rest1 = (float)(1.0 - config->beta1);
   a.beta2 = (float)config->beta2; a.rest2 = (float)(1.0 - config->beta2);
+  a.one = 1.0f;
   a.beta1_exact = config->beta1; a.beta2_exact = config->beta2;
   a.eps = (float)config->eps;
   a.factor = factor; a.d_lr = d_lr; a.d_step = d_step;
@@ -540,8 +559,8 @@ int aq_adamw(aq_stage* st, const aq_adamw_config* config, const aq_adam_tensor* 
     a.c2 = (float)(1.0 - std::pow(config->beta2, (double)config->step));
   }
   aq::AdamPart parts[aq::kAdamTable];
-  for (int64_t i = 0; i < n;) {
-    const int have = gather_parts(st, tensors, n, config->state_bits, &i, parts);
+  for (int64_t i = 0, from = 0; i < n;) {
+    const int have = gather_parts(st, tensors, n, config->state_bits, &i, &from, parts);
     AQ_TRY(launched(st, aq::launch_adamw(st->dtype, config->state_bits, parts, have, a, st->sms, st->stream), who));
   }
   return AQ_OK;
