@@ -37,7 +37,7 @@ template <int N> struct Table {
   uint32_t unit;                              // elements that a warp takes at a time, blocks of 256
 };
 
-// ---- eight elements of a lane: neighbours by one access of up to 32 bytes (`wide`), otherwise every 32nd element -------------
+// ---- eight elements of a lane: neighbours by one access of up to 32 bytes, or every 32nd element one by one ---------------
 
 template <typename T> struct Eight {            // 16-bit types: two to a word
   static constexpr int W = 4;
@@ -75,33 +75,24 @@ template <> struct Eight<uint8_t> {             // codes: four to a word
   static __device__ void store_one(uint8_t* p, int j, const uint32_t* w) { *p = (uint8_t)(w[j / 4] >> (8 * (j & 3))); }
 };
 
-// Which elements of a tensor a lane has.
+// Every 32nd element of a tensor: those that a lane has.
 struct Lane8 {
-  bool wide;                                    // all eight are there
   uint32_t at, numel;                           // the first one
   __device__ bool has(int j) const { return at + 32 * j < numel; }
 };
 template <typename T> __device__ void take(const Lane8& l, const void* from, uint32_t* w) {
   const T* const p = static_cast<const T*>(from) + l.at;
-  if (l.wide) {
-    Eight<T>::load(p, w);
-  } else {
 #pragma unroll
-    for (int i = 0; i < Eight<T>::W; ++i) w[i] = 0;
+  for (int i = 0; i < Eight<T>::W; ++i) w[i] = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (l.has(j)) Eight<T>::load_one(p + 32 * j, j, w);
-  }
+  for (int j = 0; j < 8; ++j)
+    if (l.has(j)) Eight<T>::load_one(p + 32 * j, j, w);
 }
 template <typename T> __device__ void put(const Lane8& l, void* to, const uint32_t* w) {
   T* const p = static_cast<T*>(to) + l.at;
-  if (l.wide) {
-    Eight<T>::store(p, w);
-  } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (l.has(j)) Eight<T>::store_one(p + 32 * j, j, w);
-  }
+  for (int j = 0; j < 8; ++j)
+    if (l.has(j)) Eight<T>::store_one(p + 32 * j, j, w);
 }
 
 // ---- copies to shared memory that a warp waits for later ------------------------------------------------------
@@ -172,7 +163,8 @@ __device__ uint32_t random_bits(uint32_t scrambled) {           // of (element +
 }
 // Codes of m[8] and v[8].  A moment is scaled so that the format's exponents are binary32's smallest, subnormal numbers among them; the
 // format's last bit is then bit 20 or 21, the random number is added below it, and the bits above are the code.
-__device__ __forceinline__ void store_codes(const float2* m, const float2* v, int em, int ev, uint32_t place, uint32_t stride, uint32_t key, uint32_t* cm, uint32_t* cv) {
+template <int STRIDE>
+__device__ __forceinline__ void store_codes(const float2* m, const float2* v, int em, int ev, uint32_t place, uint32_t key, uint32_t* cm, uint32_t* cv) {
   float2 ym[4], yv[4];
   const float im = power_of_two(254 - em), iv = power_of_two(254 - ev);
   if (em <= 127 + 29 && ev <= 127 + 37) {                       // times 2^-120 and 2^-112 they still are binary32 numbers
@@ -190,7 +182,7 @@ __device__ __forceinline__ void store_codes(const float2* m, const float2* v, in
   const uint32_t scrambled = (place + key) * kRoot3;
 #pragma unroll
   for (int j = 0; j < 8; j += 2) {
-    const uint32_t u = random_bits(scrambled + (uint32_t)j * (stride * kRoot3)), w = random_bits(scrambled + (uint32_t)(j + 1) * (stride * kRoot3));
+    const uint32_t u = random_bits(scrambled + (uint32_t)j * (STRIDE * kRoot3)), w = random_bits(scrambled + (uint32_t)(j + 1) * (STRIDE * kRoot3));
     tm[j] = __float_as_uint(ym[j / 2].x) + (u & 0xffffu) * 16;  // the sign stays in bit 31
     tm[j + 1] = __float_as_uint(ym[j / 2].y) + (w & 0xffffu) * 16;
     tv[j] = __float_as_uint(yv[j / 2].x) + (u >> 16) * 32;
@@ -239,9 +231,9 @@ template <typename T, int BITS> struct Written {
 
 struct Settings { float factor, beta1, rest1, beta2, rest2, one, eps, step_size, root_c2, decay; uint32_t key; };
 
-// Eight elements of a lane, a block's 256 of a warp; place, stride: of the lane's elements in their tensor.
-template <typename T, int BITS, bool MIXED>
-__device__ __forceinline__ void update(const Settings& a, const Read<T, BITS, MIXED>& r, bool grad32, bool master, uint32_t place, uint32_t stride, Written<T, BITS>& o) {
+// Eight elements of a lane, a block's 256 of a warp; place: of the lane's first one in its tensor, the others STRIDE apart.
+template <typename T, int BITS, bool MIXED, int STRIDE>
+__device__ __forceinline__ void update(const Settings& a, const Read<T, BITS, MIXED>& r, bool grad32, bool master, uint32_t place, Written<T, BITS>& o) {
   float2 m[4], v[4];
   float largest_m = 0.0f, largest_v = 0.0f;
 #pragma unroll
@@ -275,7 +267,7 @@ __device__ __forceinline__ void update(const Settings& a, const Read<T, BITS, MI
   if (BITS == 8) {
     const uint32_t bits_m = largest_of_warp(largest_m), bits_v = largest_of_warp(largest_v);
     const int em = scale_exponent(bits_m, 8), ev = scale_exponent(bits_v, 15);
-    store_codes(m, v, em, ev, place, stride, a.key, o.m, o.v);
+    store_codes<STRIDE>(m, v, em, ev, place, a.key, o.m, o.v);
     const float nan = __int_as_float(0x7fc00000);               // a block with an infinity or NaN is NaN from here on
     o.sm = bits_m < 0x7f800000u ? power_of_two(em) : nan;
     o.sv = bits_v < 0x7f800000u ? power_of_two(ev) : nan;
@@ -329,7 +321,7 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
   constexpr uint32_t P = Rg::P;
   extern __shared__ __align__(16) uint8_t rings[];
   __shared__ Clock shared_clock;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0);   // for the compiler to see that a warp goes one way
   uint32_t here = shared_address(rings) + warp * 2 * Rg::kSlot, there = here + Rg::kSlot;
   next_may_launch();
   wait_for_previous();
@@ -387,7 +379,7 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
   const float lr = shared_clock.lr;
 
   float unit_sm = 0.0f, unit_sv = 0.0f;                         // lane i: scales of the unit's block i
-  int in_unit = 0;
+  uint32_t in_unit = 0;
 #pragma unroll 1
   while (k.here(table)) {
     const AdamPart& part = table.part[k.t];
@@ -403,12 +395,12 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
       }
       copies_end();
     }
+    const uint32_t e = k.at + lane * 8;
 #pragma unroll 1
-    for (uint32_t i = 0; i < blocks; ++i) {
-      const uint32_t at = k.at + i * 256;
-      const Lane8 l{i < wide, at + (i < wide ? lane * 8 : lane), part.numel};
+    for (uint32_t i = 0; i < wide; ++i) {
       Read<T, BITS, MIXED> r;
-      if (BITS == 8 && i < wide) {
+      const uint32_t to = e + i * 256;
+      if (BITS == 8) {
         const uint32_t block = here + i * Rg::kBlock;
         if (grad32) shared32(block + lane * 32, r.g); else shared_eight<T>(block + lane * 8 * sizeof(T), r.g);
         if (master) shared32(block + Rg::kParam + lane * 32, r.p); else shared_eight<T>(block + Rg::kParam + lane * 8 * sizeof(T), r.p);
@@ -419,23 +411,37 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
         r.sm = __uint_as_float(scales[0]);
         r.sv = __uint_as_float(scales[1]);
       } else {
-        if (grad32) take<float>(l, part.grad, r.g); else take<T>(l, part.grad, r.g);
-        if (master) take<float>(l, part.master, r.p); else take<T>(l, part.param, r.p);
-        take<State>(l, part.m, r.m);
-        take<State>(l, part.v, r.v);
-        if (BITS == 8) { r.sm = part.m_scale[at / 256]; r.sv = part.v_scale[at / 256]; }
+        if (grad32) Eight<float>::load(static_cast<const float*>(part.grad) + to, r.g); else Eight<T>::load(static_cast<const T*>(part.grad) + to, r.g);
+        if (master) Eight<float>::load(part.master + to, r.p); else Eight<T>::load(static_cast<const T*>(part.param) + to, r.p);
+        Eight<State>::load(static_cast<const State*>(part.m) + to, r.m);
+        Eight<State>::load(static_cast<const State*>(part.v) + to, r.v);
       }
       Written<T, BITS> o;
-      update<T, BITS, MIXED>(set, r, grad32, master, part.place + l.at, l.wide ? 1 : 32, o);
+      update<T, BITS, MIXED, 1>(set, r, grad32, master, part.place + to, o);
+      if (master) Eight<float>::store(part.master + to, o.master);
+      Eight<T>::store(static_cast<T*>(part.param) + to, o.p);
+      Eight<State>::store(static_cast<State*>(part.m) + to, o.m);
+      Eight<State>::store(static_cast<State*>(part.v) + to, o.v);
+      if (BITS == 8 && lane == in_unit + i) { unit_sm = o.sm; unit_sv = o.sv; }
+    }
+#pragma unroll 1
+    for (uint32_t i = wide; i < blocks; ++i) {                  // elements in turn, the last block's as far as they go
+      const Lane8 l{k.at + i * 256 + lane, part.numel};
+      Read<T, BITS, MIXED> r;
+      if (grad32) take<float>(l, part.grad, r.g); else take<T>(l, part.grad, r.g);
+      if (master) take<float>(l, part.master, r.p); else take<T>(l, part.param, r.p);
+      take<State>(l, part.m, r.m);
+      take<State>(l, part.v, r.v);
+      if (BITS == 8) { r.sm = part.m_scale[k.at / 256 + i]; r.sv = part.v_scale[k.at / 256 + i]; }
+      Written<T, BITS> o;
+      update<T, BITS, MIXED, 32>(set, r, grad32, master, part.place + l.at, o);
       if (master) put<float>(l, part.master, o.master);
       put<T>(l, part.param, o.p);
       put<State>(l, part.m, o.m);
       put<State>(l, part.v, o.v);
-      if (BITS == 8) {
-        if (lane == in_unit) { unit_sm = o.sm; unit_sv = o.sv; }
-        ++in_unit;
-      }
+      if (BITS == 8 && lane == in_unit + i) { unit_sm = o.sm; unit_sv = o.sv; }
     }
+    in_unit += blocks;
     if (BITS == 8) {                                            // the scales of a unit leave together: pieces of a sector cost as much as whole ones
       if (k.left == blocks) {
         if (lane < in_unit) {
@@ -468,9 +474,14 @@ __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(const __grid_co
   for (Walk<N> k(table, blockIdx.x * kAdamWarps + warp, gridDim.x * kAdamWarps); k.here(table); k.next(table, 1)) {
     const AdamPart& part = table.part[k.t];
     const bool wide = (part.flags & kPartWide) && k.at + 256 <= part.numel, grad32 = part.flags & kPartGradF32;
-    const Lane8 l{wide, k.at + (wide ? lane * 8 : lane), part.numel};
     uint32_t w[8];
-    if (grad32) take<float>(l, part.grad, w); else take<T>(l, part.grad, w);
+    if (wide) {
+      const uint32_t e = k.at + lane * 8;
+      if (grad32) Eight<float>::load(static_cast<const float*>(part.grad) + e, w); else Eight<T>::load(static_cast<const T*>(part.grad) + e, w);
+    } else {
+      const Lane8 l{k.at + lane, part.numel};
+      if (grad32) take<float>(l, part.grad, w); else take<T>(l, part.grad, w);
+    }
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
