@@ -529,7 +529,8 @@ int aq_layer_norm_grad(aq_stage* st, const void* dy, int64_t lddy, const void* d
 /*
  * One tensor of aq_adamw or aq_grad_norm (which reads grad, numel and grad_dtype only).  The array is host memory and is
  * read before the call returns; its addresses are device addresses.  Tensors are contiguous, may be empty, and may not overlap (a tensor
- * that two layers share is listed once).  Element alignment; addresses that are multiples of eight elements are faster.
+ * that two layers share is listed once).  Element alignment; faster are
+ * addresses of a tensor that are all equally far from a multiple of eight elements, with 8-bit moments those that are multiples.
  */
 typedef struct {
   void* param;            /* T[numel] (in/out; with a master: out) */

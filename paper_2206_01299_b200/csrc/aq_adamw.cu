@@ -27,7 +27,7 @@ namespace aq {
 namespace {
 
 constexpr int kAdamThreads = 256, kAdamWarps = kAdamThreads / 32;
-constexpr int kAdamCtas = 2, kNormCtasPerSm = 8;    // CTAs on a multiprocessor
+constexpr int kAdamCtas = 2, kNormCtasPerSm = 4;    // CTAs on a multiprocessor
 constexpr uint32_t kRoot3 = 0xBB67AE85u, kGolden = 0x9E3779B9u;   // fractions of the square root of 3 and of the golden ratio, times 2^32
 
 template <int N> struct Table {
@@ -462,33 +462,57 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
 // ---- 2-norm of the gradients ------------------------------------------------------------------------------------
 
 // Squares of eight elements are added in binary32, then everything in binary64: a stage has up to billions of them.
+template <typename G> __device__ double eight_squares(const uint32_t* w) {
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 g = Eight<G>::open(w, i);
+    s = fmaf(g.x, g.x, fmaf(g.y, g.y, s));
+  }
+  return (double)s;
+}
+// A warp's blocks of one tensor, from element `at` on.  Four blocks are on their way at a time: 492M fp16 gradients take 144 us, with one 206 us.
+template <typename G> __device__ double squares(const AdamPart& part, uint32_t at, uint32_t blocks, int lane) {
+  const G* const g = static_cast<const G*>(part.grad);
+  double sum = 0.0;
+  uint32_t i = 0;
+  if (part.flags & kPartWide) {
+    const uint32_t wide = min(blocks, (part.numel - at) / 256);
+    const G* const from = g + at + lane * 8;
+    for (; i + 4 <= wide; i += 4) {
+      uint32_t w[4][Eight<G>::W];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) Eight<G>::load(from + (i + j) * 256, w[j]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum += eight_squares<G>(w[j]);
+    }
+    for (; i < wide; ++i) {
+      uint32_t w[Eight<G>::W];
+      Eight<G>::load(from + i * 256, w);
+      sum += eight_squares<G>(w);
+    }
+  }
+#pragma unroll 1
+  for (; i < blocks; ++i) {
+    uint32_t w[Eight<G>::W];
+    take<G>(Lane8{at + i * 256 + lane, part.numel}, g, w);
+    sum += eight_squares<G>(w);
+  }
+  return sum;
+}
+
 template <typename T, int N>
-__global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(const __grid_constant__ Table<N> table, const __grid_constant__ NormScalars a) {
+__global__ void __launch_bounds__(kAdamThreads, kNormCtasPerSm) grad_norm_kernel(const __grid_constant__ Table<N> table, const __grid_constant__ NormScalars a) {
   __shared__ double sums[kAdamWarps];
   __shared__ bool last_cta;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0);
   next_may_launch();
   wait_for_previous();
   double sum = 0.0;
 #pragma unroll 1
-  for (Walk<N> k(table, blockIdx.x * kAdamWarps + warp, gridDim.x * kAdamWarps); k.here(table); k.next(table, 1)) {
+  for (Walk<N> k(table, blockIdx.x * kAdamWarps + warp, gridDim.x * kAdamWarps); k.here(table); k.next(table, k.left)) {
     const AdamPart& part = table.part[k.t];
-    const bool wide = (part.flags & kPartWide) && k.at + 256 <= part.numel, grad32 = part.flags & kPartGradF32;
-    uint32_t w[8];
-    if (wide) {
-      const uint32_t e = k.at + lane * 8;
-      if (grad32) Eight<float>::load(static_cast<const float*>(part.grad) + e, w); else Eight<T>::load(static_cast<const T*>(part.grad) + e, w);
-    } else {
-      const Lane8 l{k.at + lane, part.numel};
-      if (grad32) take<float>(l, part.grad, w); else take<T>(l, part.grad, w);
-    }
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 g = grad32 ? Eight<float>::open(w, i) : Eight<T>::open(w, i);
-      s = fmaf(g.x, g.x, fmaf(g.y, g.y, s));
-    }
-    sum += (double)s;
+    sum += part.flags & kPartGradF32 ? squares<float>(part, k.at, k.left, lane) : squares<T>(part, k.at, k.left, lane);
   }
   auto join = [&](double x) {                 // the CTA's sum, for thread 0
 #pragma unroll

@@ -189,6 +189,9 @@ int check_adam_state(aq_stage* st, const char* who, int64_t i, const aq_adam_ten
   return AQ_OK;
 }
 
+// Elements of p until the next multiple of eight of them.
+int until_eight(const void* p, int bytes) { return (int)((8 - (reinterpret_cast<uintptr_t>(p) / bytes & 7)) & 7); }
+
 // The next tensors that are not empty, from element *from of tensor *i on, in parts of at most kPartMost elements, at most kAdamTable of
 // them; bits 0: gradients only.
 int gather_parts(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, int bits, int64_t* i, int64_t* from, aq::AdamPart* parts) {
@@ -196,12 +199,19 @@ int gather_parts(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, int bit
   for (; *i < n; ++*i, *from = 0) {
     const aq_adam_tensor& t = tensors[*i];
     const int size = (int)size_of(st->dtype), grad_size = (int)size_of(t.grad_dtype), state_size = bits == 8 ? 1 : 4;
-    bool wide = !misaligned(t.grad, 8 * grad_size);
-    if (bits) wide = wide && !misaligned(t.param, 8 * size) && !misaligned(t.master, 32) && !misaligned(t.m, 8 * state_size) && !misaligned(t.v, 8 * state_size);
+    // how far all addresses are from a multiple of eight elements, if they agree
+    const int head = until_eight(t.grad, grad_size);
+    bool agree = true;
+    if (bits) agree = until_eight(t.param, size) == head && (!t.master || until_eight(t.master, 4) == head) && until_eight(t.m, state_size) == head && until_eight(t.v, state_size) == head;
+    if (bits == 8 && head) agree = false;                    // its blocks are counted from the tensor's beginning
     const bool f32 = t.grad_dtype == AQ_FP32 && st->dtype != AQ_FP32;
-    for (; *from < t.numel; *from += aq::kPartMost) {
+    for (int64_t count; *from < t.numel; *from += count) {
       if (have == aq::kAdamTable) return have;
-      const int64_t e = *from, left = t.numel - e;
+      const int64_t e = *from;
+      // a few elements by themselves, and the rest begins where wide accesses may
+      const bool first = agree && head && e == 0;
+      count = first ? head : aq::kPartMost;
+      if (count > t.numel - e) count = t.numel - e;
       auto at = [e](const void* p, int bytes) { return p ? const_cast<char*>(static_cast<const char*>(p)) + e * bytes : nullptr; };
       aq::AdamPart& p = parts[have++];
       p = aq::AdamPart{};
@@ -214,9 +224,9 @@ int gather_parts(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, int bit
         if (bits == 8) { p.m_scale = t.m_scale + e / 256; p.v_scale = t.v_scale + e / 256; }
         p.decay = t.weight_decay;
       }
-      p.numel = (uint32_t)(left < aq::kPartMost ? left : aq::kPartMost);
+      p.numel = (uint32_t)count;
       p.place = (uint32_t)e;
-      p.flags = (wide ? aq::kPartWide : 0u) | (f32 ? aq::kPartGradF32 : 0u);
+      p.flags = (agree && !first ? aq::kPartWide : 0u) | (f32 ? aq::kPartGradF32 : 0u);
     }
   }
   return have;
