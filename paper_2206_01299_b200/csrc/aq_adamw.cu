@@ -95,34 +95,18 @@ template <typename T> __device__ void put(const Lane8& l, void* to, const uint32
     if (l.has(j)) Eight<T>::store_one(p + 32 * j, j, w);
 }
 
-// ---- copies to shared memory that a warp waits for later ------------------------------------------------------
+// ---- eight elements to and from shared memory ---------------------------------------------------------------
 
-__device__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
-__device__ void copy8(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory"); }
-__device__ void copy4(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory"); }
-__device__ void copy32(uint32_t to, const void* from) { copy16(to, from); copy16(to + 16, static_cast<const char*>(from) + 16); }
-template <typename T> __device__ void copy_eight(uint32_t to, const void* from) { if (sizeof(T) == 4) copy32(to, from); else copy16(to, from); }
-__device__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// a warp's 256 values, 16 bytes a lane at a time
+__device__ void copy_1k(uint32_t to, const char* from) { copy16(to, from); copy16(to + 512, from + 512); }
+template <typename T> __device__ void copy_block(uint32_t to, const char* from) { if (sizeof(T) == 4) copy_1k(to, from); else copy16(to, from); }
 __device__ void shared8(uint32_t from, uint32_t* w) { asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(from) : "memory"); }
 __device__ void shared16(uint32_t from, uint32_t* w) { asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from) : "memory"); }
 __device__ void shared32(uint32_t from, uint32_t* w) { shared16(from, w); shared16(from + 16, w + 4); }
 template <typename T> __device__ void shared_eight(uint32_t from, uint32_t* w) { if constexpr (sizeof(T) == 4) shared32(from, w); else shared16(from, w); }
 
-// ---- arithmetic on pairs: one instruction for two, each rounded as a single one is ---------------------------------------
+// ---- arithmetic of the step -----------------------------------------------------------------------------------
 
-__device__ float2 both(float x) { return make_float2(x, x); }
-__device__ float2 mul2(float2 a, float2 b) {
-  float2 c;
-  asm("{.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmul.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;}" : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return c;
-}
-__device__ float2 fma2(float2 a, float2 b, float2 d) {
-  float2 c;
-  asm("{.reg .b64 x, y, z, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 w, {%6, %7};\nfma.rn.f32x2 z, x, y, w;\nmov.b64 {%0, %1}, z;}"
-      : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(d.x), "f"(d.y));
-  return c;
-}
 // a + b, where both may be products that have been rounded: a packed product and sum become one fused operation in the assembler, rounding
 // modes or not, and a factor of one that it does not know keeps them apart
 __device__ float2 sum2(float2 a, float2 b, float one) { return fma2(a, both(one), b); }
@@ -337,15 +321,15 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
     const AdamPart& part = table.part[k.t];
     const uint32_t blocks = wide_blocks(k), e = k.at + lane * 8;
     const bool grad32 = MIXED && (part.flags & kPartGradF32), master = MIXED && part.master;
-    const char* const g = static_cast<const char*>(part.grad) + (size_t)e * (grad32 ? 4 : sizeof(T));
-    const char* const p = master ? reinterpret_cast<const char*>(part.master + e) : reinterpret_cast<const char*>(static_cast<T*>(part.param) + e);
+    const char* const g = static_cast<const char*>(part.grad) + (size_t)k.at * (grad32 ? 4 : sizeof(T)) + lane * 16;
+    const char* const p = (master ? reinterpret_cast<const char*>(part.master + k.at) : reinterpret_cast<const char*>(static_cast<T*>(part.param) + k.at)) + lane * 16;
     const uint8_t *const m = static_cast<uint8_t*>(part.m) + e, *const v = static_cast<uint8_t*>(part.v) + e;
 #pragma unroll
     for (uint32_t i = 0; i < P; ++i) {
       if (i >= blocks) break;
       const uint32_t block = to + i * Rg::kBlock;
-      if (grad32) copy32(block + lane * 32, g + i * 1024); else copy_eight<T>(block + lane * 8 * sizeof(T), g + i * 256 * sizeof(T));
-      if (master) copy32(block + Rg::kParam + lane * 32, p + i * 1024); else copy_eight<T>(block + Rg::kParam + lane * 8 * sizeof(T), p + i * 256 * sizeof(T));
+      if (grad32) copy_1k(block + lane * 16, g + i * 1024); else copy_block<T>(block + lane * 16, g + i * 256 * sizeof(T));
+      if (master) copy_1k(block + Rg::kParam + lane * 16, p + i * 1024); else copy_block<T>(block + Rg::kParam + lane * 16, p + i * 256 * sizeof(T));
       copy8(block + Rg::kM + lane * 8, m + i * 256);
       copy8(block + Rg::kV + lane * 8, v + i * 256);
     }

@@ -20,7 +20,16 @@
 namespace aq {
 namespace {
 
-// A lane's piece of a row: 16 bytes, or one element where rows are not whole 16-byte pieces.
+template <typename T> struct Scalar {
+  static __device__ float open(T x) { return (float)x; }
+  static __device__ T close(float x) { return Num<T>::one(x); }
+};
+template <> struct Scalar<float> {
+  static __device__ float open(float x) { return x; }
+  static __device__ float close(float x) { return x; }
+};
+
+// A lane's piece of a row: 16 bytes, or one element where rows do not begin on 16-byte boundaries.
 template <typename T, bool WHOLE> struct Piece;
 template <typename T> struct Piece<T, true> {
   static constexpr int N = 8;
@@ -44,14 +53,6 @@ template <> struct Piece<float, true> {
   static __device__ void open(Raw v, float* f) { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
   static __device__ Raw close(const float* f) { return make_float4(f[0], f[1], f[2], f[3]); }
 };
-template <typename T> struct Scalar {
-  static __device__ float open(T x) { return (float)x; }
-  static __device__ T close(float x) { return Num<T>::one(x); }
-};
-template <> struct Scalar<float> {
-  static __device__ float open(float x) { return x; }
-  static __device__ float close(float x) { return x; }
-};
 template <typename T> struct Piece<T, false> {
   static constexpr int N = 1;
   using Raw = T;
@@ -60,6 +61,26 @@ template <typename T> struct Piece<T, false> {
   static __device__ void open(Raw v, float* f) { f[0] = Scalar<T>::open(v); }
   static __device__ Raw close(const float* f) { return Scalar<T>::close(f[0]); }
 };
+
+// Pieces of which a row has `left` elements only: zeros behind them, and only they are stored.
+template <typename Pc, typename T> __device__ typename Pc::Raw load_piece(const T* p, int left) {
+  if (left >= Pc::N) return Pc::load(p);
+  float f[Pc::N];
+#pragma unroll
+  for (int j = 0; j < Pc::N; ++j) f[j] = j < left ? Scalar<T>::open(p[j]) : 0.0f;
+  return Pc::close(f);
+}
+template <typename Pc, typename T> __device__ void store_piece(T* p, typename Pc::Raw v, int left) {
+  if (left >= Pc::N) {
+    Pc::store(p, v);
+    return;
+  }
+  float f[Pc::N];
+  Pc::open(v, f);
+#pragma unroll
+  for (int j = 0; j < Pc::N; ++j)
+    if (j < left) p[j] = Scalar<T>::close(f[j]);
+}
 
 __device__ float warp_sum(float x) {
 #pragma unroll
@@ -85,47 +106,42 @@ template <int W> __device__ float cta_sum(float x, float* shared) {
 template <typename T, bool WHOLE, int W, int P>
 __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) layer_norm_kernel(const LayerNormArgs a) {
   using Pc = Piece<T, WHOLE>;
-  constexpr int N = Pc::N, kThreads = 32 * W;
+  constexpr int N = Pc::N, kStep = 32 * W * N;
   __shared__ float shared[2][W];
   const long long row = W == 1 ? (long long)blockIdx.x * 4 + threadIdx.x / 32 : blockIdx.x;
   const int lane = W == 1 ? threadIdx.x & 31 : threadIdx.x;
   next_may_launch();
   wait_for_previous();
   if (W == 1 && row >= a.rows) return;
-  const int pieces = a.hidden / N;
   const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
+  const int left = a.hidden - lane * N;                       // elements of the row from the lane's first piece on; its pieces are kStep apart
   typename Pc::Raw v[P];
 #pragma unroll
-  for (int i = 0; i < P; ++i) {
-    const int at = lane + i * kThreads;
-    if (at < pieces) v[i] = Pc::load(x + at * N);
-  }
-  float total = 0.0f;
+  for (int i = 0; i < P; ++i)
+    if (left > i * kStep) v[i] = load_piece<Pc>(x + lane * N + i * kStep, left - i * kStep);
   if (a.residual) {
     const T* const r = static_cast<const T*>(a.residual) + row * a.ldr;
     T* const sum = a.sum ? static_cast<T*>(a.sum) + row * a.lds : nullptr;
     typename Pc::Raw o[P];
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int at = lane + i * kThreads;
-      if (at < pieces) o[i] = Pc::load(r + at * N);
-    }
+    for (int i = 0; i < P; ++i)
+      if (left > i * kStep) o[i] = load_piece<Pc>(r + lane * N + i * kStep, left - i * kStep);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int at = lane + i * kThreads;
-      if (at >= pieces) continue;
+      if (left <= i * kStep) continue;
       float f[N], e[N];
       Pc::open(v[i], f);
       Pc::open(o[i], e);
 #pragma unroll
       for (int j = 0; j < N; ++j) f[j] += e[j];
       v[i] = Pc::close(f);
-      if (sum) Pc::store(sum + at * N, v[i]);
+      if (sum) store_piece<Pc>(sum + lane * N + i * kStep, v[i], left - i * kStep);
     }
   }
+  float total = 0.0f;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    if (lane + i * kThreads >= pieces) continue;
+    if (left <= i * kStep) continue;
     float f[N];
     Pc::open(v[i], f);
 #pragma unroll
@@ -136,11 +152,17 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) layer_norm_kernel(const
   float squares = 0.0f;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    if (lane + i * kThreads >= pieces) continue;
+    if (left <= i * kStep) continue;
     float f[N];
     Pc::open(v[i], f);
+    if (left - i * kStep >= N) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) squares = fmaf(f[j] - mean, f[j] - mean, squares);
+      for (int j = 0; j < N; ++j) squares = fmaf(f[j] - mean, f[j] - mean, squares);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j < left - i * kStep) squares = fmaf(f[j] - mean, f[j] - mean, squares);
+    }
   }
   const float rstd = 1.0f / sqrtf(fmaf(cta_sum<W>(squares, shared[1]), inverse, a.eps));
   if (lane == 0) {
@@ -150,25 +172,25 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) layer_norm_kernel(const
   T* const y = static_cast<T*>(a.y) + row * a.ldy;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    const int at = lane + i * kThreads;
-    if (at >= pieces) continue;
+    if (left <= i * kStep) continue;
+    const int at = lane * N + i * kStep;
     float f[N], w[N], b[N];
     Pc::open(v[i], f);
     if (a.w) {
-      Pc::open(Pc::load(static_cast<const T*>(a.w) + at * N), w);
+      Pc::open(load_piece<Pc>(static_cast<const T*>(a.w) + at, left - i * kStep), w);
     } else {
 #pragma unroll
       for (int j = 0; j < N; ++j) w[j] = 1.0f;
     }
     if (a.b) {
-      Pc::open(Pc::load(static_cast<const T*>(a.b) + at * N), b);
+      Pc::open(load_piece<Pc>(static_cast<const T*>(a.b) + at, left - i * kStep), b);
     } else {
 #pragma unroll
       for (int j = 0; j < N; ++j) b[j] = 0.0f;
     }
 #pragma unroll
     for (int j = 0; j < N; ++j) f[j] = fmaf((f[j] - mean) * rstd, w[j], b[j]);
-    Pc::store(y + at * N, Pc::close(f));
+    store_piece<Pc>(y + at, Pc::close(f), left - i * kStep);
   }
 }
 
@@ -227,7 +249,7 @@ template <typename T, bool WHOLE, int W, int P> cudaError_t run(const LayerNormA
 
 template <typename T> cudaError_t run_forward(const LayerNormArgs& a, cudaStream_t s) {
   if (a.whole) {
-    const int pieces = a.hidden / Piece<T, true>::N;
+    const int pieces = (a.hidden + Piece<T, true>::N - 1) / Piece<T, true>::N;
     if (pieces <= 32) return run<T, true, 1, 1>(a, s);
     if (pieces <= 64) return run<T, true, 1, 2>(a, s);
     if (pieces <= 128) return run<T, true, 1, 4>(a, s);
@@ -245,131 +267,222 @@ template <typename T> cudaError_t run_forward(const LayerNormArgs& a, cudaStream
 
 // ---- gradient ------------------------------------------------------------------------------------------------
 
-constexpr int kGradRows = 2;                  // rows of a CTA (of a warp, where a row is a warp's) at a time
-constexpr int kGradCtasPerSm = 2;
-
-// Sums of four values over a warp: halves are exchanged first, so that six shuffles do for twenty.  Lane l gets value l / 8.
-__device__ float warp_sum4(const float* v, int lane) {
-  const bool up = lane & 16, side = lane & 8;
-  const float a = (up ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, up ? v[0] : v[2], 16);
-  const float b = (up ? v[3] : v[1]) + __shfl_xor_sync(0xffffffffu, up ? v[1] : v[3], 16);
-  float x = (side ? b : a) + __shfl_xor_sync(0xffffffffu, side ? a : b, 8);
+// Sixteen bytes of a row in pairs.
+template <typename T> struct Pairs {
+  static constexpr int N = 4;
+  static __device__ void open(uint4 raw, float2* f) {
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-  for (int o = 4; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  return x;
+    for (int i = 0; i < 4; ++i) f[i] = Num<T>::open(w[i]);
+  }
+  static __device__ uint4 close(const float2* f) {
+    return make_uint4(Num<T>::close(f[0].x, f[0].y), Num<T>::close(f[1].x, f[1].y), Num<T>::close(f[2].x, f[2].y), Num<T>::close(f[3].x, f[3].y));
+  }
+};
+template <> struct Pairs<float> {
+  static constexpr int N = 2;
+  static __device__ void open(uint4 raw, float2* f) {
+    f[0] = make_float2(__uint_as_float(raw.x), __uint_as_float(raw.y));
+    f[1] = make_float2(__uint_as_float(raw.z), __uint_as_float(raw.w));
+  }
+  static __device__ uint4 close(const float2* f) { return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y)); }
+};
+
+// Sums of V values over a warp: halves are exchanged first, so that a handful of shuffles do for 5 V.  Lane l gets value l / (32 / V).
+template <int V> __device__ float warp_sums(const float* v, int lane) {
+  float x[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) x[i] = v[i];
+#pragma unroll
+  for (int n = V / 2, o = 16; n; n /= 2, o /= 2) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int i = 0; i < n; ++i) x[i] = (up ? x[i + n] : x[i]) + __shfl_xor_sync(0xffffffffu, up ? x[i] : x[i + n], o);
+  }
+#pragma unroll
+  for (int o = 16 / V; o; o >>= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+  return x[0];
 }
 
-// WARP: a row is a warp's, eight rows' walks to a CTA.  Otherwise the CTA has a thread to every piece of a row.
-template <typename T, bool WARP, int MAX>
-__global__ void __launch_bounds__(MAX, MAX <= 256 ? kGradCtasPerSm : 1) layer_norm_grad_kernel(const LayerNormGradArgs a) {
-  using Pc = Piece<T, true>;
-  constexpr int N = Pc::N, R = kGradRows;
-  __shared__ float4 exchange[2][WARP ? 1 : MAX / 32];
-  __shared__ float sums[WARP ? 2 : 1][WARP ? 8 : 1][WARP ? 32 * N : 1];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, warps = blockDim.x / 32;
-  const int piece = WARP ? lane : threadIdx.x;
+// Sums of dw and db are kept in rows of whole sectors: pieces of a sector cost as much to write as all of it.
+__host__ __device__ constexpr int padded_hidden(int hidden) { return (hidden + 7) / 8 * 8; }
+__device__ void store_sums(float* to, const float2* f, int pairs) {
+  if (pairs == 4) {
+    asm volatile("st.global.v8.f32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                 ::"f"(f[0].x), "f"(f[0].y), "f"(f[1].x), "f"(f[1].y), "f"(f[2].x), "f"(f[2].y), "f"(f[3].x), "f"(f[3].y), "l"(to) : "memory");
+  } else {
+    *reinterpret_cast<float4*>(to) = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
+  }
+}
+
+constexpr int kGradWalks = 8;                 // rows' walks of a CTA where a row is a warp's
+constexpr int kGradSlots = 2;                 // batches of rows that a thread has in shared memory: the one it works on and the next
+
+// A CTA's threads have Q pieces of 16 bytes of a row each (WARP: a warp's lanes, and eight walks to a CTA) and take R rows at a time.  The next rows
+// are copied to shared memory meanwhile, each thread's elements by itself and for itself.  Elements behind a row's end are zeros there and add
+// nothing to any sum.
+template <typename T, bool WARP, int R, int Q, int MAX, int CTAS>
+__global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerNormGradArgs a) {
+  using Ps = Pairs<T>;
+  constexpr int H = Ps::N, N = 2 * H, V = 2 * R;
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ float exchange[2][WARP ? 1 : MAX / 32][V];
+  __shared__ float stats[kGradSlots][MAX / 32][V];
+  __shared__ float sums[WARP ? 2 : 1][WARP ? kGradWalks : 1][WARP ? 32 * N * Q : 1];
+  const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), warps = blockDim.x / 32;
+  const bool skip = a.dsum != nullptr;
+  // shared memory: a thread's 16 bytes of every piece, array and row; `part` from one to the next
+  const uint32_t part = blockDim.x * 16, row_bytes = part * Q * (skip ? 3 : 2), mine = shared_address(ring) + threadIdx.x * 16;
   next_may_launch();
   wait_for_previous();
-  const bool holds = piece < a.hidden / N;
-  const int column = holds ? piece * N : 0;                   // a thread without a piece reads the row's first and uses nothing of it
-  const long long walks = WARP ? (long long)gridDim.x * 8 : gridDim.x;
-  const long long walk = WARP ? (long long)blockIdx.x * 8 + warp : blockIdx.x;
-  const T* const s_rows = static_cast<const T*>(a.s) + column;
-  const T* const g_rows = static_cast<const T*>(a.dy) + column;
-  const T* const k_rows = a.dsum ? static_cast<const T*>(a.dsum) + column : nullptr;
-  T* const o_rows = a.dx ? static_cast<T*>(a.dx) + column : nullptr;
-  float w[N], dw[N], db[N];
+  const int walks = WARP ? gridDim.x * kGradWalks : gridDim.x, walk = WARP ? blockIdx.x * kGradWalks + warp : blockIdx.x;
+  int column[Q], have[Q];                                      // of the thread's elements those in the row
+  float2 w[Q][H], dw[Q][H], db[Q][H];
 #pragma unroll
-  for (int j = 0; j < N; ++j) { w[j] = 1.0f; dw[j] = 0.0f; db[j] = 0.0f; }
-  if (a.w) Pc::open(Pc::load(static_cast<const T*>(a.w) + column), w);
-  const float inverse = 1.0f / (float)a.hidden;
-  typename Pc::Raw ns[R], ng[R], nk[R];
-  float nmean[R], nrstd[R];
-  auto load = [&](long long row) {
+  for (int q = 0; q < Q; ++q) {
+    column[q] = (WARP ? lane + 32 * q : (int)(threadIdx.x + q * blockDim.x)) * N;
+    have[q] = min(max(a.hidden - column[q], 0), N);
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const long long r = min(row + i, a.rows - 1);
-      ns[i] = Pc::load(s_rows + r * a.lds);
-      ng[i] = Pc::load(g_rows + r * a.lddy);
-      if (k_rows) nk[i] = Pc::load(k_rows + r * a.ldds);
-      nmean[i] = __ldg(a.mean + r);
-      nrstd[i] = __ldg(a.rstd + r);
-    }
-  };
-  long long row = walk * R;
-  if (row < a.rows) load(row);
-  int turn = 0;
-  for (; row < a.rows; row += walks * R, turn ^= 1) {
-    float n[R][N], g[R][N], rstd[R], part[2 * R];
-    typename Pc::Raw skip[R];
+    for (int j = 0; j < H; ++j) w[q][j] = dw[q][j] = db[q][j] = make_float2(0.0f, 0.0f);
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      Pc::open(ns[i], n[i]);
-      Pc::open(ng[i], g[i]);
-      skip[i] = nk[i];
-      rstd[i] = nrstd[i];
-      const bool counts = holds && row + i < a.rows;
-      part[2 * i] = part[2 * i + 1] = 0.0f;
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        n[i][j] = (n[i][j] - nmean[i]) * rstd[i];
-        if (counts) {                                          // what does not may be NaN or infinite: left out, not times 0
-          dw[j] = fmaf(g[i][j], n[i][j], dw[j]);
-          db[j] += g[i][j];
-        }
-        g[i][j] *= w[j];
-        part[2 * i] += g[i][j];
-        part[2 * i + 1] = fmaf(g[i][j], n[i][j], part[2 * i + 1]);
-      }
-      if (!holds) part[2 * i] = part[2 * i + 1] = 0.0f;
-    }
-    if (row + walks * R < a.rows) load(row + walks * R);
-    if (!o_rows) continue;
-    const float x = warp_sum4(part, lane);                     // value lane / 8
-    float joined[4];
-    if (WARP) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) joined[i] = __shfl_sync(0xffffffffu, x, 8 * i);
-    } else {
-      if (lane % 8 == 0) reinterpret_cast<float*>(&exchange[turn][warp])[lane / 8] = x;
-      __syncthreads();
-      joined[0] = joined[1] = joined[2] = joined[3] = 0.0f;
-      for (int i = 0; i < warps; ++i) {
-        const float4 o = exchange[turn][i];
-        joined[0] += o.x; joined[1] += o.y; joined[2] += o.z; joined[3] += o.w;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      if (!holds || row + i >= a.rows) continue;
-      const float c1 = joined[2 * i] * inverse, c2 = joined[2 * i + 1] * inverse;
-      float o[N], k[N];
-#pragma unroll
-      for (int j = 0; j < N; ++j) o[j] = rstd[i] * (g[i][j] - fmaf(n[i][j], c2, c1));
-      if (k_rows) {
-        Pc::open(skip[i], k);
-#pragma unroll
-        for (int j = 0; j < N; ++j) o[j] += k[j];
-      }
-      Pc::store(o_rows + (row + i) * a.lddx, Pc::close(o));
+    for (int j = 0; j < N; ++j) {
+      if (j >= have[q]) break;
+      (j & 1 ? w[q][j / 2].y : w[q][j / 2].x) = a.w ? Scalar<T>::open(static_cast<const T*>(a.w)[column[q] + j]) : 1.0f;
     }
   }
+  const float inverse = 1.0f / (float)a.hidden;
+  // the next batch's rows: addresses move on by constants
+  const long long first = (long long)walk * R;
+  const T *s = static_cast<const T*>(a.s) + first * a.lds, *g = static_cast<const T*>(a.dy) + first * a.lddy;
+  const T* k = skip ? static_cast<const T*>(a.dsum) + first * a.ldds : nullptr;
+  T* o = a.dx ? static_cast<T*>(a.dx) + first * a.lddx : nullptr;
+  const float* stat = (lane & 1 ? a.rstd : a.mean) + first + (lane % V) / 2;
+  const int step = walks * R;
+  long long left = a.rows - first;                             // rows from the next batch to ask for on
+  auto ask = [&](int slot) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if (i >= left) break;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const int bytes = have[q] * (int)sizeof(T), at = bytes ? column[q] : 0;   // a thread without elements reads nothing, from a valid address
+        const uint32_t to = mine + (slot * R + i) * row_bytes + q * part;
+        copy16(to, s + i * a.lds + at, bytes);
+        copy16(to + Q * part, g + i * a.lddy + at, bytes);
+        if (skip) copy16(to + 2 * Q * part, k + i * a.ldds + at, bytes);
+      }
+    }
+    if (lane < V && lane / 2 < left) copy4(shared_address(&stats[slot][warp][lane]), stat);   // mean and rstd of the rows, for the warp
+    s += step * a.lds;
+    g += step * a.lddy;
+    if (skip) k += step * a.ldds;
+    stat += step;
+    left -= step;
+  };
+  if (left > 0) ask(0);
+  copies_end();
+  int slot = 0;
+#pragma unroll 1
+  for (int here = (int)min(a.rows - first, (long long)0x7fffffff); here > 0; here -= step, slot ^= 1) {   // rows from this batch on
+    __syncwarp();                                              // the warp has read the other slot's statistics
+    if (left > 0) ask(slot ^ 1);
+    copies_end();
+    copies_wait<1>();
+    __syncwarp();
+    auto take = [&](int i, int array, int q, float2* f) { Ps::open(shared16(mine + (slot * R + i) * row_bytes + (array * Q + q) * part), f); };
+    float sum[V];
+    float2 n[R][Q][H], y[R][Q][H];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      sum[2 * i] = sum[2 * i + 1] = 0.0f;
+      if (i >= here) break;
+      const float mean = stats[slot][warp][2 * i], rstd = stats[slot][warp][2 * i + 1];
+      float2 sg = make_float2(0.0f, 0.0f), sgn = sg;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        take(i, 0, q, n[i][q]);
+        take(i, 1, q, y[i][q]);
+#pragma unroll
+        for (int j = 0; j < H; ++j) {
+          n[i][q][j] = mul2(add2(n[i][q][j], both(-mean)), both(rstd));
+          dw[q][j] = fma2(y[i][q][j], n[i][q][j], dw[q][j]);
+          db[q][j] = add2(db[q][j], y[i][q][j]);
+          y[i][q][j] = mul2(y[i][q][j], w[q][j]);
+          sg = add2(sg, y[i][q][j]);
+          sgn = fma2(y[i][q][j], n[i][q][j], sgn);
+        }
+      }
+      sum[2 * i] = sg.x + sg.y;
+      sum[2 * i + 1] = sgn.x + sgn.y;
+    }
+    if (!o) continue;
+    float x = warp_sums<V>(sum, lane);                         // value lane / (32 / V)
+    if (WARP) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum[i] = __shfl_sync(0xffffffffu, x, i * (32 / V)) * inverse;
+    } else {
+      if (lane % (32 / V) == 0) exchange[slot][warp][lane / (32 / V)] = x;
+      __syncthreads();
+      x = 0.0f;
+      for (int i = lane / V; i < warps; i += 32 / V) x += exchange[slot][i][lane % V];
+#pragma unroll
+      for (int m = V; m < 32; m *= 2) x += __shfl_xor_sync(0xffffffffu, x, m);
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum[i] = __shfl_sync(0xffffffffu, x, i) * inverse;
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if (i >= here) break;
+      const float rstd = stats[slot][warp][2 * i + 1];
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        if (!have[q]) continue;
+        float2 f[H];
+        if (skip) take(i, 2, q, f);
+#pragma unroll
+        for (int j = 0; j < H; ++j) {
+          const float2 d = add2(fma2(n[i][q][j], both(-sum[2 * i + 1]), y[i][q][j]), both(-sum[2 * i]));
+          f[j] = skip ? fma2(d, both(rstd), f[j]) : mul2(d, both(rstd));
+        }
+        T* const to = o + i * a.lddx + column[q];
+        if (have[q] == N) {
+          *reinterpret_cast<uint4*>(to) = Ps::close(f);
+        } else {
+#pragma unroll
+          for (int j = 0; j < N; ++j)
+            if (j < have[q]) to[j] = Scalar<T>::close(j & 1 ? f[j / 2].y : f[j / 2].x);
+        }
+      }
+    }
+    o += step * a.lddx;
+  }
   if (!a.dw && !a.db) return;
-  float* const out = a.partials + (long long)blockIdx.x * 2 * a.hidden;
+  const int padded = padded_hidden(a.hidden);
+  float* const out = a.partials + (long long)blockIdx.x * 2 * padded;
   if (WARP) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) { sums[0][warp][lane * N + j] = dw[j]; sums[1][warp][lane * N + j] = db[j]; }
+    for (int q = 0; q < Q; ++q) {
+#pragma unroll
+      for (int j = 0; j < H; ++j) {
+        reinterpret_cast<float2*>(&sums[0][warp][column[q]])[j] = dw[q][j];
+        reinterpret_cast<float2*>(&sums[WARP ? 1 : 0][warp][column[q]])[j] = db[q][j];
+      }
+    }
     __syncthreads();
-    for (int e = threadIdx.x; e < 2 * a.hidden; e += 256) {
-      const int t = e >= a.hidden, j = e - t * a.hidden;
+    for (int e = threadIdx.x; e < 2 * padded; e += blockDim.x) {
+      const int t = e >= padded, j = e - t * padded;
       float s = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s += sums[t][i][j];
+      for (int i = 0; i < (WARP ? kGradWalks : 1); ++i) s += sums[WARP ? t : 0][i][j];
       out[e] = s;
     }
-  } else if (holds) {
+  } else {
 #pragma unroll
-    for (int j = 0; j < N; ++j) { out[column + j] = dw[j]; out[a.hidden + column + j] = db[j]; }
+    for (int q = 0; q < Q; ++q) {
+      if (!have[q]) continue;
+      store_sums(out + column[q], dw[q], H);
+      store_sums(out + padded + column[q], db[q], H);
+    }
   }
 }
 
@@ -397,7 +510,7 @@ __global__ void __launch_bounds__(kColumns * kWalks) layer_norm_columns_kernel(c
     float x = 0.0f;
 #pragma unroll
     for (int i = 0; i < kWalks; ++i) x += sums[threadIdx.y][i][threadIdx.x];
-    a.partials[((long long)blockIdx.y * 2 + threadIdx.y) * a.hidden + column] = x;
+    a.partials[((long long)blockIdx.y * 2 + threadIdx.y) * padded_hidden(a.hidden) + column] = x;
   }
 }
 
@@ -428,64 +541,86 @@ __global__ void __launch_bounds__(kRowThreads) layer_norm_rows_kernel(const Laye
   }
 }
 
-// dw and db from the sums of the CTAs: a warp's lanes take neighbouring columns, the warps of a CTA every eighth row of sums.
-__global__ void __launch_bounds__(256) layer_norm_join_kernel(const float* partials, int parts, int hidden, float* dw, float* db) {
-  __shared__ float sums[8][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+// dw and db from the sums of the CTAs: a warp's lanes take neighbouring columns, the warps of a CTA every kJoinWarps-th row of sums.
+constexpr int kJoinWarps = 16;
+__global__ void __launch_bounds__(32 * kJoinWarps) layer_norm_join_kernel(const float* partials, int parts, int hidden, float* dw, float* db) {
+  __shared__ float sums[kJoinWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, padded = padded_hidden(hidden);
   const long long e = (long long)blockIdx.x * 32 + lane;
   next_may_launch();
   wait_for_previous();
   float s = 0.0f;
-  if (e < 2ll * hidden) {
+  if (e < 2ll * padded) {
 #pragma unroll 8
-    for (int i = warp; i < parts; i += 8) s += __ldcg(partials + i * 2ll * hidden + e);
+    for (int i = warp; i < parts; i += kJoinWarps) s += __ldcg(partials + i * 2ll * padded + e);
   }
   sums[warp][lane] = s;
   __syncthreads();
-  if (warp || e >= 2ll * hidden) return;
+  if (warp) return;
 #pragma unroll
-  for (int i = 1; i < 8; ++i) s += sums[i][lane];
-  float* const out = e < hidden ? dw : db;
-  if (out) out[e < hidden ? e : e - hidden] = s;
+  for (int i = 1; i < kJoinWarps; ++i) s += sums[i][lane];
+  const long long column = e < padded ? e : e - padded;
+  float* const out = e < padded ? dw : db;
+  if (out && column < hidden && e < 2ll * padded) out[column] = s;
 }
 
-// How a gradient is computed: rows of a warp, rows of a CTA with a thread to a piece, or by columns and rows apart.
-struct GradPlan { int threads; bool warp, apart; long long parts; };
-template <typename T> GradPlan grad_plan(const LayerNormGradArgs& a) {
-  const int pieces = a.hidden / Piece<T, true>::N;
+// How a gradient is computed: rows of a warp, rows of a CTA, or by columns and rows apart.  Threads have eight elements of a row, or
+// sixteen of rows wider than 2048, and as many CTAs run as are resident at a time.
+constexpr int kGradNarrow = 256, kGradWide = 512;             // threads of the CTAs that the registers are cut for
+constexpr int kGradRows = 2;                                  // rows at a time, where threads have eight elements
+constexpr int kSharedOfSm = 227 * 1024;
+struct GradPlan { int threads, each; bool warp, apart; int bytes; long long parts; };
+GradPlan grad_plan(const LayerNormGradArgs& a) {
   GradPlan p{};
-  p.apart = !a.whole || pieces > 1024;
+  p.each = a.hidden <= 8 * kGradNarrow ? 8 : 16;
+  p.apart = !a.whole || a.hidden > 16 * kGradWide;
   if (p.apart) {
     const long long strips = (a.hidden + kColumns - 1) / kColumns, walks = (a.rows + kWalks - 1) / kWalks;
     const long long most = (8ll * a.sms + strips - 1) / strips;
     p.parts = walks < most ? walks : most;
     return p;
   }
-  p.warp = pieces <= 32;
-  p.threads = p.warp ? 256 : (pieces + 31) / 32 * 32;
-  // as many CTAs as are resident at a time
-  const int per_sm = p.threads > 256 ? 1 : kGradCtasPerSm * (256 / p.threads);
-  const long long batches = (a.rows + kGradRows * (p.warp ? 8 : 1) - 1) / (kGradRows * (p.warp ? 8 : 1));
-  p.parts = batches < (long long)per_sm * a.sms ? batches : (long long)per_sm * a.sms;
+  p.warp = a.hidden <= 8 * 32;
+  const int piece = 16 / a.size, pieces = (a.hidden + piece - 1) / piece, of_thread = p.each / piece;
+  p.threads = p.warp ? 32 * kGradWalks : ((pieces + of_thread - 1) / of_thread + 31) / 32 * 32;
+  const int rows = p.each == 8 ? kGradRows : 1;
+  p.bytes = kGradSlots * rows * (a.dsum ? 3 : 2) * p.threads * p.each * a.size;
+  int per_sm = p.threads > kGradNarrow ? 1 : 2 * (kGradNarrow / p.threads);
+  if (per_sm > kSharedOfSm / (p.bytes + 2048)) per_sm = kSharedOfSm / (p.bytes + 2048);
+  const int batch = rows * (p.warp ? kGradWalks : 1);
+  const long long batches = (a.rows + batch - 1) / batch, most = (long long)per_sm * a.sms;
+  p.parts = batches < most ? batches : most;
   return p;
 }
 
+template <typename T, bool WARP, int R, int Q, int MAX, int CTAS> cudaError_t start_grad(const LayerNormGradArgs& a, const GradPlan& p, cudaStream_t s) {
+  const auto kernel = layer_norm_grad_kernel<T, WARP, R, Q, MAX, CTAS>;
+  if (p.bytes > 24 * 1024) {                                  // with the static arrays more than the 48 KB that need no asking
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.bytes);
+    if (e != cudaSuccess) return e;
+  }
+  return launch(kernel, dim3((unsigned)p.parts), dim3(p.threads), p.bytes, s, a);
+}
+
 template <typename T> cudaError_t run_grad(const LayerNormGradArgs& a, cudaStream_t s) {
-  const GradPlan p = grad_plan<T>(a);
+  constexpr int kPiece = 16 / sizeof(T);
+  const GradPlan p = grad_plan(a);
   const bool sums = a.dw || a.db;
   cudaError_t e = cudaSuccess;
   if (p.apart) {
     if (sums) e = launch(layer_norm_columns_kernel<T>, dim3((unsigned)((a.hidden + kColumns - 1) / kColumns), (unsigned)p.parts), dim3(kColumns, kWalks), 0, s, a);
     if (e == cudaSuccess && a.dx) e = launch(layer_norm_rows_kernel<T>, dim3((unsigned)a.rows), dim3(kRowThreads), 0, s, a);
   } else if (p.warp) {
-    e = launch(layer_norm_grad_kernel<T, true, 256>, dim3((unsigned)p.parts), dim3(p.threads), 0, s, a);
-  } else if (p.threads <= 256) {
-    e = launch(layer_norm_grad_kernel<T, false, 256>, dim3((unsigned)p.parts), dim3(p.threads), 0, s, a);
+    e = start_grad<T, true, kGradRows, 8 / kPiece, kGradNarrow, 2>(a, p, s);
+  } else if (p.each == 8) {
+    e = start_grad<T, false, kGradRows, 8 / kPiece, kGradNarrow, 2>(a, p, s);
+  } else if (p.threads <= kGradNarrow) {
+    e = start_grad<T, false, 1, 16 / kPiece, kGradNarrow, 2>(a, p, s);
   } else {
-    e = launch(layer_norm_grad_kernel<T, false, 1024>, dim3((unsigned)p.parts), dim3(p.threads), 0, s, a);
+    e = start_grad<T, false, 1, 16 / kPiece, kGradWide, 1>(a, p, s);
   }
   if (e != cudaSuccess || !sums) return e;
-  return launch(layer_norm_join_kernel, dim3((unsigned)((2ll * a.hidden + 31) / 32)), dim3(256), 0, s, (const float*)a.partials, (int)p.parts, a.hidden, a.dw, a.db);
+  return launch(layer_norm_join_kernel, dim3((unsigned)((2ll * padded_hidden(a.hidden) + 31) / 32)), dim3(32 * kJoinWarps), 0, s, (const float*)a.partials, (int)p.parts, a.hidden, a.dw, a.db);
 }
 
 }  // namespace
@@ -495,11 +630,7 @@ cudaError_t launch_layer_norm(int dtype, const LayerNormArgs& a, cudaStream_t s)
   if (dtype == AQ_BF16) return run_forward<__nv_bfloat16>(a, s);
   return run_forward<float>(a, s);
 }
-long long layer_norm_grad_parts(int dtype, const LayerNormGradArgs& a) {
-  if (dtype == AQ_FP16) return grad_plan<__half>(a).parts;
-  if (dtype == AQ_BF16) return grad_plan<__nv_bfloat16>(a).parts;
-  return grad_plan<float>(a).parts;
-}
+long long layer_norm_grad_bytes(const LayerNormGradArgs& a) { return grad_plan(a).parts * 2 * padded_hidden(a.hidden) * (long long)sizeof(float); }
 cudaError_t launch_layer_norm_grad(int dtype, const LayerNormGradArgs& a, cudaStream_t s) {
   if (dtype == AQ_FP16) return run_grad<__half>(a, s);
   if (dtype == AQ_BF16) return run_grad<__nv_bfloat16>(a, s);

@@ -90,7 +90,7 @@ struct LayerNormArgs {
   void* sum; long long lds;               // may be null
   void* y; long long ldy;
   float *mean, *rstd;                     // may be null
-  bool whole;                             // rows are whole 16-byte pieces, all on 16-byte boundaries
+  bool whole;                             // rows, w and b begin on 16-byte boundaries
   int sms;
 };
 
@@ -103,9 +103,9 @@ struct LayerNormGradArgs {
   long long rows; int hidden;
   void* dx; long long lddx;               // may be null
   float *dw, *db;                         // may be null
-  float* partials;                        // workspace, layer_norm_grad_parts(a) x [2][hidden]: sums of dw, db
+  float* partials;                        // workspace, layer_norm_grad_bytes of it: sums of dw and db of each CTA
   bool whole;
-  int sms;
+  int size, sms;                          // size: of an element
 };
 
 // A tensor of a step, or a part of a long one, as the kernels read it.
@@ -155,8 +155,8 @@ long long ffn_grad_partial_bytes(const FfnGradArgs& a);
 cudaError_t launch_ffn(int dtype, const FfnArgs& a, cudaStream_t s);
 cudaError_t launch_ffn_grad(int dtype, const FfnGradArgs& a, cudaStream_t s);
 cudaError_t launch_layer_norm(int dtype, const LayerNormArgs& a, cudaStream_t s);
-// sums of dw and db that a call keeps in `partials`; goes by the sizes, `whole`, sms and the type
-long long layer_norm_grad_parts(int dtype, const LayerNormGradArgs& a);
+// bytes of `partials` that a call with dw or db needs; goes by the sizes, dsum, `whole` and sms
+long long layer_norm_grad_bytes(const LayerNormGradArgs& a);
 cudaError_t launch_layer_norm_grad(int dtype, const LayerNormGradArgs& a, cudaStream_t s);
 // `parts`: 0..kAdamTable tensors, none of them empty; they travel in the launch's arguments
 cudaError_t launch_adamw(int dtype, int state_bits, const AdamPart* parts, int n, const AdamScalars& a, int sms, cudaStream_t s);

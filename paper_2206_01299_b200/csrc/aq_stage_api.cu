@@ -146,7 +146,7 @@ aq::QkArgs qk_args(aq_stage* st, const aq_qk_shape* sh, int64_t rows, const void
 
 unsigned size_of(int dtype) { return dtype == AQ_FP32 ? 4 : 2; }
 
-// A T[..][hidden] operand of the layer norm: element alignment and any stride do; `whole` stays true for 16-byte pieces.
+// A T[..][hidden] operand of the layer norm: element alignment and any stride do; `whole` stays true for rows on 16-byte boundaries.
 int check_norm_rows(aq_stage* st, const char* who, const char* name, const void* p, int64_t ld, int64_t hidden, bool* whole) {
   const unsigned size = size_of(st->dtype);
   if (!p || misaligned(p, size)) return fail(st, AQ_EINVAL, "%s: %s is null or misaligned", who, name);
@@ -160,7 +160,7 @@ int check_norm(aq_stage* st, const char* who, int64_t rows, int hidden, const vo
   if (hidden < 1 || hidden > (1 << 20)) return fail(st, AQ_EINVAL, "%s: hidden must be in 1..2^20 (got %d)", who, hidden);
   const unsigned size = size_of(st->dtype);
   if (misaligned(w, size) || misaligned(b, size)) return fail(st, AQ_EINVAL, "%s: w or b is misaligned", who);
-  *whole = hidden % (16 / size) == 0 && !misaligned(w, 16) && !misaligned(b, 16);
+  *whole = !misaligned(w, 16) && !misaligned(b, 16);
   return AQ_OK;
 }
 
@@ -513,8 +513,8 @@ int aq_layer_norm_grad(aq_stage* st, const void* dy, int64_t lddy, const void* d
   AQ_TRY(check_in_place(st, who, dx, lddx, s, lds));
   if (!mean || !rstd || misaligned(mean, 4) || misaligned(rstd, 4)) return fail(st, AQ_EINVAL, "%s: mean or rstd is null or misaligned", who);
   if (!dx && !dw && !db) return AQ_OK;
-  aq::LayerNormGradArgs a{dy, lddy, dsum, ldds, s, lds, w, mean, rstd, rows, hidden, dx, lddx, dw, db, nullptr, whole, st->sms};
-  if (dw || db) AQ_TRY(ensure_work(st, (size_t)aq::layer_norm_grad_parts(st->dtype, a) * 2 * (size_t)hidden * sizeof(float)));
+  aq::LayerNormGradArgs a{dy, lddy, dsum, ldds, s, lds, w, mean, rstd, rows, hidden, dx, lddx, dw, db, nullptr, whole, (int)size_of(st->dtype), st->sms};
+  if (dw || db) AQ_TRY(ensure_work(st, (size_t)aq::layer_norm_grad_bytes(a)));
   a.partials = static_cast<float*>(st->work);
   return launched(st, aq::launch_layer_norm_grad(st->dtype, a, st->stream), who);
 }

@@ -63,6 +63,41 @@ __device__ bool warp_wait(int lane, uint32_t bar, uint32_t parity, uint32_t* sta
   return __shfl_sync(0xffffffffu, ok, 0) != 0;
 }
 
+// asynchronous copies to shared memory, in groups that the thread waits for later; `bytes` short of 16 are read, the rest is filled with zeros
+__device__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+__device__ void copy8(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory"); }
+__device__ void copy4(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory"); }
+__device__ void copy16(uint32_t to, const void* from, uint32_t bytes) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory"); }
+__device__ void copy4(uint32_t to, const void* from, uint32_t bytes) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory"); }
+__device__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ uint4 shared16(uint32_t from) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(from) : "memory");
+  return v;
+}
+
+// arithmetic on pairs: one instruction for two, each rounded as a single one is (a product and a sum may be fused all the same)
+
+__device__ float2 both(float x) { return make_float2(x, x); }
+__device__ float2 mul2(float2 a, float2 b) {
+  float2 c;
+  asm("{.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmul.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;}" : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
+}
+__device__ float2 fma2(float2 a, float2 b, float2 d) {
+  float2 c;
+  asm("{.reg .b64 x, y, z, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 w, {%6, %7};\nfma.rn.f32x2 z, x, y, w;\nmov.b64 {%0, %1}, z;}"
+      : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(d.x), "f"(d.y));
+  return c;
+}
+__device__ float2 add2(float2 a, float2 b) {
+  float2 c;
+  asm("{.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nadd.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;}" : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
+}
+
 // A launch that may be placed while the stream's previous kernel drains (the kernels wait for its results themselves).
 template <typename... Params, typename... Args>
 cudaError_t launch(void (*kernel)(Params...), dim3 ctas, dim3 threads, size_t shared, cudaStream_t s, Args... args) {
