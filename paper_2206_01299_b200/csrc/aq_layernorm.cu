@@ -62,16 +62,16 @@ template <typename T> struct Piece<T, false> {
   static __device__ Raw close(const float* f) { return Scalar<T>::close(f[0]); }
 };
 
-// Pieces of which a row has `left` elements only: zeros behind them, and only they are stored.
-template <typename Pc, typename T> __device__ typename Pc::Raw load_piece(const T* p, int left) {
-  if (left >= Pc::N) return Pc::load(p);
+// A piece of which a row has the elements [lo, hi) only: zeros around them, and only they are stored.
+template <typename Pc, typename T> __device__ typename Pc::Raw load_piece(const T* p, int lo, int hi) {
+  if (lo <= 0 && hi >= Pc::N) return Pc::load(p);
   float f[Pc::N];
 #pragma unroll
-  for (int j = 0; j < Pc::N; ++j) f[j] = j < left ? Scalar<T>::open(p[j]) : 0.0f;
+  for (int j = 0; j < Pc::N; ++j) f[j] = j >= lo && j < hi ? Scalar<T>::open(p[j]) : 0.0f;
   return Pc::close(f);
 }
-template <typename Pc, typename T> __device__ void store_piece(T* p, typename Pc::Raw v, int left) {
-  if (left >= Pc::N) {
+template <typename Pc, typename T> __device__ void store_piece(T* p, typename Pc::Raw v, int lo, int hi) {
+  if (lo <= 0 && hi >= Pc::N) {
     Pc::store(p, v);
     return;
   }
@@ -79,7 +79,33 @@ template <typename Pc, typename T> __device__ void store_piece(T* p, typename Pc
   Pc::open(v, f);
 #pragma unroll
   for (int j = 0; j < Pc::N; ++j)
-    if (j < left) p[j] = Scalar<T>::close(f[j]);
+    if (j >= lo && j < hi) p[j] = Scalar<T>::close(f[j]);
+}
+// N values at p, which are a piece of [0, hidden) that begins at `at`: where that is off the 16-byte boundaries, out of the two pieces that hold them.
+template <typename Pc, typename T> __device__ void load_weights(const T* w, int at, int hidden, float* f) {
+  constexpr int N = Pc::N;
+  if (N == 1 || at < N || at + 2 * N > hidden) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = at + j >= 0 && at + j < hidden ? Scalar<T>::open(w[at + j]) : 0.0f;
+    return;
+  }
+  const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(w + at) & 15);   // the same for a whole warp
+  const uint4* const from = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(w + at) - off);
+  const uint4 a = __ldg(from), b = off ? __ldg(from + 1) : a;
+  uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  if (off & 8) {
+#pragma unroll
+    for (int i = 0; i < 6; ++i) v[i] = v[i + 2];
+  }
+  if (off & 4) {
+#pragma unroll
+    for (int i = 0; i < 5; ++i) v[i] = v[i + 1];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(v[i], v[i + 1], (off & 3) * 8);
+  typename Pc::Raw raw;
+  memcpy(&raw, v, sizeof raw);
+  Pc::open(raw, f);
 }
 
 __device__ float warp_sum(float x) {
@@ -102,8 +128,9 @@ template <int W> __device__ float cta_sum(float x, float* shared) {
 
 // ---- forward -------------------------------------------------------------------------------------------------
 
-// W warps to a row, P pieces to a lane; four rows to a CTA where a row is a warp's.
-template <typename T, bool WHOLE, int W, int P>
+// W warps to a row, P pieces to a lane; four rows to a CTA where a row is a warp's.  EDGE: rows may begin and end inside a piece, all operands'
+// at the same place (a row's first piece then begins before it), and w and b are off the boundaries.
+template <typename T, bool WHOLE, bool EDGE, int W, int P>
 __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) layer_norm_kernel(const LayerNormArgs a) {
   using Pc = Piece<T, WHOLE>;
   constexpr int N = Pc::N, kStep = 32 * W * N;
@@ -114,34 +141,38 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) layer_norm_kernel(const
   wait_for_previous();
   if (W == 1 && row >= a.rows) return;
   const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
-  const int left = a.hidden - lane * N;                       // elements of the row from the lane's first piece on; its pieces are kStep apart
+  const int first = lane * N - (EDGE ? (int)(reinterpret_cast<uintptr_t>(x) / sizeof(T) % N) : 0);   // of the lane's first piece; the others are kStep apart
+  auto at = [&](int i) { return first + i * kStep; };
+  auto lo = [&](int i) { return EDGE ? -at(i) : 0; };         // of a piece's elements those in the row
+  auto hi = [&](int i) { return EDGE ? a.hidden - at(i) : N; };
+  auto has = [&](int i) { return at(i) < a.hidden; };
   typename Pc::Raw v[P];
 #pragma unroll
   for (int i = 0; i < P; ++i)
-    if (left > i * kStep) v[i] = load_piece<Pc>(x + lane * N + i * kStep, left - i * kStep);
+    if (has(i)) v[i] = load_piece<Pc>(x + at(i), lo(i), hi(i));
   if (a.residual) {
     const T* const r = static_cast<const T*>(a.residual) + row * a.ldr;
     T* const sum = a.sum ? static_cast<T*>(a.sum) + row * a.lds : nullptr;
     typename Pc::Raw o[P];
 #pragma unroll
     for (int i = 0; i < P; ++i)
-      if (left > i * kStep) o[i] = load_piece<Pc>(r + lane * N + i * kStep, left - i * kStep);
+      if (has(i)) o[i] = load_piece<Pc>(r + at(i), lo(i), hi(i));
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      if (left <= i * kStep) continue;
+      if (!has(i)) continue;
       float f[N], e[N];
       Pc::open(v[i], f);
       Pc::open(o[i], e);
 #pragma unroll
       for (int j = 0; j < N; ++j) f[j] += e[j];
       v[i] = Pc::close(f);
-      if (sum) store_piece<Pc>(sum + lane * N + i * kStep, v[i], left - i * kStep);
+      if (sum) store_piece<Pc>(sum + at(i), v[i], lo(i), hi(i));
     }
   }
   float total = 0.0f;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    if (left <= i * kStep) continue;
+    if (!has(i)) continue;
     float f[N];
     Pc::open(v[i], f);
 #pragma unroll
@@ -152,16 +183,16 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) layer_norm_kernel(const
   float squares = 0.0f;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    if (left <= i * kStep) continue;
+    if (!has(i)) continue;
     float f[N];
     Pc::open(v[i], f);
-    if (left - i * kStep >= N) {
+    if (!EDGE || (lo(i) <= 0 && hi(i) >= N)) {
 #pragma unroll
       for (int j = 0; j < N; ++j) squares = fmaf(f[j] - mean, f[j] - mean, squares);
     } else {
 #pragma unroll
       for (int j = 0; j < N; ++j)
-        if (j < left - i * kStep) squares = fmaf(f[j] - mean, f[j] - mean, squares);
+        if (j >= lo(i) && j < hi(i)) squares = fmaf(f[j] - mean, f[j] - mean, squares);
     }
   }
   const float rstd = 1.0f / sqrtf(fmaf(cta_sum<W>(squares, shared[1]), inverse, a.eps));
@@ -170,27 +201,32 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) layer_norm_kernel(const
     if (a.rstd) a.rstd[row] = rstd;
   }
   T* const y = static_cast<T*>(a.y) + row * a.ldy;
+  const T* const wt = static_cast<const T*>(a.w);
+  const T* const bs = static_cast<const T*>(a.b);
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    if (left <= i * kStep) continue;
-    const int at = lane * N + i * kStep;
+    if (!has(i)) continue;
     float f[N], w[N], b[N];
     Pc::open(v[i], f);
-    if (a.w) {
-      Pc::open(load_piece<Pc>(static_cast<const T*>(a.w) + at, left - i * kStep), w);
-    } else {
+    if (!wt) {
 #pragma unroll
       for (int j = 0; j < N; ++j) w[j] = 1.0f;
-    }
-    if (a.b) {
-      Pc::open(load_piece<Pc>(static_cast<const T*>(a.b) + at, left - i * kStep), b);
+    } else if (EDGE) {
+      load_weights<Pc>(wt, at(i), a.hidden, w);
     } else {
+      Pc::open(Pc::load(wt + at(i)), w);
+    }
+    if (!bs) {
 #pragma unroll
       for (int j = 0; j < N; ++j) b[j] = 0.0f;
+    } else if (EDGE) {
+      load_weights<Pc>(bs, at(i), a.hidden, b);
+    } else {
+      Pc::open(Pc::load(bs + at(i)), b);
     }
 #pragma unroll
     for (int j = 0; j < N; ++j) f[j] = fmaf((f[j] - mean) * rstd, w[j], b[j]);
-    store_piece<Pc>(y + at, Pc::close(f), left - i * kStep);
+    store_piece<Pc>(y + at(i), Pc::close(f), lo(i), hi(i));
   }
 }
 
@@ -242,27 +278,35 @@ __global__ void __launch_bounds__(kLongThreads) layer_norm_long_kernel(const Lay
   }
 }
 
-template <typename T, bool WHOLE, int W, int P> cudaError_t run(const LayerNormArgs& a, cudaStream_t s) {
+template <typename T, bool WHOLE, bool EDGE, int W, int P> cudaError_t run(const LayerNormArgs& a, cudaStream_t s) {
   const unsigned ctas = (unsigned)(W == 1 ? (a.rows + 3) / 4 : a.rows);
-  return launch(layer_norm_kernel<T, WHOLE, W, P>, dim3(ctas), W == 1 ? 128 : 32 * W, 0, s, a);
+  return launch(layer_norm_kernel<T, WHOLE, EDGE, W, P>, dim3(ctas), dim3(W == 1 ? 128 : 32 * W), 0, s, a);
 }
-
+template <typename T> cudaError_t run_long(const LayerNormArgs& a, cudaStream_t s) {
+  return launch(layer_norm_long_kernel<T>, dim3((unsigned)a.rows), dim3(kLongThreads), 0, s, a);
+}
+// Pieces of 16 bytes; a shifted row may need one more.
+template <typename T, bool EDGE> cudaError_t run_pieces(const LayerNormArgs& a, cudaStream_t s) {
+  constexpr int N = Piece<T, true>::N;
+  const int pieces = (a.hidden + (EDGE ? N - 1 : 0) + N - 1) / N;
+  if (pieces <= 32) return run<T, true, EDGE, 1, 1>(a, s);
+  if (pieces <= 64) return run<T, true, EDGE, 1, 2>(a, s);
+  if (pieces <= 128) return run<T, true, EDGE, 1, 4>(a, s);
+  if (pieces <= 256) return run<T, true, EDGE, 1, 8>(a, s);
+  if (pieces <= 512) return run<T, true, EDGE, 4, 4>(a, s);
+  if (pieces <= 1024) return run<T, true, EDGE, 8, 4>(a, s);
+  if (pieces <= 2048) return run<T, true, EDGE, 16, 4>(a, s);
+  if (pieces <= 4096) return run<T, true, EDGE, 16, 8>(a, s);
+  return run_long<T>(a, s);
+}
 template <typename T> cudaError_t run_forward(const LayerNormArgs& a, cudaStream_t s) {
-  if (a.whole) {
-    const int pieces = (a.hidden + Piece<T, true>::N - 1) / Piece<T, true>::N;
-    if (pieces <= 32) return run<T, true, 1, 1>(a, s);
-    if (pieces <= 64) return run<T, true, 1, 2>(a, s);
-    if (pieces <= 128) return run<T, true, 1, 4>(a, s);
-    if (pieces <= 256) return run<T, true, 1, 8>(a, s);
-    if (pieces <= 512) return run<T, true, 4, 4>(a, s);
-    if (pieces <= 1024) return run<T, true, 4, 8>(a, s);
-    if (pieces <= 4096) return run<T, true, 16, 8>(a, s);
-  } else {
-    if (a.hidden <= 256) return run<T, false, 1, 8>(a, s);
-    if (a.hidden <= 1024) return run<T, false, 1, 32>(a, s);
-    if (a.hidden <= 8192) return run<T, false, 8, 32>(a, s);
-  }
-  return launch(layer_norm_long_kernel<T>, dim3((unsigned)a.rows), kLongThreads, 0, s, a);
+  if (a.rows_at == kRowsWhole) return run_pieces<T, false>(a, s);
+  if (a.rows_at == kRowsAlike) return run_pieces<T, true>(a, s);
+  if (a.hidden <= 256) return run<T, false, true, 1, 8>(a, s);
+  if (a.hidden <= 1024) return run<T, false, true, 1, 32>(a, s);
+  if (a.hidden <= 2048) return run<T, false, true, 8, 8>(a, s);
+  if (a.hidden <= 8192) return run<T, false, true, 8, 32>(a, s);
+  return run_long<T>(a, s);
 }
 
 // ---- gradient ------------------------------------------------------------------------------------------------
@@ -320,8 +364,8 @@ constexpr int kGradSlots = 2;                 // batches of rows that a thread h
 
 // A CTA's threads have Q pieces of 16 bytes of a row each (WARP: a warp's lanes, and eight walks to a CTA) and take R rows at a time.  The next rows
 // are copied to shared memory meanwhile, each thread's elements by itself and for itself.  Elements behind a row's end are zeros there and add
-// nothing to any sum.
-template <typename T, bool WARP, int R, int Q, int MAX, int CTAS>
+// nothing to any sum.  EDGE: rows begin inside a piece, every `period`-th one at the same place; a CTA (a warp) takes rows that do.
+template <typename T, bool EDGE, bool WARP, int R, int Q, int MAX, int CTAS>
 __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerNormGradArgs a) {
   using Ps = Pairs<T>;
   constexpr int H = Ps::N, N = 2 * H, V = 2 * R;
@@ -336,40 +380,46 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
   next_may_launch();
   wait_for_previous();
   const int walks = WARP ? gridDim.x * kGradWalks : gridDim.x, walk = WARP ? blockIdx.x * kGradWalks + warp : blockIdx.x;
-  int column[Q], have[Q];                                      // of the thread's elements those in the row
+  // rows: `kind`, kind + period ... begin at the same place in their first piece; of those, every walk of the kind takes R at a time in turn
+  const int period = EDGE ? a.period : 1, kind = EDGE ? walk % period : 0, turn = EDGE ? walk / period : walk;
+  const int shift = EDGE ? (int)(kind * (a.lds % N) % N) : 0;
+  int column[Q], lo[Q], hi[Q];                                 // of the thread's elements those in the row
   float2 w[Q][H], dw[Q][H], db[Q][H];
 #pragma unroll
   for (int q = 0; q < Q; ++q) {
-    column[q] = (WARP ? lane + 32 * q : (int)(threadIdx.x + q * blockDim.x)) * N;
-    have[q] = min(max(a.hidden - column[q], 0), N);
+    column[q] = (WARP ? lane + 32 * q : (int)(threadIdx.x + q * blockDim.x)) * N - shift;
+    lo[q] = EDGE ? max(-column[q], 0) : 0;
+    hi[q] = min(max(a.hidden - column[q], 0), N);
 #pragma unroll
     for (int j = 0; j < H; ++j) w[q][j] = dw[q][j] = db[q][j] = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      if (j >= have[q]) break;
+      if (j < lo[q] || j >= hi[q]) continue;
       (j & 1 ? w[q][j / 2].y : w[q][j / 2].x) = a.w ? Scalar<T>::open(static_cast<const T*>(a.w)[column[q] + j]) : 1.0f;
     }
   }
   const float inverse = 1.0f / (float)a.hidden;
   // the next batch's rows: addresses move on by constants
-  const long long first = (long long)walk * R;
+  const long long first = kind + (long long)turn * R * period, kinds = (a.rows - kind + period - 1) / period;   // rows of the kind
   const T *s = static_cast<const T*>(a.s) + first * a.lds, *g = static_cast<const T*>(a.dy) + first * a.lddy;
   const T* k = skip ? static_cast<const T*>(a.dsum) + first * a.ldds : nullptr;
   T* o = a.dx ? static_cast<T*>(a.dx) + first * a.lddx : nullptr;
-  const float* stat = (lane & 1 ? a.rstd : a.mean) + first + (lane % V) / 2;
-  const int step = walks * R;
-  long long left = a.rows - first;                             // rows from the next batch to ask for on
+  const float* stat = (lane & 1 ? a.rstd : a.mean) + first + (lane % V) / 2 * period;
+  const int step = walks * R, each = walks / period * R;       // rows, and rows of the kind, from one batch to the next
+  long long left = kinds - (long long)turn * R;                // rows of the kind from the next batch to ask for on
+  int here = (int)min(max(left, 0ll), (long long)0x7fffffff);  // ... from the batch that is worked on
   auto ask = [&](int slot) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       if (i >= left) break;
+      const long long r = i * period;
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
-        const int bytes = have[q] * (int)sizeof(T), at = bytes ? column[q] : 0;   // a thread without elements reads nothing, from a valid address
+        const int bytes = hi[q] * (int)sizeof(T), at = bytes ? column[q] : 0;   // a thread without elements reads nothing, from a valid address
         const uint32_t to = mine + (slot * R + i) * row_bytes + q * part;
-        copy16(to, s + i * a.lds + at, bytes);
-        copy16(to + Q * part, g + i * a.lddy + at, bytes);
-        if (skip) copy16(to + 2 * Q * part, k + i * a.ldds + at, bytes);
+        copy16(to, s + r * a.lds + at, bytes);
+        copy16(to + Q * part, g + r * a.lddy + at, bytes);
+        if (skip) copy16(to + 2 * Q * part, k + r * a.ldds + at, bytes);
       }
     }
     if (lane < V && lane / 2 < left) copy4(shared_address(&stats[slot][warp][lane]), stat);   // mean and rstd of the rows, for the warp
@@ -377,13 +427,13 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
     g += step * a.lddy;
     if (skip) k += step * a.ldds;
     stat += step;
-    left -= step;
+    left -= each;
   };
   if (left > 0) ask(0);
   copies_end();
   int slot = 0;
 #pragma unroll 1
-  for (int here = (int)min(a.rows - first, (long long)0x7fffffff); here > 0; here -= step, slot ^= 1) {   // rows from this batch on
+  for (; here > 0; here -= each, slot ^= 1) {
     __syncwarp();                                              // the warp has read the other slot's statistics
     if (left > 0) ask(slot ^ 1);
     copies_end();
@@ -403,8 +453,14 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
         take(i, 0, q, n[i][q]);
         take(i, 1, q, y[i][q]);
 #pragma unroll
+        for (int j = 0; j < H; ++j) n[i][q][j] = mul2(add2(n[i][q][j], both(-mean)), both(rstd));
+        if (EDGE && lo[q]) {                                   // what the row before left there
+#pragma unroll
+          for (int j = 0; j < N; ++j)
+            if (j < lo[q]) (j & 1 ? n[i][q][j / 2].y : n[i][q][j / 2].x) = (j & 1 ? y[i][q][j / 2].y : y[i][q][j / 2].x) = 0.0f;
+        }
+#pragma unroll
         for (int j = 0; j < H; ++j) {
-          n[i][q][j] = mul2(add2(n[i][q][j], both(-mean)), both(rstd));
           dw[q][j] = fma2(y[i][q][j], n[i][q][j], dw[q][j]);
           db[q][j] = add2(db[q][j], y[i][q][j]);
           y[i][q][j] = mul2(y[i][q][j], w[q][j]);
@@ -436,7 +492,7 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
       const float rstd = stats[slot][warp][2 * i + 1];
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
-        if (!have[q]) continue;
+        if (hi[q] <= lo[q]) continue;
         float2 f[H];
         if (skip) take(i, 2, q, f);
 #pragma unroll
@@ -444,13 +500,13 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
           const float2 d = add2(fma2(n[i][q][j], both(-sum[2 * i + 1]), y[i][q][j]), both(-sum[2 * i]));
           f[j] = skip ? fma2(d, both(rstd), f[j]) : mul2(d, both(rstd));
         }
-        T* const to = o + i * a.lddx + column[q];
-        if (have[q] == N) {
+        T* const to = o + (long long)(i * period) * a.lddx + column[q];
+        if (hi[q] - lo[q] == N) {
           *reinterpret_cast<uint4*>(to) = Ps::close(f);
         } else {
 #pragma unroll
           for (int j = 0; j < N; ++j)
-            if (j < have[q]) to[j] = Scalar<T>::close(j & 1 ? f[j / 2].y : f[j / 2].x);
+            if (j >= lo[q] && j < hi[q]) to[j] = Scalar<T>::close(j & 1 ? f[j / 2].y : f[j / 2].x);
         }
       }
     }
@@ -463,9 +519,10 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
 #pragma unroll
-      for (int j = 0; j < H; ++j) {
-        reinterpret_cast<float2*>(&sums[0][warp][column[q]])[j] = dw[q][j];
-        reinterpret_cast<float2*>(&sums[WARP ? 1 : 0][warp][column[q]])[j] = db[q][j];
+      for (int j = 0; j < N; ++j) {
+        if (j < lo[q] || j >= hi[q]) continue;
+        sums[0][warp][column[q] + j] = j & 1 ? dw[q][j / 2].y : dw[q][j / 2].x;
+        sums[WARP ? 1 : 0][warp][column[q] + j] = j & 1 ? db[q][j / 2].y : db[q][j / 2].x;
       }
     }
     __syncthreads();
@@ -476,10 +533,24 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
       for (int i = 0; i < (WARP ? kGradWalks : 1); ++i) s += sums[WARP ? t : 0][i][j];
       out[e] = s;
     }
+  } else if (EDGE) {                                           // by way of the ring, which holds two sums per column and more
+    __syncthreads();
+    float* const f = reinterpret_cast<float*>(ring);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        if (j < lo[q] || j >= hi[q]) continue;
+        f[column[q] + j] = j & 1 ? dw[q][j / 2].y : dw[q][j / 2].x;
+        f[padded + column[q] + j] = j & 1 ? db[q][j / 2].y : db[q][j / 2].x;
+      }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < padded / 2; e += blockDim.x) reinterpret_cast<float4*>(out)[e] = reinterpret_cast<const float4*>(f)[e];
   } else {
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      if (!have[q]) continue;
+      if (!hi[q]) continue;
       store_sums(out + column[q], dw[q], H);
       store_sums(out + padded + column[q], db[q], H);
     }
@@ -569,19 +640,24 @@ __global__ void __launch_bounds__(32 * kJoinWarps) layer_norm_join_kernel(const 
 constexpr int kGradNarrow = 256, kGradWide = 512;             // threads of the CTAs that the registers are cut for
 constexpr int kGradRows = 2;                                  // rows at a time, where threads have eight elements
 constexpr int kSharedOfSm = 227 * 1024;
-struct GradPlan { int threads, each; bool warp, apart; int bytes; long long parts; };
+struct GradPlan { int threads, each, period; bool warp, apart, edge; int bytes; long long parts; };
 GradPlan grad_plan(const LayerNormGradArgs& a) {
   GradPlan p{};
-  p.each = a.hidden <= 8 * kGradNarrow ? 8 : 16;
-  p.apart = !a.whole || a.hidden > 16 * kGradWide;
+  const int piece = 16 / a.size;
+  p.edge = a.rows_at == kRowsAlike;
+  const int span = a.hidden + (p.edge ? piece - 1 : 0);       // a shifted row's first piece begins before it
+  p.period = 1;
+  for (long long ld = a.lds; p.edge && ld * p.period % piece;) ++p.period;   // at most eight
+  p.each = span <= 8 * kGradNarrow ? 8 : 16;
+  p.apart = a.rows_at == kRowsAny || span > 16 * kGradWide;
   if (p.apart) {
     const long long strips = (a.hidden + kColumns - 1) / kColumns, walks = (a.rows + kWalks - 1) / kWalks;
     const long long most = (8ll * a.sms + strips - 1) / strips;
     p.parts = walks < most ? walks : most;
     return p;
   }
-  p.warp = a.hidden <= 8 * 32;
-  const int piece = 16 / a.size, pieces = (a.hidden + piece - 1) / piece, of_thread = p.each / piece;
+  p.warp = span <= 8 * 32;
+  const int pieces = (span + piece - 1) / piece, of_thread = p.each / piece;
   p.threads = p.warp ? 32 * kGradWalks : ((pieces + of_thread - 1) / of_thread + 31) / 32 * 32;
   const int rows = p.each == 8 ? kGradRows : 1;
   p.bytes = kGradSlots * rows * (a.dsum ? 3 : 2) * p.threads * p.each * a.size;
@@ -590,11 +666,13 @@ GradPlan grad_plan(const LayerNormGradArgs& a) {
   const int batch = rows * (p.warp ? kGradWalks : 1);
   const long long batches = (a.rows + batch - 1) / batch, most = (long long)per_sm * a.sms;
   p.parts = batches < most ? batches : most;
+  if (!p.warp) p.parts = (p.parts + p.period - 1) / p.period * p.period;   // as many walks of every kind of rows
   return p;
 }
 
-template <typename T, bool WARP, int R, int Q, int MAX, int CTAS> cudaError_t start_grad(const LayerNormGradArgs& a, const GradPlan& p, cudaStream_t s) {
-  const auto kernel = layer_norm_grad_kernel<T, WARP, R, Q, MAX, CTAS>;
+template <typename T, bool EDGE, bool WARP, int R, int Q, int MAX, int CTAS> cudaError_t start_grad(LayerNormGradArgs a, const GradPlan& p, cudaStream_t s) {
+  a.period = p.period;
+  const auto kernel = layer_norm_grad_kernel<T, EDGE, WARP, R, Q, MAX, CTAS>;
   if (p.bytes > 24 * 1024) {                                  // with the static arrays more than the 48 KB that need no asking
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.bytes);
     if (e != cudaSuccess) return e;
@@ -602,22 +680,23 @@ template <typename T, bool WARP, int R, int Q, int MAX, int CTAS> cudaError_t st
   return launch(kernel, dim3((unsigned)p.parts), dim3(p.threads), p.bytes, s, a);
 }
 
-template <typename T> cudaError_t run_grad(const LayerNormGradArgs& a, cudaStream_t s) {
+template <typename T, bool EDGE> cudaError_t run_walks(const LayerNormGradArgs& a, const GradPlan& p, cudaStream_t s) {
   constexpr int kPiece = 16 / sizeof(T);
+  if (p.warp) return start_grad<T, EDGE, true, kGradRows, 8 / kPiece, kGradNarrow, 2>(a, p, s);
+  if (p.each == 8) return start_grad<T, EDGE, false, kGradRows, 8 / kPiece, kGradNarrow, 2>(a, p, s);
+  if (p.threads <= kGradNarrow) return start_grad<T, EDGE, false, 1, 16 / kPiece, kGradNarrow, 2>(a, p, s);
+  return start_grad<T, EDGE, false, 1, 16 / kPiece, kGradWide, 1>(a, p, s);
+}
+
+template <typename T> cudaError_t run_grad(const LayerNormGradArgs& a, cudaStream_t s) {
   const GradPlan p = grad_plan(a);
   const bool sums = a.dw || a.db;
   cudaError_t e = cudaSuccess;
   if (p.apart) {
     if (sums) e = launch(layer_norm_columns_kernel<T>, dim3((unsigned)((a.hidden + kColumns - 1) / kColumns), (unsigned)p.parts), dim3(kColumns, kWalks), 0, s, a);
     if (e == cudaSuccess && a.dx) e = launch(layer_norm_rows_kernel<T>, dim3((unsigned)a.rows), dim3(kRowThreads), 0, s, a);
-  } else if (p.warp) {
-    e = start_grad<T, true, kGradRows, 8 / kPiece, kGradNarrow, 2>(a, p, s);
-  } else if (p.each == 8) {
-    e = start_grad<T, false, kGradRows, 8 / kPiece, kGradNarrow, 2>(a, p, s);
-  } else if (p.threads <= kGradNarrow) {
-    e = start_grad<T, false, 1, 16 / kPiece, kGradNarrow, 2>(a, p, s);
   } else {
-    e = start_grad<T, false, 1, 16 / kPiece, kGradWide, 1>(a, p, s);
+    e = p.edge ? run_walks<T, true>(a, p, s) : run_walks<T, false>(a, p, s);
   }
   if (e != cudaSuccess || !sums) return e;
   return launch(layer_norm_join_kernel, dim3((unsigned)((2ll * padded_hidden(a.hidden) + 31) / 32)), dim3(32 * kJoinWarps), 0, s, (const float*)a.partials, (int)p.parts, a.hidden, a.dw, a.db);

@@ -81,6 +81,10 @@ struct FfnGradArgs {
   int sms, pairs;
 };
 
+// Where the rows of a layer norm's operands begin: all on 16-byte boundaries (forward: w and b too, and rows are whole pieces of 16
+// bytes), at the same distance from one in all operands (gradient: the first rows on boundaries), or anywhere.
+enum { kRowsWhole = 0, kRowsAlike = 1, kRowsAny = 2 };
+
 struct LayerNormArgs {
   const void* x; long long ldx;
   const void* residual; long long ldr;    // may be null
@@ -90,7 +94,7 @@ struct LayerNormArgs {
   void* sum; long long lds;               // may be null
   void* y; long long ldy;
   float *mean, *rstd;                     // may be null
-  bool whole;                             // rows, w and b begin on 16-byte boundaries
+  int rows_at;                            // where rows begin
   int sms;
 };
 
@@ -104,7 +108,7 @@ struct LayerNormGradArgs {
   void* dx; long long lddx;               // may be null
   float *dw, *db;                         // may be null
   float* partials;                        // workspace, layer_norm_grad_bytes of it: sums of dw and db of each CTA
-  bool whole;
+  int rows_at, period;                    // period: rows from one to the next that begins at the same place in a 16-byte piece; set by the launch
   int size, sms;                          // size: of an element
 };
 
@@ -155,7 +159,7 @@ long long ffn_grad_partial_bytes(const FfnGradArgs& a);
 cudaError_t launch_ffn(int dtype, const FfnArgs& a, cudaStream_t s);
 cudaError_t launch_ffn_grad(int dtype, const FfnGradArgs& a, cudaStream_t s);
 cudaError_t launch_layer_norm(int dtype, const LayerNormArgs& a, cudaStream_t s);
-// bytes of `partials` that a call with dw or db needs; goes by the sizes, dsum, `whole` and sms
+// bytes of `partials` that a call with dw or db needs; goes by the sizes, dsum, rows_at and sms
 long long layer_norm_grad_bytes(const LayerNormGradArgs& a);
 cudaError_t launch_layer_norm_grad(int dtype, const LayerNormGradArgs& a, cudaStream_t s);
 // `parts`: 0..kAdamTable tensors, none of them empty; they travel in the launch's arguments

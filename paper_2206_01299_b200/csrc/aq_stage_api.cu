@@ -146,21 +146,32 @@ aq::QkArgs qk_args(aq_stage* st, const aq_qk_shape* sh, int64_t rows, const void
 
 unsigned size_of(int dtype) { return dtype == AQ_FP32 ? 4 : 2; }
 
-// A T[..][hidden] operand of the layer norm: element alignment and any stride do; `whole` stays true for rows on 16-byte boundaries.
-int check_norm_rows(aq_stage* st, const char* who, const char* name, const void* p, int64_t ld, int64_t hidden, bool* whole) {
+// How the rows of a layer norm's operands lie to one another and to 16-byte boundaries.
+struct NormRows {
+  bool some = false, begin = true, whole = true, alike = true;   // begin: the first rows on boundaries; whole: all
+  int64_t place = 0, stride = 0;                                 // in elements, mod a piece
+};
+
+// A T[..][hidden] operand of the layer norm: element alignment and any stride do.
+int check_norm_rows(aq_stage* st, const char* who, const char* name, const void* p, int64_t ld, int64_t hidden, NormRows* r) {
   const unsigned size = size_of(st->dtype);
   if (!p || misaligned(p, size)) return fail(st, AQ_EINVAL, "%s: %s is null or misaligned", who, name);
   if (ld < hidden || ld > (1ll << 38)) return fail(st, AQ_EINVAL, "%s: the row stride of %s must be at least %lld", who, name, (long long)hidden);
-  if (misaligned(p, 16) || ld % (16 / size)) *whole = false;
+  const int64_t piece = 16 / size, place = (int64_t)(reinterpret_cast<uintptr_t>(p) / size % piece), stride = ld % piece;
+  if (r->some && (place != r->place || stride != r->stride)) r->alike = false;
+  if (place) r->begin = false;
+  if (place || stride) r->whole = false;
+  r->some = true;
+  r->place = place;
+  r->stride = stride;
   return AQ_OK;
 }
 
-int check_norm(aq_stage* st, const char* who, int64_t rows, int hidden, const void* w, const void* b, bool* whole) {
+int check_norm(aq_stage* st, const char* who, int64_t rows, int hidden, const void* w, const void* b) {
   if (rows < 0 || rows > 0x7fffffffll) return fail(st, AQ_EINVAL, "%s: rows must be in 0..2^31-1", who);
   if (hidden < 1 || hidden > (1 << 20)) return fail(st, AQ_EINVAL, "%s: hidden must be in 1..2^20 (got %d)", who, hidden);
   const unsigned size = size_of(st->dtype);
   if (misaligned(w, size) || misaligned(b, size)) return fail(st, AQ_EINVAL, "%s: w or b is misaligned", who);
-  *whole = !misaligned(w, 16) && !misaligned(b, 16);
   return AQ_OK;
 }
 
@@ -468,23 +479,25 @@ int aq_layer_norm(aq_stage* st, const void* x, int64_t ldx, const void* residual
                   int64_t rows, int hidden, void* sum, int64_t lds, void* y, int64_t ldy, float* mean, float* rstd) {
   if (!st) return AQ_EINVAL;
   const char* who = "aq_layer_norm";
-  bool whole;
-  AQ_TRY(check_norm(st, who, rows, hidden, w, b, &whole));
+  NormRows r;
+  AQ_TRY(check_norm(st, who, rows, hidden, w, b));
   if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(st, AQ_EINVAL, "%s: eps must be finite and not negative", who);
   if (misaligned(mean, 4) || misaligned(rstd, 4)) return fail(st, AQ_EINVAL, "%s: mean or rstd is misaligned", who);
   if (sum && !residual) return fail(st, AQ_EINVAL, "%s: sum without residual", who);
   if (rows == 0) return AQ_OK;
-  AQ_TRY(check_norm_rows(st, who, "x", x, ldx, hidden, &whole));
-  AQ_TRY(check_norm_rows(st, who, "y", y, ldy, hidden, &whole));
-  if (residual) AQ_TRY(check_norm_rows(st, who, "residual", residual, ldr, hidden, &whole));
-  if (sum) AQ_TRY(check_norm_rows(st, who, "sum", sum, lds, hidden, &whole));
+  AQ_TRY(check_norm_rows(st, who, "x", x, ldx, hidden, &r));
+  AQ_TRY(check_norm_rows(st, who, "y", y, ldy, hidden, &r));
+  if (residual) AQ_TRY(check_norm_rows(st, who, "residual", residual, ldr, hidden, &r));
+  if (sum) AQ_TRY(check_norm_rows(st, who, "sum", sum, lds, hidden, &r));
   if (sum && sum == y) return fail(st, AQ_EINVAL, "%s: sum and y are two outputs", who);
   AQ_TRY(check_in_place(st, who, y, ldy, x, ldx));
   AQ_TRY(check_in_place(st, who, y, ldy, residual, ldr));
   AQ_TRY(check_in_place(st, who, sum, lds, x, ldx));
   AQ_TRY(check_in_place(st, who, sum, lds, residual, ldr));
   DeviceGuard guard(st->device);
-  const aq::LayerNormArgs a{x, ldx, residual, ldr, w, b, eps, rows, hidden, sum, lds, y, ldy, mean, rstd, whole, st->sms};
+  const bool whole = r.whole && hidden % (16 / size_of(st->dtype)) == 0 && !misaligned(w, 16) && !misaligned(b, 16);
+  const aq::LayerNormArgs a{x, ldx, residual, ldr, w, b, eps, rows, hidden, sum, lds, y, ldy, mean, rstd,
+                            whole ? aq::kRowsWhole : r.alike ? aq::kRowsAlike : aq::kRowsAny, st->sms};
   return launched(st, aq::launch_layer_norm(st->dtype, a, st->stream), who);
 }
 
@@ -492,8 +505,8 @@ int aq_layer_norm_grad(aq_stage* st, const void* dy, int64_t lddy, const void* d
                        const float* mean, const float* rstd, int64_t rows, int hidden, void* dx, int64_t lddx, float* dw, float* db) {
   if (!st) return AQ_EINVAL;
   const char* who = "aq_layer_norm_grad";
-  bool whole;
-  AQ_TRY(check_norm(st, who, rows, hidden, w, nullptr, &whole));
+  NormRows r;
+  AQ_TRY(check_norm(st, who, rows, hidden, w, nullptr));
   if (misaligned(dw, 4) || misaligned(db, 4)) return fail(st, AQ_EINVAL, "%s: dw or db is misaligned", who);
   DeviceGuard guard(st->device);
   if (rows == 0) {                                           // no token: the weights' gradients are sums of nothing
@@ -504,16 +517,17 @@ int aq_layer_norm_grad(aq_stage* st, const void* dy, int64_t lddy, const void* d
     }
     return AQ_OK;
   }
-  AQ_TRY(check_norm_rows(st, who, "dy", dy, lddy, hidden, &whole));
-  AQ_TRY(check_norm_rows(st, who, "s", s, lds, hidden, &whole));
-  if (dsum) AQ_TRY(check_norm_rows(st, who, "dsum", dsum, ldds, hidden, &whole));
-  if (dx) AQ_TRY(check_norm_rows(st, who, "dx", dx, lddx, hidden, &whole));
+  AQ_TRY(check_norm_rows(st, who, "dy", dy, lddy, hidden, &r));
+  AQ_TRY(check_norm_rows(st, who, "s", s, lds, hidden, &r));
+  if (dsum) AQ_TRY(check_norm_rows(st, who, "dsum", dsum, ldds, hidden, &r));
+  if (dx) AQ_TRY(check_norm_rows(st, who, "dx", dx, lddx, hidden, &r));
   AQ_TRY(check_in_place(st, who, dx, lddx, dy, lddy));
   AQ_TRY(check_in_place(st, who, dx, lddx, dsum, ldds));
   AQ_TRY(check_in_place(st, who, dx, lddx, s, lds));
   if (!mean || !rstd || misaligned(mean, 4) || misaligned(rstd, 4)) return fail(st, AQ_EINVAL, "%s: mean or rstd is null or misaligned", who);
   if (!dx && !dw && !db) return AQ_OK;
-  aq::LayerNormGradArgs a{dy, lddy, dsum, ldds, s, lds, w, mean, rstd, rows, hidden, dx, lddx, dw, db, nullptr, whole, (int)size_of(st->dtype), st->sms};
+  aq::LayerNormGradArgs a{dy, lddy, dsum, ldds, s, lds, w, mean, rstd, rows, hidden, dx, lddx, dw, db, nullptr,
+                          r.whole ? aq::kRowsWhole : r.alike && r.begin ? aq::kRowsAlike : aq::kRowsAny, 1, (int)size_of(st->dtype), st->sms};
   if (dw || db) AQ_TRY(ensure_work(st, (size_t)aq::layer_norm_grad_bytes(a)));
   a.partials = static_cast<float*>(st->work);
   return launched(st, aq::launch_layer_norm_grad(st->dtype, a, st->stream), who);

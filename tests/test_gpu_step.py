@@ -84,11 +84,11 @@ def check_norm(dtype, s, w, b, eps, y, mean, rstd):
     close(y, y64, tol, "y")
 
 
-def run_norm(aq, st, dtype, x, r, w, b, eps, pad=0, offset=0, keep=True):
+def run_norm(aq, st, dtype, x, r, w, b, eps, pad=0, offset=0, keep=True, offset_y=None):
     """With guarded buffers; (s, y, mean, rstd)."""
     rows, d = x.shape
     t = TYPES[dtype]
-    bx, by = Guarded(rows, d, t, pad, offset).put(x), Guarded(rows, d, t, pad, offset)
+    bx, by = Guarded(rows, d, t, pad, offset).put(x), Guarded(rows, d, t, pad, offset if offset_y is None else offset_y)
     br = None if r is None else Guarded(rows, d, t, pad, offset).put(r)
     bs = Guarded(rows, d, t, pad, offset) if r is not None and keep else None
     mean, rstd = torch.zeros(rows + 8, device="cuda"), torch.zeros(rows + 8, device="cuda")
@@ -113,6 +113,19 @@ def test_layer_norm(aq, stage, dtype, d):
     for rows, pad, offset, residual, keep in ((1, 0, 0, False, True), (5, 0, 0, True, True), (3, 8, 8, True, False), (6, 1, 3, True, True)):
         x, r, w, b, _, _ = norm_inputs(rows, d, dtype)
         s, y, mean, rstd = run_norm(aq, stage, dtype, x, r if residual else None, w, b, 1e-5, pad, offset, keep)
+        check_norm(dtype, s, w, b, 1e-5, y, mean, rstd)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("d", WIDTHS)
+def test_layer_norm_rows_off_the_boundaries(aq, stage, dtype, d):
+    """Rows that begin anywhere in 16 bytes, in all operands alike or not, weights too."""
+    set_type(aq, stage, dtype)
+    for rows, pad, offset, offset_y in ((9, 0, 0, 0), (9, 3, 0, 0), (9, 2, 1, 1), (9, 4, 5, 5), (5, 1, 0, 1), (5, 8, 2, 0)):
+        x, r, w, b, _, _ = norm_inputs(rows, d, dtype, seed=pad)
+        wide = torch.zeros(d + 3, dtype=TYPES[dtype], device="cuda")
+        wide[3:] = w.cuda()
+        s, y, mean, rstd = run_norm(aq, stage, dtype, x, r, wide[3:], b, 1e-5, pad, offset, True, offset_y)
         check_norm(dtype, s, w, b, 1e-5, y, mean, rstd)
 
 
@@ -194,7 +207,7 @@ def statistics(s, eps=1e-5):
 @pytest.mark.parametrize("d", WIDTHS)
 def test_layer_norm_grad(aq, stage, dtype, d):
     set_type(aq, stage, dtype)
-    for rows, pad, offset, skip in ((1, 0, 0, False), (5, 0, 0, True), (37, 8, 8, True), (6, 1, 3, True)):
+    for rows, pad, offset, skip in ((1, 0, 0, False), (5, 0, 0, True), (37, 8, 8, True), (6, 1, 3, True), (41, 3, 0, True), (23, 1, 0, False), (19, 2, 0, True)):
         s, _, w, _, dy, dsum = norm_inputs(rows, d, dtype, seed=1)
         mean, rstd = statistics(s)
         got = run_norm_grad(aq, stage, dtype, dy, dsum if skip else None, s, w, mean, rstd, pad, offset)
@@ -202,15 +215,42 @@ def test_layer_norm_grad(aq, stage, dtype, d):
 
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
-@pytest.mark.parametrize("rows,d", [(5000, 768), (3001, 1600), (2000, 1021), (20011, 24), (700, 5000), (301, 12000), (9000, 3)])
-def test_layer_norm_grad_many_rows(aq, stage, dtype, rows, d):
+@pytest.mark.parametrize("rows,d,pad", [(5000, 768, 0), (3001, 1600, 0), (3001, 1600, 4), (2000, 1021, 0), (2000, 1021, 3), (20011, 24, 0), (20011, 24, 1), (700, 5000, 0),
+                                        (700, 5001, 1), (301, 12000, 0), (9000, 3, 0), (1500, 250, 1), (1500, 2045, 0), (900, 8190, 0)])
+def test_layer_norm_grad_many_rows(aq, stage, dtype, rows, d, pad):
     set_type(aq, stage, dtype)
     s, _, w, _, dy, dsum = norm_inputs(rows, d, dtype, seed=2)
     mean, rstd = statistics(s)
-    got = run_norm_grad(aq, stage, dtype, dy, dsum, s, w, mean, rstd)
+    got = run_norm_grad(aq, stage, dtype, dy, dsum, s, w, mean, rstd, pad)
     check_norm_grad(dtype, dy, dsum, s, w, mean, rstd, got)
-    again = run_norm_grad(aq, stage, dtype, dy, dsum, s, w, mean, rstd)
+    again = run_norm_grad(aq, stage, dtype, dy, dsum, s, w, mean, rstd, pad)
     assert all(torch.equal(a, b) for a, b in zip(got, again))               # the same bits
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d,pad", [(30, 1), (64, 3), (1021, 0), (1021, 3), (1600, 5), (4099, 0), (9001, 2)])
+def test_layer_norm_grad_next_to_rows_and_padding_that_are_not_finite(aq, stage, dtype, d, pad):
+    """A row of NaN makes its own dx NaN and dw, db; without it in them the others are as if it were not there; padding counts for nothing."""
+    set_type(aq, stage, dtype)
+    rows, t = 21, TYPES[dtype]
+    s, _, w, _, dy, dsum = norm_inputs(rows, d, dtype, seed=6)
+    mean, rstd = statistics(s)
+    bufs = []
+    for v in (dy, dsum, s):
+        buf = torch.full((rows, d + pad), math.nan, dtype=t, device="cuda")
+        buf[:, :d] = v.cuda()
+        bufs.append(buf)
+    out, ld = torch.zeros((rows, d + pad), dtype=t, device="cuda"), d + pad
+    dw, db = torch.zeros(d, device="cuda"), torch.zeros(d, device="cuda")
+    call = lambda: aq.aq_layer_norm_grad(stage, bufs[0], ld, bufs[1], ld, bufs[2], ld, w.cuda(), mean.cuda(), rstd.cuda(), rows, d, out, ld, dw, db)  # noqa: E731
+    call()
+    check_norm_grad(dtype, dy, dsum, s, w, mean, rstd, (out[:, :d], dw, db))
+    assert not out[:, d:].any()
+    bufs[0][7, :d] = math.nan
+    call()
+    keep = [r for r in range(rows) if r != 7]
+    assert bool(out[7, :d].isnan().all()) and bool(dw.isnan().all()) and bool(db.isnan().all())
+    check_norm_grad(dtype, dy[keep], dsum[keep], s[keep], w, mean[keep], rstd[keep], (out[keep, :d], None, None))
 
 
 @pytest.mark.parametrize("d", [64, 1600, 1021])
