@@ -361,7 +361,6 @@ __device__ void store_sums(float* to, const float2* f, int pairs) {
 
 constexpr int kGradWalks = 8;                 // rows' walks of a CTA where a row is a warp's
 constexpr int kGradSlots = 2;                 // batches of rows that a thread has in shared memory: the one it works on and the next
-
 // A CTA's threads have Q pieces of 16 bytes of a row each (WARP: a warp's lanes, and eight walks to a CTA) and take R rows at a time.  The next rows
 // are copied to shared memory meanwhile, each thread's elements by itself and for itself.  Elements behind a row's end are zeros there and add
 // nothing to any sum.  EDGE: rows begin inside a piece, every `period`-th one at the same place; a CTA (a warp) takes rows that do.
@@ -371,12 +370,13 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
   constexpr int H = Ps::N, N = 2 * H, V = 2 * R;
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float exchange[2][WARP ? 1 : MAX / 32][V];
-  __shared__ float stats[kGradSlots][MAX / 32][V];
+  __shared__ float2 stats[kGradSlots][MAX / 32][R];
   __shared__ float sums[WARP ? 2 : 1][WARP ? kGradWalks : 1][WARP ? 32 * N * Q : 1];
   const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), warps = blockDim.x / 32;
   const bool skip = a.dsum != nullptr;
-  // shared memory: a thread's 16 bytes of every piece, array and row; `part` from one to the next
-  const uint32_t part = blockDim.x * 16, row_bytes = part * Q * (skip ? 3 : 2), mine = shared_address(ring) + threadIdx.x * 16;
+  // shared memory: the threads' 16 bytes of a piece side by side; a piece, a row of three arrays and a slot further on
+  constexpr uint32_t kPart = MAX * 16, kRow = 3 * Q * kPart, kSlot = R * kRow;
+  const uint32_t mine = shared_address(ring) + threadIdx.x * 16;
   next_may_launch();
   wait_for_previous();
   const int walks = WARP ? gridDim.x * kGradWalks : gridDim.x, walk = WARP ? blockIdx.x * kGradWalks + warp : blockIdx.x;
@@ -406,9 +406,9 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
   T* o = a.dx ? static_cast<T*>(a.dx) + first * a.lddx : nullptr;
   const float* stat = (lane & 1 ? a.rstd : a.mean) + first + (lane % V) / 2 * period;
   const int step = walks * R, each = walks / period * R;       // rows, and rows of the kind, from one batch to the next
-  long long left = kinds - (long long)turn * R;                // rows of the kind from the next batch to ask for on
-  int here = (int)min(max(left, 0ll), (long long)0x7fffffff);  // ... from the batch that is worked on
+  int left = (int)max(kinds - (long long)turn * R, 0ll), here = left;   // rows of the kind from the next batch to ask for on; from the one that is worked on
   auto ask = [&](int slot) {
+    const uint32_t there = mine + slot * kSlot;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       if (i >= left) break;
@@ -416,13 +416,13 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         const int bytes = hi[q] * (int)sizeof(T), at = bytes ? column[q] : 0;   // a thread without elements reads nothing, from a valid address
-        const uint32_t to = mine + (slot * R + i) * row_bytes + q * part;
+        const uint32_t to = there + i * kRow + q * kPart;
         copy16(to, s + r * a.lds + at, bytes);
-        copy16(to + Q * part, g + r * a.lddy + at, bytes);
-        if (skip) copy16(to + 2 * Q * part, k + r * a.ldds + at, bytes);
+        copy16(to + Q * kPart, g + r * a.lddy + at, bytes);
+        if (skip) copy16(to + 2 * Q * kPart, k + r * a.ldds + at, bytes);
       }
     }
-    if (lane < V && lane / 2 < left) copy4(shared_address(&stats[slot][warp][lane]), stat);   // mean and rstd of the rows, for the warp
+    if (lane < V && lane / 2 < left) copy4(shared_address(&stats[slot][warp][0]) + lane * 4, stat);   // mean and rstd of the rows, for the warp
     s += step * a.lds;
     g += step * a.lddy;
     if (skip) k += step * a.ldds;
@@ -439,14 +439,16 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
     copies_end();
     copies_wait<1>();
     __syncwarp();
-    auto take = [&](int i, int array, int q, float2* f) { Ps::open(shared16(mine + (slot * R + i) * row_bytes + (array * Q + q) * part), f); };
-    float sum[V];
+    const uint32_t now = mine + slot * kSlot;
+    auto take = [&](int i, int array, int q, float2* f) { Ps::open(shared16(now + i * kRow + (array * Q + q) * kPart), f); };
+    float sum[V], rstds[R];
     float2 n[R][Q][H], y[R][Q][H];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       sum[2 * i] = sum[2 * i + 1] = 0.0f;
       if (i >= here) break;
-      const float mean = stats[slot][warp][2 * i], rstd = stats[slot][warp][2 * i + 1];
+      const float2 st = stats[slot][warp][i];
+      const float mean = st.x, rstd = rstds[i] = st.y;
       float2 sg = make_float2(0.0f, 0.0f), sgn = sg;
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
@@ -489,7 +491,7 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       if (i >= here) break;
-      const float rstd = stats[slot][warp][2 * i + 1];
+      const float rstd = rstds[i];
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         if (hi[q] <= lo[q]) continue;
@@ -637,10 +639,10 @@ __global__ void __launch_bounds__(32 * kJoinWarps) layer_norm_join_kernel(const 
 
 // How a gradient is computed: rows of a warp, rows of a CTA, or by columns and rows apart.  Threads have eight elements of a row, or
 // sixteen of rows wider than 2048, and as many CTAs run as are resident at a time.
-constexpr int kGradNarrow = 256, kGradWide = 512;             // threads of the CTAs that the registers are cut for
+constexpr int kGradSmall = 64, kGradNarrow = 256, kGradWide = 512;   // threads of the CTAs that registers and shared memory are cut for
 constexpr int kGradRows = 2;                                  // rows at a time, where threads have eight elements
 constexpr int kSharedOfSm = 227 * 1024;
-struct GradPlan { int threads, each, period; bool warp, apart, edge; int bytes; long long parts; };
+struct GradPlan { int threads, most, each, period; bool warp, apart, edge; int bytes; long long parts; };
 GradPlan grad_plan(const LayerNormGradArgs& a) {
   GradPlan p{};
   const int piece = 16 / a.size;
@@ -660,12 +662,15 @@ GradPlan grad_plan(const LayerNormGradArgs& a) {
   const int pieces = (span + piece - 1) / piece, of_thread = p.each / piece;
   p.threads = p.warp ? 32 * kGradWalks : ((pieces + of_thread - 1) / of_thread + 31) / 32 * 32;
   const int rows = p.each == 8 ? kGradRows : 1;
-  p.bytes = kGradSlots * rows * (a.dsum ? 3 : 2) * p.threads * p.each * a.size;
-  int per_sm = p.threads > kGradNarrow ? 1 : 2 * (kGradNarrow / p.threads);
+  p.most = p.threads <= kGradSmall ? kGradSmall : p.threads <= kGradNarrow ? kGradNarrow : kGradWide;
+  p.bytes = p.most * kGradSlots * rows * 3 * of_thread * 16;
+  int per_sm = kGradWide / p.most * (p.most / p.threads);
   if (per_sm > kSharedOfSm / (p.bytes + 2048)) per_sm = kSharedOfSm / (p.bytes + 2048);
   const int batch = rows * (p.warp ? kGradWalks : 1);
   const long long batches = (a.rows + batch - 1) / batch, most = (long long)per_sm * a.sms;
-  p.parts = batches < most ? batches : most;
+  // four batches to a CTA at least, if every multiprocessor has one all the same
+  const long long few = batches / 4 > a.sms ? batches / 4 : batches < a.sms ? batches : a.sms;
+  p.parts = few < most ? few : most;
   if (!p.warp) p.parts = (p.parts + p.period - 1) / p.period * p.period;   // as many walks of every kind of rows
   return p;
 }
@@ -683,8 +688,9 @@ template <typename T, bool EDGE, bool WARP, int R, int Q, int MAX, int CTAS> cud
 template <typename T, bool EDGE> cudaError_t run_walks(const LayerNormGradArgs& a, const GradPlan& p, cudaStream_t s) {
   constexpr int kPiece = 16 / sizeof(T);
   if (p.warp) return start_grad<T, EDGE, true, kGradRows, 8 / kPiece, kGradNarrow, 2>(a, p, s);
+  if (p.each == 8 && p.most == kGradSmall) return start_grad<T, EDGE, false, kGradRows, 8 / kPiece, kGradSmall, 8>(a, p, s);
   if (p.each == 8) return start_grad<T, EDGE, false, kGradRows, 8 / kPiece, kGradNarrow, 2>(a, p, s);
-  if (p.threads <= kGradNarrow) return start_grad<T, EDGE, false, 1, 16 / kPiece, kGradNarrow, 2>(a, p, s);
+  if (p.most <= kGradNarrow) return start_grad<T, EDGE, false, 1, 16 / kPiece, kGradNarrow, 2>(a, p, s);
   return start_grad<T, EDGE, false, 1, 16 / kPiece, kGradWide, 1>(a, p, s);
 }
 
