@@ -148,7 +148,7 @@ __device__ uint32_t random_bits(uint32_t scrambled) {           // of (element +
 // Codes of m[8] and v[8].  A moment is scaled so that the format's exponents are binary32's smallest, subnormal numbers among them; the
 // format's last bit is then bit 20 or 21, the random number is added below it, and the bits above are the code.
 template <int STRIDE>
-__device__ __forceinline__ void store_codes(const float2* m, const float2* v, int em, int ev, uint32_t place, uint32_t key, uint32_t* cm, uint32_t* cv) {
+__device__ __forceinline__ void store_codes(const float2* m, const float2* v, int em, int ev, uint32_t place, uint32_t wrapped, uint32_t key, uint32_t* cm, uint32_t* cv) {
   float2 ym[4], yv[4];
   const float im = power_of_two(254 - em), iv = power_of_two(254 - ev);
   if (em <= 127 + 29 && ev <= 127 + 37) {                       // times 2^-120 and 2^-112 they still are binary32 numbers
@@ -166,7 +166,13 @@ __device__ __forceinline__ void store_codes(const float2* m, const float2* v, in
   const uint32_t scrambled = (place + key) * kRoot3;
 #pragma unroll
   for (int j = 0; j < 8; j += 2) {
-    const uint32_t u = random_bits(scrambled + (uint32_t)j * (STRIDE * kRoot3)), w = random_bits(scrambled + (uint32_t)(j + 1) * (STRIDE * kRoot3));
+    uint32_t u = scrambled + (uint32_t)j * ((STRIDE ? STRIDE : 1) * kRoot3), w = scrambled + (uint32_t)(j + 1) * ((STRIDE ? STRIDE : 1) * kRoot3);
+    if (STRIDE == 0) {
+      if (j < wrapped) u += 256 * kRoot3;
+      if (j + 1 < wrapped) w += 256 * kRoot3;
+    }
+    u = random_bits(u);
+    w = random_bits(w);
     tm[j] = __float_as_uint(ym[j / 2].x) + (u & 0xffffu) * 16;  // the sign stays in bit 31
     tm[j + 1] = __float_as_uint(ym[j / 2].y) + (w & 0xffffu) * 16;
     tv[j] = __float_as_uint(yv[j / 2].x) + (u >> 16) * 32;
@@ -215,9 +221,10 @@ template <typename T, int BITS> struct Written {
 
 struct Settings { float factor, beta1, rest1, beta2, rest2, one, eps, step_size, root_c2, decay; uint32_t key; };
 
-// Eight elements of a lane, a block's 256 of a warp; place: of the lane's first one in its tensor, the others STRIDE apart.
+// Eight elements of a lane, a block's 256 of a warp; place: of the lane's first one in its tensor, the others STRIDE apart.  STRIDE 0: one apart,
+// and the first `wrapped` ones 256 further on.
 template <typename T, int BITS, bool MIXED, int STRIDE>
-__device__ __forceinline__ void update(const Settings& a, const Read<T, BITS, MIXED>& r, bool grad32, bool master, uint32_t place, Written<T, BITS>& o) {
+__device__ __forceinline__ void update(const Settings& a, const Read<T, BITS, MIXED>& r, bool grad32, bool master, uint32_t place, uint32_t wrapped, Written<T, BITS>& o) {
   float2 m[4], v[4];
   float largest_m = 0.0f, largest_v = 0.0f;
 #pragma unroll
@@ -251,7 +258,7 @@ __device__ __forceinline__ void update(const Settings& a, const Read<T, BITS, MI
   if (BITS == 8) {
     const uint32_t bits_m = largest_of_warp(largest_m), bits_v = largest_of_warp(largest_v);
     const int em = scale_exponent(bits_m, 8), ev = scale_exponent(bits_v, 15);
-    store_codes<STRIDE>(m, v, em, ev, place, a.key, o.m, o.v);
+    store_codes<STRIDE>(m, v, em, ev, place, wrapped, a.key, o.m, o.v);
     const float nan = __int_as_float(0x7fc00000);               // a block with an infinity or NaN is NaN from here on
     o.sm = bits_m < 0x7f800000u ? power_of_two(em) : nan;
     o.sv = bits_v < 0x7f800000u ? power_of_two(ev) : nan;
@@ -289,13 +296,50 @@ template <int N> struct Walk {
   }
 };
 
+// Blocks that begin r elements behind a multiple of eight, in all operands: lane 0 has the block's first 8 - r elements and its last r, the
+// other lanes have eight on the grid, which begins r elements before the block.  Of w words with PER elements each, bits of those below r.
+template <int PER> __device__ uint32_t below(uint32_t r, int w) {
+  const int n = min(max((int)r - PER * w, 0), PER) * (32 / PER);
+  return n < 32 ? (1u << n) - 1 : 0xffffffffu;
+}
+template <int PER, int W> __device__ void merge_below(uint32_t r, uint32_t* w, const uint32_t* low) {
+#pragma unroll
+  for (int i = 0; i < W; ++i) { const uint32_t m = below<PER>(r, i); w[i] = (w[i] & ~m) | (low[i] & m); }
+}
+// A lane's eight elements of such a block; `to`: the grid's.  `last`: lane 0's words of the block before, whose last r elements lie in its first
+// eight of the grid here; without them (`open`) lane 0 stores only what is this block's.
+template <typename T> __device__ void put_shifted(T* to, uint32_t r, int lane, bool open, uint32_t* w, uint32_t* last) {
+  constexpr int W = Eight<T>::W, PER = 8 / W;
+  uint32_t now[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) now[i] = w[i];
+  if (lane == 0) {
+    if (open) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j >= r) Eight<T>::store_one(to + j, j, w);
+    } else {
+      merge_below<PER, W>(r, now, last);
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) last[i] = w[i];
+  }
+  if (lane || !open) Eight<T>::store(to, now);
+}
+// lane 0's last r elements of the last block
+template <typename T> __device__ void put_last(T* to, uint32_t r, const uint32_t* last) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (j < r) Eight<T>::store_one(to + j, j, last);
+}
+
 // Shared memory of the 8-bit moments: every warp has two slots for a piece of P blocks each.  A block's gradients, parameters,
-// codes of m and of v; behind the blocks their scales in pairs.
+// codes of m and of v, and of a shifted block the eight elements of each behind the grid's first 256; behind the blocks their scales in pairs.
 template <typename T, bool MIXED> struct Ring {
   static constexpr int kValues = 256 * (MIXED ? 4 : (int)sizeof(T)), P = kValues == 512 ? 4 : 1;
-  static constexpr int kParam = kValues, kM = 2 * kValues, kV = kM + 256, kBlock = kV + 256, kScales = P * kBlock, kSlot = kScales + (P * 8 + 15) / 16 * 16;
+  static constexpr int kParam = kValues, kM = 2 * kValues, kV = kM + 256, kMore = kV + 256, kBlock = kMore + kValues / 16 + 16, kScales = P * kBlock, kSlot = kScales + (P * 8 + 15) / 16 * 16;
   static constexpr int kBytes = kAdamWarps * 2 * kSlot;
-  static_assert(kSlot % 16 == 0, "copies start on 16-byte boundaries");
+  static_assert(kBlock % 16 == 0 && kSlot % 16 == 0, "copies start on 16-byte boundaries");
 };
 
 template <typename T, int BITS, bool MIXED, int N>
@@ -312,28 +356,41 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
   Settings set{a.factor ? __ldg(a.factor) : 1.0f, a.beta1, a.rest1, a.beta2, a.rest2, a.one, a.eps, 0, 0, 0, 0};
   if (!(fabsf(set.factor) < __int_as_float(0x7f800000))) return;   // a step that is to be left out
 
-  // of a piece's blocks those that are whole and of aligned tensors
+  // of a piece's blocks those from `first` to `end` lie on the grid of eight elements, or all as far behind it, with the grid's elements around
+  // them in the same tensor
+  struct Wide { uint32_t first, end, shift; };
   auto wide_blocks = [&](const Walk<N>& k) {
     const AdamPart& part = table.part[k.t];
-    return part.flags & kPartWide ? min(min(k.left, P), (part.numel - k.at) / 256) : 0u;
+    const uint32_t shift = BITS == 8 ? part.flags >> kPartShiftBit : 0, more = shift ? 8 - shift : 0, rest = part.numel - k.at;
+    Wide w{shift && k.at == 0 ? 1u : 0u, part.flags & kPartWide && rest > more ? min(min(k.left, P), (rest - more) / 256) : 0u, shift};
+    if (w.end < w.first) w.end = w.first = 0;
+    return w;
   };
   auto ask = [&](const Walk<N>& k, uint32_t to) {
     const AdamPart& part = table.part[k.t];
-    const uint32_t blocks = wide_blocks(k), e = k.at + lane * 8;
+    const Wide wide = wide_blocks(k);
+    const uint32_t at = k.at - wide.shift, e = at + lane * 8;   // below 0 for the first block of a shifted tensor, which is left out
     const bool grad32 = MIXED && (part.flags & kPartGradF32), master = MIXED && part.master;
-    const char* const g = static_cast<const char*>(part.grad) + (size_t)k.at * (grad32 ? 4 : sizeof(T)) + lane * 16;
-    const char* const p = (master ? reinterpret_cast<const char*>(part.master + k.at) : reinterpret_cast<const char*>(static_cast<T*>(part.param) + k.at)) + lane * 16;
-    const uint8_t *const m = static_cast<uint8_t*>(part.m) + e, *const v = static_cast<uint8_t*>(part.v) + e;
+    const int gs = grad32 ? 4 : (int)sizeof(T), ps = master ? 4 : (int)sizeof(T);
+    const char* const g = static_cast<const char*>(part.grad) + (long long)(int)at * gs + lane * 16;
+    const char* const p = (master ? reinterpret_cast<const char*>(part.master) : static_cast<const char*>(part.param)) + (long long)(int)at * ps + lane * 16;
+    const uint8_t *const m = static_cast<uint8_t*>(part.m) + (int)e, *const v = static_cast<uint8_t*>(part.v) + (int)e;
 #pragma unroll
     for (uint32_t i = 0; i < P; ++i) {
-      if (i >= blocks) break;
+      if (i >= wide.end) break;
+      if (i < wide.first) continue;
       const uint32_t block = to + i * Rg::kBlock;
       if (grad32) copy_1k(block + lane * 16, g + i * 1024); else copy_block<T>(block + lane * 16, g + i * 256 * sizeof(T));
       if (master) copy_1k(block + Rg::kParam + lane * 16, p + i * 1024); else copy_block<T>(block + Rg::kParam + lane * 16, p + i * 256 * sizeof(T));
       copy8(block + Rg::kM + lane * 8, m + i * 256);
       copy8(block + Rg::kV + lane * 8, v + i * 256);
+      if (wide.shift) {                                         // gs + ps lanes for gradients and parameters, one each for the codes
+        const char* const from = lane < gs ? g + (i + 1) * 256 * gs - lane * 8 : lane < gs + ps ? p + (i + 1) * 256 * ps - gs * 8 - lane * 8
+                                 : reinterpret_cast<const char*>(lane == gs + ps ? m : v) + (i + 1) * 256 - lane * 8;
+        if (lane < gs + ps + 2) copy8(block + Rg::kMore + lane * 8, from);
+      }
     }
-    if ((lane & 15) < blocks) copy4(to + Rg::kScales + (lane & 15) * 8 + (lane >> 4) * 4, (lane & 16 ? part.v_scale : part.m_scale) + k.at / 256 + (lane & 15));
+    if ((lane & 15) >= wide.first && (lane & 15) < wide.end) copy4(to + Rg::kScales + (lane & 15) * 8 + (lane >> 4) * 4, (lane & 16 ? part.v_scale : part.m_scale) + k.at / 256 + (lane & 15));
   };
   Walk<N> k(table, blockIdx.x * kAdamWarps + warp, gridDim.x * kAdamWarps), ahead = k;
   if (BITS == 8) {
@@ -368,7 +425,8 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
   while (k.here(table)) {
     const AdamPart& part = table.part[k.t];
     const bool grad32 = MIXED && (part.flags & kPartGradF32), master = MIXED && part.master;
-    const uint32_t blocks = min(k.left, P), wide = wide_blocks(k);
+    const uint32_t blocks = min(k.left, P);
+    const Wide wide = wide_blocks(k);
     set.decay = lr * part.decay;
     if (BITS == 8) {                                            // the next piece goes where the whole warp has read the last one
       copies_wait<0>();
@@ -379,37 +437,79 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
       }
       copies_end();
     }
+    auto from_ring = [&](uint32_t i, Read<T, BITS, MIXED>& r) {
+      const uint32_t block = here + i * Rg::kBlock;
+      if (grad32) shared32(block + lane * 32, r.g); else shared_eight<T>(block + lane * 8 * sizeof(T), r.g);
+      if (master) shared32(block + Rg::kParam + lane * 32, r.p); else shared_eight<T>(block + Rg::kParam + lane * 8 * sizeof(T), r.p);
+      shared8(block + Rg::kM + lane * 8, r.m);
+      shared8(block + Rg::kV + lane * 8, r.v);
+      uint32_t scales[2];
+      shared8(here + Rg::kScales + i * 8, scales);
+      r.sm = __uint_as_float(scales[0]);
+      r.sv = __uint_as_float(scales[1]);
+    };
     const uint32_t e = k.at + lane * 8;
+    if (BITS == 32 || !wide.shift) {
 #pragma unroll 1
-    for (uint32_t i = 0; i < wide; ++i) {
-      Read<T, BITS, MIXED> r;
-      const uint32_t to = e + i * 256;
-      if (BITS == 8) {
-        const uint32_t block = here + i * Rg::kBlock;
-        if (grad32) shared32(block + lane * 32, r.g); else shared_eight<T>(block + lane * 8 * sizeof(T), r.g);
-        if (master) shared32(block + Rg::kParam + lane * 32, r.p); else shared_eight<T>(block + Rg::kParam + lane * 8 * sizeof(T), r.p);
-        shared8(block + Rg::kM + lane * 8, r.m);
-        shared8(block + Rg::kV + lane * 8, r.v);
-        uint32_t scales[2];
-        shared8(here + Rg::kScales + i * 8, scales);
-        r.sm = __uint_as_float(scales[0]);
-        r.sv = __uint_as_float(scales[1]);
-      } else {
-        if (grad32) Eight<float>::load(static_cast<const float*>(part.grad) + to, r.g); else Eight<T>::load(static_cast<const T*>(part.grad) + to, r.g);
-        if (master) Eight<float>::load(part.master + to, r.p); else Eight<T>::load(static_cast<const T*>(part.param) + to, r.p);
-        Eight<State>::load(static_cast<const State*>(part.m) + to, r.m);
-        Eight<State>::load(static_cast<const State*>(part.v) + to, r.v);
+      for (uint32_t i = 0; i < wide.end; ++i) {
+        Read<T, BITS, MIXED> r;
+        const uint32_t to = e + i * 256;
+        if (BITS == 8) {
+          from_ring(i, r);
+        } else {
+          if (grad32) Eight<float>::load(static_cast<const float*>(part.grad) + to, r.g); else Eight<T>::load(static_cast<const T*>(part.grad) + to, r.g);
+          if (master) Eight<float>::load(part.master + to, r.p); else Eight<T>::load(static_cast<const T*>(part.param) + to, r.p);
+          Eight<State>::load(static_cast<const State*>(part.m) + to, r.m);
+          Eight<State>::load(static_cast<const State*>(part.v) + to, r.v);
+        }
+        Written<T, BITS> o;
+        update<T, BITS, MIXED, 1>(set, r, grad32, master, part.place + to, 0, o);
+        if (master) Eight<float>::store(part.master + to, o.master);
+        Eight<T>::store(static_cast<T*>(part.param) + to, o.p);
+        Eight<State>::store(static_cast<State*>(part.m) + to, o.m);
+        Eight<State>::store(static_cast<State*>(part.v) + to, o.v);
+        if (BITS == 8 && lane == in_unit + i) { unit_sm = o.sm; unit_sv = o.sv; }
       }
-      Written<T, BITS> o;
-      update<T, BITS, MIXED, 1>(set, r, grad32, master, part.place + to, o);
-      if (master) Eight<float>::store(part.master + to, o.master);
-      Eight<T>::store(static_cast<T*>(part.param) + to, o.p);
-      Eight<State>::store(static_cast<State*>(part.m) + to, o.m);
-      Eight<State>::store(static_cast<State*>(part.v) + to, o.v);
-      if (BITS == 8 && lane == in_unit + i) { unit_sm = o.sm; unit_sv = o.sv; }
+    }
+    if constexpr (BITS == 8) {
+      if (wide.shift) {
+        const uint32_t shift = wide.shift, wrapped = lane ? 0 : shift;
+        Written<T, BITS> last;
+#pragma unroll 1
+        for (uint32_t i = wide.first; i < wide.end; ++i) {
+          Read<T, BITS, MIXED> r;
+          from_ring(i, r);
+          // lane 0's elements below `shift` come from behind the grid's 256
+          const uint32_t more = here + i * Rg::kBlock + Rg::kMore, gs = grad32 ? 4 : sizeof(T), ps = master ? 4 : sizeof(T);
+          uint32_t low[8];
+          if (grad32) { shared32(more, low); merge_below<1, 8>(wrapped, r.g, low); } else { shared_eight<T>(more, low); merge_below<8 / Eight<T>::W, Eight<T>::W>(wrapped, r.g, low); }
+          if (master) { shared32(more + gs * 8, low); merge_below<1, 8>(wrapped, r.p, low); } else { shared_eight<T>(more + gs * 8, low); merge_below<8 / Eight<T>::W, Eight<T>::W>(wrapped, r.p, low); }
+          shared8(more + (gs + ps) * 8, low);
+          merge_below<4, 2>(wrapped, r.m, low);
+          shared8(more + (gs + ps) * 8 + 8, low);
+          merge_below<4, 2>(wrapped, r.v, low);
+          const uint32_t to = e - shift + i * 256;
+          Written<T, BITS> o;
+          update<T, BITS, MIXED, 0>(set, r, grad32, master, part.place + to, wrapped, o);
+          const bool open = i == wide.first;
+          if (master) put_shifted(part.master + (int)to, shift, lane, open, o.master, last.master);
+          put_shifted(static_cast<T*>(part.param) + (int)to, shift, lane, open, o.p, last.p);
+          put_shifted(static_cast<State*>(part.m) + (int)to, shift, lane, open, o.m, last.m);
+          put_shifted(static_cast<State*>(part.v) + (int)to, shift, lane, open, o.v, last.v);
+          if (lane == in_unit + i) { unit_sm = o.sm; unit_sv = o.sv; }
+        }
+        if (lane == 0 && wide.first < wide.end) {
+          const uint32_t to = k.at - shift + wide.end * 256;
+          if (master) put_last(part.master + to, shift, last.master);
+          put_last(static_cast<T*>(part.param) + to, shift, last.p);
+          put_last(static_cast<State*>(part.m) + to, shift, last.m);
+          put_last(static_cast<State*>(part.v) + to, shift, last.v);
+        }
+      }
     }
 #pragma unroll 1
-    for (uint32_t i = wide; i < blocks; ++i) {                  // elements in turn, the last block's as far as they go
+    for (uint32_t n = blocks - (wide.end - wide.first), i = wide.first ? 0 : wide.end; n; --n, i = i + 1 == wide.first ? wide.end : i + 1) {
+      // elements in turn, the last block's as far as they go
       const Lane8 l{k.at + i * 256 + lane, part.numel};
       Read<T, BITS, MIXED> r;
       if (grad32) take<float>(l, part.grad, r.g); else take<T>(l, part.grad, r.g);
@@ -418,7 +518,7 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
       take<State>(l, part.v, r.v);
       if (BITS == 8) { r.sm = part.m_scale[k.at / 256 + i]; r.sv = part.v_scale[k.at / 256 + i]; }
       Written<T, BITS> o;
-      update<T, BITS, MIXED, 32>(set, r, grad32, master, part.place + l.at, o);
+      update<T, BITS, MIXED, 32>(set, r, grad32, master, part.place + l.at, 0, o);
       if (master) put<float>(l, part.master, o.master);
       put<T>(l, part.param, o.p);
       put<State>(l, part.m, o.m);

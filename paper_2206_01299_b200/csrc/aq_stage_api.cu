@@ -214,13 +214,12 @@ int gather_parts(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, int bit
     const int head = until_eight(t.grad, grad_size);
     bool agree = true;
     if (bits) agree = until_eight(t.param, size) == head && (!t.master || until_eight(t.master, 4) == head) && until_eight(t.m, state_size) == head && until_eight(t.v, state_size) == head;
-    if (bits == 8 && head) agree = false;                    // its blocks are counted from the tensor's beginning
     const bool f32 = t.grad_dtype == AQ_FP32 && st->dtype != AQ_FP32;
     for (int64_t count; *from < t.numel; *from += count) {
       if (have == aq::kAdamTable) return have;
       const int64_t e = *from;
-      // a few elements by themselves, and the rest begins where wide accesses may
-      const bool first = agree && head && e == 0;
+      // a few elements by themselves, and the rest begins where wide accesses may; blocks of 8-bit moments are counted from the beginning and stay
+      const bool first = agree && head && e == 0 && bits != 8;
       count = first ? head : aq::kPartMost;
       if (count > t.numel - e) count = t.numel - e;
       auto at = [e](const void* p, int bytes) { return p ? const_cast<char*>(static_cast<const char*>(p)) + e * bytes : nullptr; };
@@ -237,7 +236,7 @@ int gather_parts(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, int bit
       }
       p.numel = (uint32_t)count;
       p.place = (uint32_t)e;
-      p.flags = (agree && !first ? aq::kPartWide : 0u) | (f32 ? aq::kPartGradF32 : 0u);
+      p.flags = (agree && !first ? aq::kPartWide : 0u) | (agree && bits == 8 ? (uint32_t)((8 - head) & 7) << aq::kPartShiftBit : 0u) | (f32 ? aq::kPartGradF32 : 0u);
     }
   }
   return have;

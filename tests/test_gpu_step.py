@@ -541,6 +541,34 @@ def test_adamw(aq, stage, bits, dtype, grads, master, packed):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype,grads,master", [("fp32", "fp32", False), ("bf16", "bf16", False), ("fp16", "fp32", True), ("bf16", "bf16", True)])
+@pytest.mark.parametrize("shift", list(range(8)))
+def test_adamw_of_tensors_off_the_grid_of_eight(aq, stage, bits, dtype, grads, master, shift):
+    """Tensors that all begin `shift` elements behind a multiple of eight, of lengths about those of blocks, units and pieces; and
+    operands that do not begin alike."""
+    set_type(aq, stage, dtype)
+    sizes = [600, 256, 264 + shift, 263 - shift, 1000, 1024, 2304, 2048 + 255, 70001, 300]
+    for alike in (True, False):
+        s = Set(sizes, dtype, grads, bits, master, False)
+        for name in ["param", "grad", "m", "v"] + (["master"] if master else []):
+            for i, x in enumerate(getattr(s, name)):
+                n = shift if alike or name != "grad" else (shift + 3) % 8
+                buf = torch.zeros(x.numel() + 32, dtype=x.dtype, device="cuda")
+                buf.view(torch.uint8).fill_(0x33)
+                buf[8 + n:8 + n + x.numel()].copy_(x)
+                getattr(s, name)[i] = buf[8 + n:8 + n + x.numel()]
+                s.buffers[name, i] = (buf, [getattr(s, name)[i]])
+        table = s.table(aq, stage)
+        for step in (1, 500):
+            before = s.snapshot()
+            aq.aq_adamw(stage, aq.AdamwConfig(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=step, state_bits=bits), table, len(sizes), None, None, None)
+            s.check(before, 1e-3, step)
+        for buf, (x,) in s.buffers.values():
+            x.view(torch.uint8).fill_(0x33)
+            assert bool((buf.view(torch.uint8) == 0x33).all())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_adamw_of_more_tensors_than_a_launch_takes(aq, stage, bits):
     set_type(aq, stage, "bf16")
     sizes = [(i * 37) % 700 for i in range(1005)]
