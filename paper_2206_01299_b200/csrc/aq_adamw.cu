@@ -148,7 +148,7 @@ __device__ uint32_t random_bits(uint32_t scrambled) {           // of (element +
 // Codes of m[8] and v[8].  A moment is scaled so that the format's exponents are binary32's smallest, subnormal numbers among them; the
 // format's last bit is then bit 20 or 21, the random number is added below it, and the bits above are the code.
 template <int STRIDE>
-__device__ __forceinline__ void store_codes(const float2* m, const float2* v, int em, int ev, uint32_t place, uint32_t wrapped, uint32_t key, uint32_t* cm, uint32_t* cv) {
+__device__ __forceinline__ void store_codes(const float2* m, const float2* v, int em, int ev, uint32_t place, const uint32_t* wrap, uint32_t key, uint32_t* cm, uint32_t* cv) {
   float2 ym[4], yv[4];
   const float im = power_of_two(254 - em), iv = power_of_two(254 - ev);
   if (em <= 127 + 29 && ev <= 127 + 37) {                       // times 2^-120 and 2^-112 they still are binary32 numbers
@@ -166,13 +166,8 @@ __device__ __forceinline__ void store_codes(const float2* m, const float2* v, in
   const uint32_t scrambled = (place + key) * kRoot3;
 #pragma unroll
   for (int j = 0; j < 8; j += 2) {
-    uint32_t u = scrambled + (uint32_t)j * ((STRIDE ? STRIDE : 1) * kRoot3), w = scrambled + (uint32_t)(j + 1) * ((STRIDE ? STRIDE : 1) * kRoot3);
-    if (STRIDE == 0) {
-      if (j < wrapped) u += 256 * kRoot3;
-      if (j + 1 < wrapped) w += 256 * kRoot3;
-    }
-    u = random_bits(u);
-    w = random_bits(w);
+    constexpr uint32_t kNext = (STRIDE ? STRIDE : 1) * kRoot3;
+    const uint32_t u = random_bits(scrambled + (uint32_t)j * kNext + (STRIDE ? 0 : wrap[j])), w = random_bits(scrambled + (uint32_t)(j + 1) * kNext + (STRIDE ? 0 : wrap[j + 1]));
     tm[j] = __float_as_uint(ym[j / 2].x) + (u & 0xffffu) * 16;  // the sign stays in bit 31
     tm[j + 1] = __float_as_uint(ym[j / 2].y) + (w & 0xffffu) * 16;
     tv[j] = __float_as_uint(yv[j / 2].x) + (u >> 16) * 32;
@@ -222,9 +217,9 @@ template <typename T, int BITS> struct Written {
 struct Settings { float factor, beta1, rest1, beta2, rest2, one, eps, step_size, root_c2, decay; uint32_t key; };
 
 // Eight elements of a lane, a block's 256 of a warp; place: of the lane's first one in its tensor, the others STRIDE apart.  STRIDE 0: one apart,
-// and the first `wrapped` ones 256 further on.
+// and some of them 256 further on, which `wrap` has times kRoot3.
 template <typename T, int BITS, bool MIXED, int STRIDE>
-__device__ __forceinline__ void update(const Settings& a, const Read<T, BITS, MIXED>& r, bool grad32, bool master, uint32_t place, uint32_t wrapped, Written<T, BITS>& o) {
+__device__ __forceinline__ void update(const Settings& a, const Read<T, BITS, MIXED>& r, bool grad32, bool master, uint32_t place, const uint32_t* wrap, Written<T, BITS>& o) {
   float2 m[4], v[4];
   float largest_m = 0.0f, largest_v = 0.0f;
 #pragma unroll
@@ -258,7 +253,7 @@ __device__ __forceinline__ void update(const Settings& a, const Read<T, BITS, MI
   if (BITS == 8) {
     const uint32_t bits_m = largest_of_warp(largest_m), bits_v = largest_of_warp(largest_v);
     const int em = scale_exponent(bits_m, 8), ev = scale_exponent(bits_v, 15);
-    store_codes<STRIDE>(m, v, em, ev, place, wrapped, a.key, o.m, o.v);
+    store_codes<STRIDE>(m, v, em, ev, place, wrap, a.key, o.m, o.v);
     const float nan = __int_as_float(0x7fc00000);               // a block with an infinity or NaN is NaN from here on
     o.sm = bits_m < 0x7f800000u ? power_of_two(em) : nan;
     o.sv = bits_v < 0x7f800000u ? power_of_two(ev) : nan;
@@ -302,29 +297,28 @@ template <int PER> __device__ uint32_t below(uint32_t r, int w) {
   const int n = min(max((int)r - PER * w, 0), PER) * (32 / PER);
   return n < 32 ? (1u << n) - 1 : 0xffffffffu;
 }
-template <int PER, int W> __device__ void merge_below(uint32_t r, uint32_t* w, const uint32_t* low) {
+template <int W> __device__ void merge(const uint32_t* mask, uint32_t* w, const uint32_t* low) {
 #pragma unroll
-  for (int i = 0; i < W; ++i) { const uint32_t m = below<PER>(r, i); w[i] = (w[i] & ~m) | (low[i] & m); }
+  for (int i = 0; i < W; ++i) w[i] = (w[i] & ~mask[i]) | (low[i] & mask[i]);
 }
 // A lane's eight elements of such a block; `to`: the grid's.  `last`: lane 0's words of the block before, whose last r elements lie in its first
-// eight of the grid here; without them (`open`) lane 0 stores only what is this block's.
-template <typename T> __device__ void put_shifted(T* to, uint32_t r, int lane, bool open, uint32_t* w, uint32_t* last) {
-  constexpr int W = Eight<T>::W, PER = 8 / W;
-  uint32_t now[W];
+// eight of the grid here; without them (`open`) lane 0 stores only what is this block's.  mask: of the elements below r, in lane 0.
+template <typename T> __device__ void put_shifted(T* to, uint32_t r, int lane, bool open, const uint32_t* mask, const uint32_t* w, uint32_t* last) {
+  constexpr int W = Eight<T>::W;
+  if (!open) {
+    uint32_t now[W];
 #pragma unroll
-  for (int i = 0; i < W; ++i) now[i] = w[i];
-  if (lane == 0) {
-    if (open) {
+    for (int i = 0; i < W; ++i) now[i] = (w[i] & ~mask[i]) | (last[i] & mask[i]);
+    Eight<T>::store(to, now);
+  } else if (lane) {
+    Eight<T>::store(to, w);
+  } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j >= r) Eight<T>::store_one(to + j, j, w);
-    } else {
-      merge_below<PER, W>(r, now, last);
-    }
-#pragma unroll
-    for (int i = 0; i < W; ++i) last[i] = w[i];
+    for (int j = 0; j < 8; ++j)
+      if (j >= r) Eight<T>::store_one(to + j, j, w);
   }
-  if (lane || !open) Eight<T>::store(to, now);
+#pragma unroll
+  for (int i = 0; i < W; ++i) last[i] = w[i];
 }
 // lane 0's last r elements of the last block
 template <typename T> __device__ void put_last(T* to, uint32_t r, const uint32_t* last) {
@@ -463,7 +457,7 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
           Eight<State>::load(static_cast<const State*>(part.v) + to, r.v);
         }
         Written<T, BITS> o;
-        update<T, BITS, MIXED, 1>(set, r, grad32, master, part.place + to, 0, o);
+        update<T, BITS, MIXED, 1>(set, r, grad32, master, part.place + to, nullptr, o);
         if (master) Eight<float>::store(part.master + to, o.master);
         Eight<T>::store(static_cast<T*>(part.param) + to, o.p);
         Eight<State>::store(static_cast<State*>(part.m) + to, o.m);
@@ -474,6 +468,14 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
     if constexpr (BITS == 8) {
       if (wide.shift) {
         const uint32_t shift = wide.shift, wrapped = lane ? 0 : shift;
+        uint32_t mask32[8], mask_t[Eight<T>::W], mask8[2], wrap[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          wrap[j] = j < wrapped ? 256 * kRoot3 : 0;
+          mask32[j] = below<1>(wrapped, j);
+          if (j < Eight<T>::W) mask_t[j] = below<8 / Eight<T>::W>(wrapped, j);
+          if (j < 2) mask8[j] = below<4>(wrapped, j);
+        }
         Written<T, BITS> last;
 #pragma unroll 1
         for (uint32_t i = wide.first; i < wide.end; ++i) {
@@ -482,20 +484,20 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
           // lane 0's elements below `shift` come from behind the grid's 256
           const uint32_t more = here + i * Rg::kBlock + Rg::kMore, gs = grad32 ? 4 : sizeof(T), ps = master ? 4 : sizeof(T);
           uint32_t low[8];
-          if (grad32) { shared32(more, low); merge_below<1, 8>(wrapped, r.g, low); } else { shared_eight<T>(more, low); merge_below<8 / Eight<T>::W, Eight<T>::W>(wrapped, r.g, low); }
-          if (master) { shared32(more + gs * 8, low); merge_below<1, 8>(wrapped, r.p, low); } else { shared_eight<T>(more + gs * 8, low); merge_below<8 / Eight<T>::W, Eight<T>::W>(wrapped, r.p, low); }
+          if (grad32) { shared32(more, low); merge<8>(mask32, r.g, low); } else { shared_eight<T>(more, low); merge<Eight<T>::W>(mask_t, r.g, low); }
+          if (master) { shared32(more + gs * 8, low); merge<8>(mask32, r.p, low); } else { shared_eight<T>(more + gs * 8, low); merge<Eight<T>::W>(mask_t, r.p, low); }
           shared8(more + (gs + ps) * 8, low);
-          merge_below<4, 2>(wrapped, r.m, low);
+          merge<2>(mask8, r.m, low);
           shared8(more + (gs + ps) * 8 + 8, low);
-          merge_below<4, 2>(wrapped, r.v, low);
+          merge<2>(mask8, r.v, low);
           const uint32_t to = e - shift + i * 256;
           Written<T, BITS> o;
-          update<T, BITS, MIXED, 0>(set, r, grad32, master, part.place + to, wrapped, o);
+          update<T, BITS, MIXED, 0>(set, r, grad32, master, part.place + to, wrap, o);
           const bool open = i == wide.first;
-          if (master) put_shifted(part.master + (int)to, shift, lane, open, o.master, last.master);
-          put_shifted(static_cast<T*>(part.param) + (int)to, shift, lane, open, o.p, last.p);
-          put_shifted(static_cast<State*>(part.m) + (int)to, shift, lane, open, o.m, last.m);
-          put_shifted(static_cast<State*>(part.v) + (int)to, shift, lane, open, o.v, last.v);
+          if (master) put_shifted(part.master + (int)to, shift, lane, open, mask32, o.master, last.master);
+          put_shifted(static_cast<T*>(part.param) + (int)to, shift, lane, open, mask_t, o.p, last.p);
+          put_shifted(static_cast<State*>(part.m) + (int)to, shift, lane, open, mask8, o.m, last.m);
+          put_shifted(static_cast<State*>(part.v) + (int)to, shift, lane, open, mask8, o.v, last.v);
           if (lane == in_unit + i) { unit_sm = o.sm; unit_sv = o.sv; }
         }
         if (lane == 0 && wide.first < wide.end) {
@@ -518,7 +520,7 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
       take<State>(l, part.v, r.v);
       if (BITS == 8) { r.sm = part.m_scale[k.at / 256 + i]; r.sv = part.v_scale[k.at / 256 + i]; }
       Written<T, BITS> o;
-      update<T, BITS, MIXED, 32>(set, r, grad32, master, part.place + l.at, 0, o);
+      update<T, BITS, MIXED, 32>(set, r, grad32, master, part.place + l.at, nullptr, o);
       if (master) put<float>(l, part.master, o.master);
       put<T>(l, part.param, o.p);
       put<State>(l, part.m, o.m);
@@ -651,11 +653,11 @@ template <int N> int fill(Table<N>& table, const AdamPart* parts, int n, uint32_
 template <int N, typename Kernel, typename Scalars>
 cudaError_t start(Kernel kernel, const AdamPart* parts, int n, const Scalars& a, int ctas, size_t shared, cudaStream_t s) {
   Table<N> table;
-  // the longest units, up to eight blocks (whose scales fill a sector), with which every warp has eight
+  // the longest units, up to eight blocks (whose scales fill a sector), with which every warp has four
   long long blocks = 0;
   for (int i = 0; i < n; ++i) blocks += (parts[i].numel + 255) / 256;
   uint32_t unit = 2048;
-  while (unit > 256 && blocks * 256 < 8ll * unit * ctas * kAdamWarps) unit /= 2;
+  while (unit > 256 && blocks * 256 < 4ll * unit * ctas * kAdamWarps) unit /= 2;
   const int units = fill(table, parts, n, unit), want = (units + kAdamWarps - 1) / kAdamWarps;
   return launch(kernel, dim3((unsigned)(want < 1 ? 1 : want < ctas ? want : ctas)), kAdamThreads, shared, s, table, a);
 }
