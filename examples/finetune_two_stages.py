@@ -4,9 +4,11 @@ Each stage is a transformer layer: attention whose queries and keys go through `
 block through `aq_gated_ffn`.  The activation crosses from the first stage to the second as 4-bit differences
 (`aq_encode`, `aq_wire_copy`, `aq_decode`); the second stage ends in `aq_token_logprobs`, whose mean over the batch is the
 loss; the gradient of the activation travels back in 8 bits (`aq_quant_grad`, `aq_wire_copy_grad`, `aq_dequant_grad`).
-torch does the plain products, the softmax of the attention and the chain rule between the calls.
+torch does the plain products, the softmax of the attention and the chain rule between the calls.  With `--norm layer` the
+blocks begin with `aq_layer_norm` (which adds the residual in the same pass) instead of torch's RMS norm, and with
+`--optimizer adamw` or `adamw8` a step is `aq_grad_norm` and `aq_adamw`, clipped, with moments in 32 bits or in 8.
 
-    python examples/finetune_two_stages.py [--epochs N]
+    python examples/finetune_two_stages.py [--epochs N] [--norm rms|layer] [--optimizer torch|adamw|adamw8]
 
 The data are sequences of a made-up language in which every token has four possible successors: the loss of a guess is
 ln 96 = 4.56, that of a model that knows the language ln 4 = 1.39, and less as it comes to know the sequences themselves.
@@ -68,6 +70,29 @@ class QkNormRope(torch.autograd.Function):
         return None, None, dqkv, dwq.to(T), dwk.to(T), None, None
 
 
+class LayerNorm(torch.autograd.Function):
+    """(s, y): the sum of x and residual (x itself without one), and its norm."""
+
+    @staticmethod
+    def forward(ctx, stage, x, residual, w, b):
+        rows, d = x.shape
+        y, s = torch.empty_like(x), torch.empty_like(x) if residual is not None else None
+        mean, rstd = (torch.empty(rows, dtype=torch.float32, device="cuda") for _ in range(2))
+        aq.aq_layer_norm(stage, x, d, residual, d, w, b, EPS, rows, d, s, d, y, d, mean, rstd)
+        ctx.stage, ctx.alone = stage, residual is None
+        ctx.save_for_backward(x if s is None else s, w, mean, rstd)
+        return (x.view_as(x) if s is None else s), y
+
+    @staticmethod
+    def backward(ctx, ds, dy):
+        s, w, mean, rstd = ctx.saved_tensors
+        rows, d = s.shape
+        dx = torch.empty_like(s)
+        dw, db = (torch.empty(d, dtype=torch.float32, device="cuda") for _ in range(2))
+        aq.aq_layer_norm_grad(ctx.stage, dy.contiguous(), d, ds.contiguous(), d, s, d, w, mean, rstd, rows, d, dx, d, dw, db)
+        return None, dx, None if ctx.alone else dx, dw.to(T), db.to(T)
+
+
 class TokenLogprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, stage, logits, targets):
@@ -91,12 +116,17 @@ class TokenLogprobs(torch.autograd.Function):
 class Layer:
     """One stage's transformer layer; binary32 weights, used in bf16."""
 
-    def __init__(self, g):
+    def __init__(self, g, norm="rms"):
         wide = (HEADS + 2 * KEY_HEADS) * HEAD
         shapes = dict(qkv=(wide, HIDDEN), out=(HIDDEN, HEADS * HEAD), wg=(INNER, HIDDEN), wu=(INNER, HIDDEN), down=(HIDDEN, INNER))
         self.p = {n: (torch.randn(s, generator=g) / math.sqrt(s[1])).cuda().requires_grad_(True) for n, s in shapes.items()}
         for n in ("wq", "wk"):
             self.p[n] = torch.ones(HEAD, device="cuda").requires_grad_(True)
+        self.norm = norm
+        if norm == "layer":
+            for n in ("n1", "n2"):
+                self.p[n + "w"] = torch.ones(HIDDEN, device="cuda").requires_grad_(True)
+                self.p[n + "b"] = torch.zeros(HIDDEN, device="cuda").requires_grad_(True)
         angle = torch.arange(SEQ, dtype=torch.float64)[:, None] * 100.0 ** (-torch.arange(HEAD // 2, dtype=torch.float64) * 2 / HEAD)
         self.cos_sin = torch.cat([angle.cos(), angle.sin()], 1).float().cuda()
         self.shape = aq.QkShape(heads_q=HEADS, heads_k=KEY_HEADS, head_dim=HEAD, rot_dim=HEAD, interleaved=0, eps=EPS, n_positions=SEQ)
@@ -105,7 +135,10 @@ class Layer:
         """x [batch, seq, hidden] -> the same."""
         b, p = x.shape[0], {n: w.to(T) for n, w in self.p.items()}
         rms = lambda v: (v.float() * torch.rsqrt(v.float().square().mean(-1, keepdim=True) + EPS)).to(T)  # noqa: E731
-        rows = rms(x).reshape(b * SEQ, HIDDEN)
+        if self.norm == "layer":
+            stream, rows = LayerNorm.apply(stage, x.reshape(b * SEQ, HIDDEN), None, p["n1w"], p["n1b"])
+        else:
+            rows = rms(x).reshape(b * SEQ, HIDDEN)
         qkv = rows @ p["qkv"].T
         positions = torch.arange(SEQ, dtype=torch.int32, device="cuda").repeat(b)
         q, k = QkNormRope.apply(stage, self.shape, qkv, p["wq"], p["wk"], self.cos_sin, positions)
@@ -115,9 +148,47 @@ class Layer:
         score = (q @ k.transpose(-1, -2)).float() / math.sqrt(HEAD)
         score = score.masked_fill(torch.ones(SEQ, SEQ, device="cuda").triu(1).bool(), -math.inf)
         mixed = (score.softmax(-1).to(T) @ v).transpose(1, 2).reshape(b, SEQ, HEADS * HEAD)
+        if self.norm == "layer":
+            stream, rows = LayerNorm.apply(stage, (mixed @ p["out"].T).reshape(b * SEQ, HIDDEN), stream, p["n2w"], p["n2b"])
+            h = GatedFfn.apply(stage, rows, p["wg"], p["wu"])
+            return (stream + h @ p["down"].T).view(b, SEQ, HIDDEN)
         x = x + mixed @ p["out"].T
         h = GatedFfn.apply(stage, rms(x).reshape(b * SEQ, HIDDEN), p["wg"], p["wu"])
         return x + (h @ p["down"].T).view(b, SEQ, HIDDEN)
+
+
+class AdamW:
+    """The optimizer's step over all binary32 weights: their gradients' norm, its clipping factor and the update in two launches."""
+
+    def __init__(self, params, lr, state_bits):
+        self.stage = aq.aq_stage_create()
+        aq.aq_stage_configure(self.stage, aq.AQ_DTYPE, aq.AQ_FP32)
+        self.params = params
+        for p in params:
+            p.grad = torch.zeros_like(p)                         # stays where it is: backward passes add to it
+        zeros = lambda t, n=None: [torch.zeros(n(p) if n else p.numel(), dtype=t, device="cuda") for p in params]  # noqa: E731
+        if state_bits == 8:
+            blocks = lambda p: -(-p.numel() // 256)  # noqa: E731
+            self.state = dict(m=zeros(torch.float8_e4m3fn), v=zeros(torch.float8_e5m2), m_scale=zeros(torch.float32, blocks), v_scale=zeros(torch.float32, blocks))
+        else:
+            self.state = dict(m=zeros(torch.float32), v=zeros(torch.float32))
+        self.table = aq.aq_adam_table(self.stage, params=[p.detach() for p in params], grads=[p.grad for p in params],
+                                      weight_decay=[0.01 if p.dim() > 1 else 0.0 for p in params], **self.state)
+        self.config = aq.AdamwConfig(lr=lr, beta1=0.9, beta2=0.999, eps=1e-8, state_bits=state_bits)
+        self.norm, self.factor = (torch.empty(1, device="cuda") for _ in range(2))
+        self.count = torch.zeros(1, dtype=torch.int64, device="cuda")
+
+    def zero_grad(self):
+        for p in self.params:
+            p.grad.zero_()
+
+    def step(self):
+        aq.aq_grad_norm(self.stage, self.table, len(self.params), 1.0, 1.0, self.norm, self.factor, self.count)
+        aq.aq_adamw(self.stage, self.config, self.table, len(self.params), self.factor, None, self.count)
+
+    def close(self):
+        assert aq.aq_stage_status(self.stage) == 0
+        aq.aq_stage_destroy(self.stage)
 
 
 class Boundary:
@@ -167,13 +238,13 @@ def language(seed=0):
     return tokens.cuda()
 
 
-def train(epochs=20, lr=0.005, say=print):
+def train(epochs=20, lr=0.005, say=print, norm="rms", optimizer="torch"):
     """Losses of every step."""
     g = torch.Generator().manual_seed(1)
-    tokens, layers, boundary = language(), [Layer(g), Layer(g)], Boundary()
+    tokens, layers, boundary = language(), [Layer(g, norm), Layer(g, norm)], Boundary()
     embed, head = (0.3 * torch.randn(VOCAB, HIDDEN, generator=g)).cuda().requires_grad_(True), (torch.randn(VOCAB, HIDDEN, generator=g) / 12).cuda().requires_grad_(True)
     params = [embed, head] + [w for layer in layers for w in layer.p.values()]
-    adam = torch.optim.Adam(params, lr=lr)
+    adam = torch.optim.Adam(params, lr=lr) if optimizer == "torch" else AdamW(params, lr, 8 if optimizer == "adamw8" else 32)
     stage = aq.aq_stage_create()
     aq.aq_stage_configure(stage, aq.AQ_DTYPE, aq.AQ_BF16)
     losses = []
@@ -194,6 +265,8 @@ def train(epochs=20, lr=0.005, say=print):
         say(f"epoch {epoch}: loss {losses[-1]:.3f}, entropy {entropy.mean().item():.3f}")
     assert aq.aq_stage_status(stage) == 0
     aq.aq_stage_destroy(stage)
+    if optimizer != "torch":
+        adam.close()
     boundary.close()
     return losses
 
@@ -201,4 +274,7 @@ def train(epochs=20, lr=0.005, say=print):
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--epochs", type=int, default=20)
-    train(ap.parse_args().epochs)
+    ap.add_argument("--norm", choices=["rms", "layer"], default="rms")
+    ap.add_argument("--optimizer", choices=["torch", "adamw", "adamw8"], default="torch")
+    args = ap.parse_args()
+    train(args.epochs, norm=args.norm, optimizer=args.optimizer)

@@ -668,8 +668,9 @@ constexpr int kSmallTable = 24;
 template <typename T, int BITS, bool MIXED, int N> cudaError_t run_table(const AdamPart* parts, int n, const AdamScalars& a, int sms, cudaStream_t s) {
   constexpr int kBytes = BITS == 8 ? Ring<T, MIXED>::kBytes : 0;
   const auto kernel = adamw_kernel<T, BITS, MIXED, N>;
-  if (kBytes > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+  if (kBytes) {
+    static std::atomic<uint64_t> allowed{0};
+    const cudaError_t e = allow_shared(reinterpret_cast<const void*>(kernel), kBytes, allowed);
     if (e != cudaSuccess) return e;
   }
   return start<N>(kernel, parts, n, a, kAdamCtas * sms, kBytes, s);

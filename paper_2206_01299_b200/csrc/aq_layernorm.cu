@@ -642,7 +642,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) layer_norm_join_kernel(const 
 constexpr int kGradSmall = 64, kGradNarrow = 256, kGradWide = 512;   // threads of the CTAs that registers and shared memory are cut for
 constexpr int kGradRows = 2;                                  // rows at a time, where threads have eight elements
 constexpr int kSharedOfSm = 227 * 1024;
-struct GradPlan { int threads, most, each, period; bool warp, apart, edge; int bytes; long long parts; };
+struct GradPlan { int threads, most, each, period; bool warp, apart, edge; long long parts; };
 GradPlan grad_plan(const LayerNormGradArgs& a) {
   GradPlan p{};
   const int piece = 16 / a.size;
@@ -663,9 +663,9 @@ GradPlan grad_plan(const LayerNormGradArgs& a) {
   p.threads = p.warp ? 32 * kGradWalks : ((pieces + of_thread - 1) / of_thread + 31) / 32 * 32;
   const int rows = p.each == 8 ? kGradRows : 1;
   p.most = p.threads <= kGradSmall ? kGradSmall : p.threads <= kGradNarrow ? kGradNarrow : kGradWide;
-  p.bytes = p.most * kGradSlots * rows * 3 * of_thread * 16;
+  const int bytes = p.most * kGradSlots * rows * 3 * of_thread * 16;
   int per_sm = kGradWide / p.most * (p.most / p.threads);
-  if (per_sm > kSharedOfSm / (p.bytes + 2048)) per_sm = kSharedOfSm / (p.bytes + 2048);
+  if (per_sm > kSharedOfSm / (bytes + 2048)) per_sm = kSharedOfSm / (bytes + 2048);
   const int batch = rows * (p.warp ? kGradWalks : 1);
   const long long batches = (a.rows + batch - 1) / batch, most = (long long)per_sm * a.sms;
   // four batches to a CTA at least, if every multiprocessor has one all the same
@@ -678,11 +678,11 @@ GradPlan grad_plan(const LayerNormGradArgs& a) {
 template <typename T, bool EDGE, bool WARP, int R, int Q, int MAX, int CTAS> cudaError_t start_grad(LayerNormGradArgs a, const GradPlan& p, cudaStream_t s) {
   a.period = p.period;
   const auto kernel = layer_norm_grad_kernel<T, EDGE, WARP, R, Q, MAX, CTAS>;
-  if (p.bytes > 24 * 1024) {                                  // with the static arrays more than the 48 KB that need no asking
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.bytes);
-    if (e != cudaSuccess) return e;
-  }
-  return launch(kernel, dim3((unsigned)p.parts), dim3(p.threads), p.bytes, s, a);
+  constexpr int kBytes = MAX * kGradSlots * R * 3 * Q * 16;   // as grad_plan has it
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = allow_shared(reinterpret_cast<const void*>(kernel), kBytes, allowed);
+  if (e != cudaSuccess) return e;
+  return launch(kernel, dim3((unsigned)p.parts), dim3(p.threads), kBytes, s, a);
 }
 
 template <typename T, bool EDGE> cudaError_t run_walks(const LayerNormGradArgs& a, const GradPlan& p, cudaStream_t s) {

@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/aq_b200.h"
 
 namespace aq {
@@ -96,6 +98,18 @@ __device__ float2 add2(float2 a, float2 b) {
   float2 c;
   asm("{.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nadd.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;}" : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return c;
+}
+
+// Lets a kernel have that much dynamic shared memory, once a device; `allowed`: the devices that know, one such word to a kernel.
+inline cudaError_t allow_shared(const void* kernel, int bytes, std::atomic<uint64_t>& allowed) {
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = device < 64 ? 1ull << device : 0;
+  if (allowed.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 // A launch that may be placed while the stream's previous kernel drains (the kernels wait for its results themselves).

@@ -750,6 +750,43 @@ def test_two_handles_on_two_streams(aq):
         aq.aq_stage_destroy(h)
 
 
+def test_four_threads_with_a_handle_each(aq):
+    """Different widths and kinds of moments at once: what the threads share on the host is set once and for all sizes."""
+    import threading
+    results = {}
+
+    def work(i):
+        st = aq.aq_stage_create()
+        stream = torch.cuda.Stream()
+        aq.aq_stage_configure(st, aq.AQ_DTYPE, aq.AQ_BF16)
+        aq.aq_stage_configure(st, aq.AQ_STREAM, stream.cuda_stream)
+        try:
+            d = (264, 1600, 2056, 5000)[i]
+            s, _, w, _, dy, _ = norm_inputs(64, d, "bf16", seed=i)
+            mean, rstd = statistics(s)
+            with torch.cuda.stream(stream):
+                bufs = [v.cuda() for v in (dy, s, w, mean, rstd)] + [torch.empty((64, d), dtype=torch.bfloat16, device="cuda"), torch.empty(d, device="cuda"), torch.empty(d, device="cuda")]
+                tensors = Set([3000, 77], "bf16", "bf16", 8 if i % 2 else 32, bool(i // 2), False, seed=i)
+                stream.synchronize()
+                before, table = tensors.snapshot(), tensors.table(aq, st)
+                config = aq.AdamwConfig(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1, state_bits=tensors.bits)
+                for _ in range(20):
+                    aq.aq_layer_norm_grad(st, bufs[0], d, None, 0, bufs[1], d, bufs[2], bufs[3], bufs[4], 64, d, bufs[5], d, bufs[6], bufs[7])
+                aq.aq_adamw(st, config, table, 2, None, None, None)
+                stream.synchronize()
+                check_norm_grad("bf16", dy, None, s, w, mean, rstd, bufs[5:])
+                tensors.check(before, 1e-3, 1)
+            results[i] = "done"
+        finally:
+            aq.aq_stage_destroy(st)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert results == {i: "done" for i in range(4)}
+
+
 def test_step_of_a_tensor_beyond_32_bit_offsets(aq, stage):
     """2^31 + 4097 elements with moments in 8 bits: the last blocks, and the norm of all."""
     set_type(aq, stage, "bf16")
