@@ -510,7 +510,8 @@ int aq_qk_norm_rope_grad(aq_stage* st, const aq_qk_shape* shape, int64_t rows, c
  * may be null): what aq_layer_norm_grad needs, with s.  s is rounded to T, as it is stored, before the norm.  y may be x
  * or residual, and sum may be the other of the two or residual, where their row strides are equal.  hidden in 1..2^20, rows >= 0, element
  * alignment; rows of whole 16-byte pieces on 16-byte boundaries are the fast ones.  A row with a NaN or an infinity has NaN in mean, rstd and y or
- * parts of them, and touches no other row; with eps 0 so has a row of equal values.
+ * parts of them, and touches no other row; with eps 0 so has a row of equal values.  Squares are binary32: a row with elements 1e19 and more
+ * from its mean has rstd 0.
  */
 int aq_layer_norm(aq_stage* st, const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* w, const void* b, float eps,
                   int64_t rows, int hidden, void* sum, int64_t lds, void* y, int64_t ldy, float* mean, float* rstd);
@@ -521,7 +522,8 @@ int aq_layer_norm(aq_stage* st, const void* x, int64_t ldx, const void* residual
  * dy T[rows][lddy] (in); dsum T[rows][ldds] (in; may be null): the gradient that reaches s past the norm, along the residual
  * stream; s (the stored sum, or x without a residual), mean, rstd as aq_layer_norm left them.  dx T[rows][lddx] (out; may be null) is
  * the gradient of x and of residual alike; it may be dy, dsum or s, where the row strides are equal.  dw, db float[hidden] (out; each may be null).
- * Sums of dw and db are kept in the handle's workspace, which grows as aq_gated_ffn_grad says.
+ * A row with a NaN or an infinity makes dw and db NaN, and its own dx.  Sums of dw and db are kept in the handle's workspace, which grows
+ * as aq_gated_ffn_grad says.
  */
 int aq_layer_norm_grad(aq_stage* st, const void* dy, int64_t lddy, const void* dsum, int64_t ldds, const void* s, int64_t lds, const void* w,
                        const float* mean, const float* rstd, int64_t rows, int hidden, void* dx, int64_t lddx, float* dw, float* db);
@@ -568,7 +570,7 @@ typedef struct {
  * p is the master where there is one, and param its value rounded to T; otherwise param.  factor float[1], d_lr float[1],
  * d_step int64[1] (in, device; each may be null): the gradients' factor (1 without), and the learning rate and step in the settings'
  * place, which a captured graph reads anew at every replay (a step below 1 counts as 1).  A factor that is not finite leaves every
- * tensor as it is.
+ * tensor as it is.  The quotient is within 2^-20 of its value; a v below 1.2e-38 counts as zero in it.
  * Moments in 8 bits: a block of 256 elements has a power of two as its scale, the smallest that keeps its largest magnitude in
  * the format's range (e4m3 up to 448, e5m2 up to 57344).  p goes by the new m and v as they are before they are stored.  Stored, a value becomes one of its two
  * neighbours in the format, the upper with the probability of its place between them: when that place, in 65536ths, and a random

@@ -573,17 +573,24 @@ __global__ void __launch_bounds__(kColumns * kWalks) layer_norm_columns_kernel(c
   const int column = blockIdx.x * kColumns + threadIdx.x, at = min(column, a.hidden - 1);
   next_may_launch();
   wait_for_previous();
-  float dw = 0.0f, db = 0.0f;
+  double total_w = 0.0, total_b = 0.0;                         // of up to 64 rows' sums in binary32 each
   const T* const s = static_cast<const T*>(a.s) + at;
   const T* const g = static_cast<const T*>(a.dy) + at;
-#pragma unroll 4
-  for (long long row = (long long)blockIdx.y * kWalks + threadIdx.y; row < a.rows; row += (long long)gridDim.y * kWalks) {
-    const float n = (Scalar<T>::open(s[row * a.lds]) - __ldg(a.mean + row)) * __ldg(a.rstd + row), dy = Scalar<T>::open(g[row * a.lddy]);
-    dw = fmaf(dy, n, dw);
-    db += dy;
+  const long long step = (long long)gridDim.y * kWalks;
+  for (long long row = (long long)blockIdx.y * kWalks + threadIdx.y; row < a.rows;) {
+    float dw = 0.0f, db = 0.0f;
+    const int n_rows = (int)min((a.rows - row + step - 1) / step, 64ll);
+#pragma unroll 8
+    for (int i = 0; i < n_rows; ++i, row += step) {
+      const float n = (Scalar<T>::open(s[row * a.lds]) - __ldg(a.mean + row)) * __ldg(a.rstd + row), dy = Scalar<T>::open(g[row * a.lddy]);
+      dw = fmaf(dy, n, dw);
+      db += dy;
+    }
+    total_w += (double)dw;
+    total_b += (double)db;
   }
-  sums[0][threadIdx.y][threadIdx.x] = dw;
-  sums[1][threadIdx.y][threadIdx.x] = db;
+  sums[0][threadIdx.y][threadIdx.x] = (float)total_w;
+  sums[1][threadIdx.y][threadIdx.x] = (float)total_b;
   __syncthreads();
   if (threadIdx.y < 2 && column < a.hidden) {
     float x = 0.0f;
@@ -606,13 +613,21 @@ __global__ void __launch_bounds__(kRowThreads) layer_norm_rows_kernel(const Laye
   const T* const w = static_cast<const T*>(a.w);
   T* const dx = static_cast<T*>(a.dx) + row * a.lddx;
   const float mean = a.mean[row], rstd = a.rstd[row];
-  float sum_g = 0.0f, sum_gn = 0.0f;
-  for (int j = threadIdx.x; j < a.hidden; j += kRowThreads) {
-    const float n = (Scalar<T>::open(s[j]) - mean) * rstd, g = Scalar<T>::open(dy[j]) * (w ? Scalar<T>::open(w[j]) : 1.0f);
-    sum_g += g;
-    sum_gn = fmaf(g, n, sum_gn);
+  double total_g = 0.0, total_gn = 0.0;                        // of up to 64 elements' sums in binary32 each: rows are as wide as 2^20
+  for (int j = threadIdx.x; j < a.hidden;) {
+    float sum_g = 0.0f, sum_gn = 0.0f;
+    const int n_columns = min((a.hidden - j + kRowThreads - 1) / kRowThreads, 64);
+#pragma unroll 8
+    for (int i = 0; i < n_columns; ++i, j += kRowThreads) {
+      const float n = (Scalar<T>::open(s[j]) - mean) * rstd, g = Scalar<T>::open(dy[j]) * (w ? Scalar<T>::open(w[j]) : 1.0f);
+      sum_g += g;
+      sum_gn = fmaf(g, n, sum_gn);
+    }
+    total_g += (double)sum_g;
+    total_gn += (double)sum_gn;
   }
-  const float c1 = cta_sum<kRowThreads / 32>(sum_g, shared[0]) / a.hidden, c2 = cta_sum<kRowThreads / 32>(sum_gn, shared[1]) / a.hidden;
+  const float c1 = cta_sum<kRowThreads / 32>((float)total_g, shared[0]) / a.hidden, c2 = cta_sum<kRowThreads / 32>((float)total_gn, shared[1]) / a.hidden;
+#pragma unroll 4
   for (int j = threadIdx.x; j < a.hidden; j += kRowThreads) {
     const float n = (Scalar<T>::open(s[j]) - mean) * rstd, g = Scalar<T>::open(dy[j]) * (w ? Scalar<T>::open(w[j]) : 1.0f);
     const float o = rstd * (g - fmaf(n, c2, c1));

@@ -128,7 +128,7 @@ constexpr uint32_t kPartMost = 1u << 30;
 constexpr uint32_t kPartWide = 1;         // every address is a multiple of eight elements, or as many elements behind one as flags >> kPartShiftBit says
 constexpr int kPartShiftBit = 8;          // with 8-bit moments only, whose blocks are counted from the tensor's beginning
 constexpr uint32_t kPartGradF32 = 2;      // the gradient is binary32 beside 16-bit parameters
-constexpr int kAdamTable = 400;           // tensors of a launch: 72 bytes each and 8 of a running count, of 32764 bytes of arguments
+constexpr int kAdamTable = 400;           // tensors of a launch: 72 bytes each and 4 of a running count, of 32764 bytes of arguments
 
 struct AdamScalars {
   float beta1, rest1, beta2, rest2, one;  // rest: 1 - beta; one: 1

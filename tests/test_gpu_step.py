@@ -311,6 +311,23 @@ def test_layer_norm_in_place(aq, stage, dtype, rows, d):
         assert torch.equal(a[name], dx) and torch.equal(dw, dw1) and torch.equal(db, db1), name
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_layer_norm_of_the_widest_rows(aq, stage, dtype):
+    set_type(aq, stage, dtype)
+    x, r, w, b, dy, dsum = norm_inputs(2, 2 ** 20, dtype, seed=7)
+    s, y, mean, rstd = run_norm(aq, stage, dtype, x, r, w, b, 1e-5)
+    check_norm(dtype, s, w, b, 1e-5, y, mean, rstd)
+    mean, rstd = statistics(s)
+    check_norm_grad(dtype, dy, dsum, s, w, mean, rstd, run_norm_grad(aq, stage, dtype, dy, dsum, s, w, mean, rstd))
+
+
+def test_layer_norm_grad_of_many_rows_that_begin_anywhere(aq, stage):
+    set_type(aq, stage, "fp32")
+    s, _, w, _, dy, dsum = norm_inputs(300000, 5, "fp32", seed=8)
+    mean, rstd = statistics(s)
+    check_norm_grad("fp32", dy, dsum, s, w, mean, rstd, run_norm_grad(aq, stage, "fp32", dy, dsum, s, w, mean, rstd, 0, 3))
+
+
 def test_layer_norm_grad_against_differences(aq, stage):
     """The kernels' own forward pass moved along a direction, in binary32: the slope of sum(dy y) + sum(dsum s).  With h = 2^-7 the difference
     is off by h^2 / 6 of the third derivative (a few times the sum: 1e-4) and the roundings of y, 1e-7 |y| / h."""
