@@ -20,9 +20,10 @@
 // its place between the two and a random fraction add up to one, 16 bits each for m and v from a hash of the element's index and the step
 // (two multiplications; a Weyl sequence over the steps is cheaper, but what v becomes depends on the sequence's past, and
 // v then falls 13 percent too fast).  In the bits of a binary32 that is one addition below the last bit that is kept.
-// This step's p goes by the m and v before they are rounded.  A block's values come through a ring in shared memory (loads ahead in registers
-// are put off by the compiler until they are needed: 1080 us), and the scales of eight blocks leave as one sector (a scale at a time: 130 us more).  The products and sums of m and v are rounded one by one (no
-// fused multiply-add), so that the stored codes are a matter of the formula and not of the compiler.
+// This step's p goes by the m and v before they are rounded.  The products and sums of m and v are rounded one by one (no fused
+// multiply-add), so that the stored codes are a matter of the formula and not of the compiler.  A block's values come through a ring in
+// shared memory (loads ahead in registers are put off by the compiler until they are needed: 1080 us), and the scales of eight blocks
+// leave as one sector (a scale at a time: 130 us more).
 
 #include "aq_stage.h"
 #include "aq_stage_device.cuh"

@@ -732,6 +732,50 @@ def test_step_in_a_captured_graph(aq, stage):
         del graph
 
 
+def test_layer_norm_in_a_captured_graph(aq, stage):
+    """The norm and its gradient, captured after one call that grew the workspace; a larger call in between takes another, and the
+    graph goes on with its own.  Without the call before, a capture is refused."""
+    set_type(aq, stage, "bf16")
+    rows, d = 300, 768
+    x, r, w, b, dy, dsum = norm_inputs(rows, d, "bf16", seed=9)
+    c = {n: v.cuda() for n, v in dict(x=x, r=r, w=w, b=b, dy=dy, dsum=dsum).items()}
+    s, y, dx = (torch.empty_like(c["x"]) for _ in range(3))
+    mean, rstd, dw, db = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+
+    def call():
+        aq.aq_layer_norm(stage, c["x"], d, c["r"], d, c["w"], c["b"], 1e-5, rows, d, s, d, y, d, mean, rstd)
+        aq.aq_layer_norm_grad(stage, c["dy"], d, c["dsum"], d, s, d, c["w"], mean, rstd, rows, d, dx, d, dw, db)
+
+    def capture():
+        graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            aq.aq_stage_configure(stage, aq.AQ_STREAM, torch.cuda.current_stream().cuda_stream)
+            try:
+                call()
+            finally:
+                aq.aq_stage_configure(stage, aq.AQ_STREAM, 0)
+        return graph
+    with pytest.raises(aq.AqError) as e:
+        capture()
+    assert e.value.code == aq.AQ_EUNSUPPORTED
+    call()
+    graph = capture()
+    wide = torch.zeros((600, 4096), dtype=torch.bfloat16, device="cuda")
+    f = torch.zeros(4096, device="cuda")
+    aq.aq_layer_norm_grad(stage, wide, 4096, None, 0, wide, 4096, None, torch.zeros(600, device="cuda"), torch.ones(600, device="cuda"), 600, 4096, wide, 4096, f, f.clone())
+    c["x"].mul_(0.5)
+    c["dy"].mul_(2.0)
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    total = (c["x"].cpu().float() + r.float()).bfloat16()
+    assert torch.equal(s.cpu(), total)
+    check_norm("bf16", total, w, b, 1e-5, y, mean, rstd)
+    check_norm_grad("bf16", c["dy"], dsum, total, w, mean, rstd, (dx, dw, db))
+    del graph
+
+
 def test_two_handles_on_two_streams(aq):
     """Calls on two handles at once, each on its own stream, give what each gives alone."""
     handles = [aq.aq_stage_create() for _ in range(2)]
