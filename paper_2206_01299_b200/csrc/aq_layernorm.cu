@@ -18,7 +18,8 @@
 // the barrier instead of keeping them (89 us), one row or four at a time (106 us, 87 us), a thread's copies side by side in shared memory (115 us).
 // Rows that begin inside a piece: forward a row's pieces are those of the grid it lies on, the first and last by elements; backward a CTA takes
 // every `period`-th row, which begin alike, so that its columns stay.  16384 x 1601 fp16: 80 us and 52 us (one element at a time: 217 and 152).
-// Rows of operands that begin differently, and rows over 8192 elements backward or 4096 pieces forward, go through kernels that read them again.
+// Backward, rows over 8192 elements are read once for the columns' sums and once for dx (4096 x 12000 fp16: 126 us, element by element 269). Rows of
+// operands that begin differently, and forward rows over 4096 pieces, go element by element through kernels that read them again.
 
 #include "aq_stage.h"
 #include "aq_stage_device.cuh"
@@ -635,6 +636,142 @@ __global__ void __launch_bounds__(kRowThreads) layer_norm_rows_kernel(const Laye
   }
 }
 
+// The same for wide rows on 16-byte boundaries: a lane has a piece of 16 bytes, the warps of a CTA take rows in turn.
+constexpr int kStripWarps = 8;
+template <typename T>
+__global__ void __launch_bounds__(32 * kStripWarps) layer_norm_strips_kernel(const LayerNormGradArgs a) {
+  using Ps = Pairs<T>;
+  constexpr int H = Ps::N, N = 2 * H;
+  __shared__ float2 sums[2][kStripWarps][32 * H];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, column = (blockIdx.x * 32 + lane) * N;
+  const int hi = min(max(a.hidden - column, 0), N);
+  next_may_launch();
+  wait_for_previous();
+  float2 total_w[H], total_b[H];                              // of up to 64 rows' sums each
+#pragma unroll
+  for (int j = 0; j < H; ++j) total_w[j] = total_b[j] = make_float2(0.0f, 0.0f);
+  const long long step = (long long)gridDim.y * kStripWarps;
+  auto walk = [&](auto load) {                                // load: a piece of a row
+    for (long long row = (long long)blockIdx.y * kStripWarps + warp; row < a.rows;) {
+      float2 dw[H], db[H];
+#pragma unroll
+      for (int j = 0; j < H; ++j) dw[j] = db[j] = make_float2(0.0f, 0.0f);
+      const int rows = (int)min((a.rows - row + step - 1) / step, 64ll);
+#pragma unroll 4
+      for (int i = 0; i < rows; ++i, row += step) {
+        float2 n[H], y[H];
+        load(static_cast<const T*>(a.s) + row * a.lds + column, n);
+        load(static_cast<const T*>(a.dy) + row * a.lddy + column, y);
+        const float mean = __ldg(a.mean + row), rstd = __ldg(a.rstd + row);
+#pragma unroll
+        for (int j = 0; j < H; ++j) {
+          n[j] = mul2(add2(n[j], both(-mean)), both(rstd));
+          dw[j] = fma2(y[j], n[j], dw[j]);
+          db[j] = add2(db[j], y[j]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < H; ++j) {
+        total_w[j] = add2(total_w[j], dw[j]);
+        total_b[j] = add2(total_b[j], db[j]);
+      }
+    }
+  };
+  if (hi == N) {
+    walk([](const T* p, float2* f) { Ps::open(__ldg(reinterpret_cast<const uint4*>(p)), f); });
+  } else if (hi) {
+    walk([hi](const T* p, float2* f) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) (j & 1 ? f[j / 2].y : f[j / 2].x) = j < hi ? Scalar<T>::open(p[j]) : 0.0f;
+    });
+  }
+#pragma unroll
+  for (int j = 0; j < H; ++j) { sums[0][warp][lane * H + j] = total_w[j]; sums[1][warp][lane * H + j] = total_b[j]; }
+  __syncthreads();
+  const int padded = padded_hidden(a.hidden);
+  for (int e = threadIdx.x; e < 2 * 32 * N; e += 32 * kStripWarps) {
+    const int t = e >= 32 * N, j = e - t * 32 * N, c = blockIdx.x * 32 * N + j;
+    if (c >= a.hidden) continue;
+    float x = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kStripWarps; ++i) x += reinterpret_cast<const float*>(sums[t][i])[j];
+    a.partials[((long long)blockIdx.y * 2 + t) * padded + c] = x;
+  }
+}
+
+// dx of wide rows that begin alike in all operands: a CTA has a row in registers, P pieces of 16 bytes to a thread.  Without EDGE they are whole
+// pieces on 16-byte boundaries, and so is w.
+constexpr int kWideThreads = 512;
+template <typename T, bool EDGE, int P>
+__global__ void __launch_bounds__(kWideThreads) layer_norm_wide_kernel(const LayerNormGradArgs a) {
+  using Pc = Piece<T, true>;
+  constexpr int N = Pc::N, kStep = kWideThreads * N;
+  __shared__ float shared[2][kWideThreads / 32];
+  next_may_launch();
+  wait_for_previous();
+  const long long row = blockIdx.x;
+  const T* const s = static_cast<const T*>(a.s) + row * a.lds;
+  const T* const dy = static_cast<const T*>(a.dy) + row * a.lddy;
+  const T* const skip = a.dsum ? static_cast<const T*>(a.dsum) + row * a.ldds : nullptr;
+  const T* const wt = static_cast<const T*>(a.w);
+  T* const dx = static_cast<T*>(a.dx) + row * a.lddx;
+  const int first = (int)threadIdx.x * N - (EDGE ? (int)(reinterpret_cast<uintptr_t>(s) / sizeof(T) % N) : 0);
+  auto at = [&](int i) { return first + i * kStep; };
+  auto lo = [&](int i) { return EDGE ? -at(i) : 0; };
+  auto hi = [&](int i) { return EDGE ? a.hidden - at(i) : N; };
+  auto weights = [&](int i, float* w) {
+    if (!wt) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) w[j] = 1.0f;
+    } else if (EDGE) {
+      load_weights<Pc>(wt, at(i), a.hidden, w);
+    } else {
+      Pc::open(Pc::load(wt + at(i)), w);
+    }
+  };
+  typename Pc::Raw vs[P], vy[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    if (at(i) >= a.hidden) continue;
+    vs[i] = load_piece<Pc>(s + at(i), lo(i), hi(i));
+    vy[i] = load_piece<Pc>(dy + at(i), lo(i), hi(i));
+  }
+  const float mean = __ldg(a.mean + row), rstd = __ldg(a.rstd + row);
+  float sum_g = 0.0f, sum_gn = 0.0f;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    if (at(i) >= a.hidden) continue;
+    float f[N], g[N], w[N];
+    Pc::open(vs[i], f);
+    Pc::open(vy[i], g);
+    weights(i, w);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {                              // elements around the row have dy of zero
+      g[j] *= w[j];
+      sum_g += g[j];
+      sum_gn = fmaf(g[j], (f[j] - mean) * rstd, sum_gn);
+    }
+  }
+  const float inverse = 1.0f / (float)a.hidden;
+  const float c1 = cta_sum<kWideThreads / 32>(sum_g, shared[0]) * inverse, c2 = cta_sum<kWideThreads / 32>(sum_gn, shared[1]) * inverse;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    if (at(i) >= a.hidden) continue;
+    float f[N], g[N], w[N];
+    Pc::open(vs[i], f);
+    Pc::open(vy[i], g);
+    weights(i, w);
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = rstd * (g[j] * w[j] - fmaf((f[j] - mean) * rstd, c2, c1));
+    if (skip) {
+      Pc::open(load_piece<Pc>(skip + at(i), lo(i), hi(i)), g);
+#pragma unroll
+      for (int j = 0; j < N; ++j) f[j] += g[j];
+    }
+    store_piece<Pc>(dx + at(i), Pc::close(f), lo(i), hi(i));
+  }
+}
+
 // dw and db from the sums of the CTAs: a warp's lanes take neighbouring columns, the warps of a CTA every kJoinWarps-th row of sums.
 constexpr int kJoinWarps = 16;
 __global__ void __launch_bounds__(32 * kJoinWarps) layer_norm_join_kernel(const float* partials, int parts, int hidden, float* dw, float* db) {
@@ -674,7 +811,8 @@ GradPlan grad_plan(const LayerNormGradArgs& a) {
   p.each = span <= 8 * kGradNarrow ? 8 : 16;
   p.apart = a.rows_at == kRowsAny || span > 16 * kGradWide;
   if (p.apart) {
-    const long long strips = (a.hidden + kColumns - 1) / kColumns, walks = (a.rows + kWalks - 1) / kWalks;
+    const int columns = a.rows_at == kRowsWhole ? 32 * piece : kColumns, of_cta = a.rows_at == kRowsWhole ? kStripWarps : kWalks;
+    const long long strips = (a.hidden + columns - 1) / columns, walks = (a.rows + of_cta - 1) / of_cta;
     const long long most = (8ll * a.sms + strips - 1) / strips;
     p.parts = walks < most ? walks : most;
     return p;
@@ -716,12 +854,26 @@ template <typename T, bool EDGE> cudaError_t run_walks(const LayerNormGradArgs& 
 }
 
 template <typename T> cudaError_t run_grad(const LayerNormGradArgs& a, cudaStream_t s) {
+  constexpr int kPiece = 16 / sizeof(T);
   const GradPlan p = grad_plan(a);
   const bool sums = a.dw || a.db;
   cudaError_t e = cudaSuccess;
-  if (p.apart) {
-    if (sums) e = launch(layer_norm_columns_kernel<T>, dim3((unsigned)((a.hidden + kColumns - 1) / kColumns), (unsigned)p.parts), dim3(kColumns, kWalks), 0, s, a);
-    if (e == cudaSuccess && a.dx) e = launch(layer_norm_rows_kernel<T>, dim3((unsigned)a.rows), dim3(kRowThreads), 0, s, a);
+  if (p.apart) {                                              // dw and db before dx, which may be dy or s
+    if (sums && a.rows_at == kRowsWhole) {
+      e = launch(layer_norm_strips_kernel<T>, dim3((unsigned)((a.hidden + 32 * kPiece - 1) / (32 * kPiece)), (unsigned)p.parts), dim3(32 * kStripWarps), 0, s, a);
+    } else if (sums) {
+      e = launch(layer_norm_columns_kernel<T>, dim3((unsigned)((a.hidden + kColumns - 1) / kColumns), (unsigned)p.parts), dim3(kColumns, kWalks), 0, s, a);
+    }
+    if (e == cudaSuccess && a.dx) {
+      const bool whole = a.rows_at == kRowsWhole && a.hidden % kPiece == 0 && reinterpret_cast<uintptr_t>(a.w) % 16 == 0;
+      const int span = a.hidden + kPiece - 1;
+      const dim3 rows((unsigned)a.rows), threads(kWideThreads);
+      if (whole && a.hidden <= 4 * kWideThreads * kPiece) e = launch(layer_norm_wide_kernel<T, false, 4>, rows, threads, 0, s, a);
+      else if (whole && a.hidden <= 8 * kWideThreads * kPiece) e = launch(layer_norm_wide_kernel<T, false, 8>, rows, threads, 0, s, a);
+      else if (a.rows_at != kRowsAny && span <= 4 * kWideThreads * kPiece) e = launch(layer_norm_wide_kernel<T, true, 4>, rows, threads, 0, s, a);
+      else if (a.rows_at != kRowsAny && span <= 8 * kWideThreads * kPiece) e = launch(layer_norm_wide_kernel<T, true, 8>, rows, threads, 0, s, a);
+      else e = launch(layer_norm_rows_kernel<T>, dim3((unsigned)a.rows), dim3(kRowThreads), 0, s, a);
+    }
   } else {
     e = p.edge ? run_walks<T, true>(a, p, s) : run_walks<T, false>(a, p, s);
   }

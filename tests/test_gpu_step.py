@@ -216,7 +216,7 @@ def test_layer_norm_grad(aq, stage, dtype, d):
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
 @pytest.mark.parametrize("rows,d,pad", [(5000, 768, 0), (3001, 1600, 0), (3001, 1600, 4), (2000, 1021, 0), (2000, 1021, 3), (20011, 24, 0), (20011, 24, 1), (700, 5000, 0),
-                                        (700, 5001, 1), (301, 12000, 0), (9000, 3, 0), (1500, 250, 1), (1500, 2045, 0), (900, 8190, 0)])
+                                        (700, 5001, 1), (301, 12000, 0), (9000, 3, 0), (1500, 250, 1), (1500, 2045, 0), (900, 8190, 0), (1200, 8201, 7), (300, 12001, 0), (5000, 8200, 0)])
 def test_layer_norm_grad_many_rows(aq, stage, dtype, rows, d, pad):
     set_type(aq, stage, dtype)
     s, _, w, _, dy, dsum = norm_inputs(rows, d, dtype, seed=2)
