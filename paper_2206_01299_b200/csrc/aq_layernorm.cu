@@ -394,9 +394,10 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
   float2 w[Q][H], dw[Q][H], db[Q][H];
 #pragma unroll
   for (int q = 0; q < Q; ++q) {
-    column[q] = (WARP ? lane + 32 * q : (int)(threadIdx.x + q * blockDim.x)) * N - shift;
-    lo[q] = EDGE ? max(-column[q], 0) : 0;
-    hi[q] = min(max(a.hidden - column[q], 0), N);
+    const NormPiece piece = norm_piece(WARP ? lane + 32 * q : (int)(threadIdx.x + q * blockDim.x), N, shift, a.hidden);
+    column[q] = piece.column;
+    lo[q] = EDGE ? piece.lo : 0;
+    hi[q] = piece.hi;
 #pragma unroll
     for (int j = 0; j < H; ++j) w[q][j] = dw[q][j] = db[q][j] = make_float2(0.0f, 0.0f);
 #pragma unroll
@@ -422,7 +423,7 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
       const long long r = i * period;
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
-        const int bytes = hi[q] * (int)sizeof(T), at = bytes ? column[q] : 0;   // a thread without elements reads nothing, from a valid address
+        const int bytes = hi[q] * (int)sizeof(T), at = norm_copy_from(column[q], hi[q], shift);
         const uint32_t to = there + i * kRow + q * kPart;
         copy16(to, s + r * a.lds + at, bytes);
         copy16(to + Q * kPart, g + r * a.lddy + at, bytes);

@@ -112,6 +112,17 @@ struct LayerNormGradArgs {
   int size, sms;                          // size: of an element
 };
 
+// The `index`-th piece of n elements of a row of the layer norm's gradient.  Rows begin `shift` elements behind a 16-byte boundary and pieces lie on
+// boundaries, so the first one's column is -shift; of a piece's elements [lo, hi) are the row's, none where hi is 0.
+struct NormPiece { int column, lo, hi; };
+__host__ __device__ inline NormPiece norm_piece(int index, int n, int shift, int hidden) {
+  const int column = index * n - shift, rest = hidden - column;
+  return {column, column < 0 ? -column : 0, rest < 0 ? 0 : rest < n ? rest : n};
+}
+// Column from which the asynchronous copy of a piece's first hi elements begins.  The copy of none has to begin on a boundary as well, which a
+// shifted row itself does not.
+__host__ __device__ inline int norm_copy_from(int column, int hi, int shift) { return hi ? column : -shift; }
+
 // A tensor of a step, or a part of a long one, as the kernels read it.
 struct AdamPart {
   void* param;
