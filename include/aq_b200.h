@@ -539,7 +539,7 @@ typedef struct {
   float* master;          /* [numel] binary32 copy that the step works on (in/out), or null; null with AQ_FP32 */
   const void* grad;       /* [numel] */
   void *m, *v;            /* [numel] moments (in/out): float, or e4m3 codes of m and e5m2 codes of v; zeros before the first step */
-  float *m_scale, *v_scale; /* float[ceil(numel / 256)] (in/out) with 8-bit moments: what a block's codes are multiplied by */
+  float *m_scale, *v_scale; /* float[ceil(numel / 256)] (in/out) with 8-bit moments: what a block's codes are multiplied by; null with 32 */
   int64_t numel;
   float weight_decay;     /* >= 0 */
   int32_t grad_dtype;     /* the handle's element type, or AQ_FP32 */

@@ -445,6 +445,7 @@ def aq_adam_table(st, grads, params=None, masters=None, m=None, v=None, m_scale=
             setattr(row, name, _whole(x, x.dtype))
             if name != "grad" and size:
                 written.append((x.data_ptr(), x.data_ptr() + x.numel() * x.element_size()))
+        assert not narrow or not (row.m or row.v) or (row.m_scale and row.v_scale), f"tensor {i} has 8-bit moments without m_scale or v_scale"
     written.sort()
     assert all(a[1] <= b[0] for a, b in zip(written, written[1:])), "two tensors overlap: one that layers share is listed once"
     return table

@@ -197,6 +197,8 @@ int check_adam_state(aq_stage* st, const char* who, int64_t i, const aq_adam_ten
   if (!t.m || !t.v || (bits == 32 && (misaligned(t.m, 4) || misaligned(t.v, 4)))) return fail(st, AQ_EINVAL, "%s: tensor %lld: m or v is null or misaligned", who, (long long)i);
   if (bits == 8 && (!t.m_scale || !t.v_scale || misaligned(t.m_scale, 4) || misaligned(t.v_scale, 4)))
     return fail(st, AQ_EINVAL, "%s: tensor %lld: m_scale or v_scale is null or misaligned", who, (long long)i);
+  // with scales, m and v are codes, a quarter of what a step of 32 bits reads and writes
+  if (bits == 32 && (t.m_scale || t.v_scale)) return fail(st, AQ_EINVAL, "%s: tensor %lld: m_scale and v_scale belong to state_bits 8", who, (long long)i);
   return AQ_OK;
 }
 
