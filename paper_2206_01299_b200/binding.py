@@ -421,6 +421,7 @@ def aq_adam_table(st, grads, params=None, masters=None, m=None, v=None, m_scale=
     tensors; weight_decay is a number for all of them or a list.  Moments in 8 bits are torch.float8_e4m3fn (m) and torch.float8_e5m2 (v) or
     their bytes as torch.uint8, with m_scale and v_scale.  The array holds addresses: it can be kept for as long as the
     tensors keep their places, and does not keep them alive.  Lay it out anew where gradients are allocated in every step.
+    aq_adamw refuses it with a handle of another element type.
     """
     import torch
     t, n = _stage_types.get(st), len(grads)
@@ -432,6 +433,7 @@ def aq_adam_table(st, grads, params=None, masters=None, m=None, v=None, m_scale=
     decay = [weight_decay] * n if isinstance(weight_decay, (int, float)) else weight_decay
     assert len(decay) == n and all(c is None or len(c) == n for c in columns.values()), "lists of different lengths"
     table = (AdamTensor * n)()
+    table.element_type = t                              # the parameters'; nothing in the structure tells it
     written = []
     for i, row in enumerate(table):
         row.numel, row.weight_decay, row.grad_dtype = grads[i].numel(), decay[i], codes[grads[i].dtype]
@@ -466,5 +468,8 @@ def aq_grad_norm(st, tensors, n, inv_scale, max_norm, norm, factor, step):
 
 def aq_adamw(st, config, tensors, n, factor, d_lr, d_step):
     """config: an AdamwConfig; tensors: an array of AdamTensor, or its address."""
+    t, laid_out = _stage_types.get(st), getattr(tensors, "element_type", None)
+    if laid_out is not t and laid_out is not None and t is not None:
+        raise AqError(AQ_EINVAL, f"aq_adamw: the table was laid out for parameters of {laid_out}, the handle's type is {t}")
     rc = (_lib or lib()).aq_adamw(st, C.addressof(config), _table(tensors, n), n, _whole(factor, _f32), _whole(d_lr, _f32), _whole(d_step, _i64))
     return rc and _stage_error(st, rc)

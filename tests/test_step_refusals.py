@@ -66,3 +66,49 @@ def test_8_bit_moments_without_scales_are_refused(stage):
             aq.aq_adam_table(st, **dict(c, **change))
     empty = {n: [Flat(x[0].dtype, 0, 0)] for n, x in c.items()}
     aq.aq_adam_table(st, **dict(empty, m_scale=[None], v_scale=[None]))
+
+
+def columns(t, grads, master=False):
+    f = torch.float32
+    out = dict(params=[Flat(t, 300, 1 << 20)], grads=[Flat(grads, 300, 2 << 20)], m=[Flat(f, 300, 4 << 20)], v=[Flat(f, 300, 5 << 20)])
+    return dict(out, masters=[Flat(f, 300, 3 << 20)]) if master else out
+
+
+TYPES = {aq.AQ_FP16: torch.float16, aq.AQ_BF16: torch.bfloat16, aq.AQ_FP32: torch.float32}
+
+
+@pytest.mark.parametrize("laid_out", TYPES)
+@pytest.mark.parametrize("taken", TYPES)
+def test_a_table_of_another_element_type_is_refused(stage, laid_out, taken):
+    """Binary32 gradients fit every handle, but the parameters' type is the handle's and stands nowhere in the array: 16-bit parameters would be
+    taken for binary32 ones, twice their size."""
+    st, recorder = stage
+    aq.aq_stage_configure(st, aq.AQ_DTYPE, laid_out)
+    table = aq.aq_adam_table(st, **columns(TYPES[laid_out], torch.float32))
+    other = aq.aq_stage_create()
+    for h in (st, other):
+        aq.aq_stage_configure(h, aq.AQ_DTYPE, taken)
+        n = len(recorder.calls)
+        if laid_out == taken:
+            aq.aq_adamw(h, config(32), table, 1, None, None, None)
+            assert recorder.calls[n:] == ["aq_adamw"]
+        else:
+            with pytest.raises(aq.AqError) as e:
+                aq.aq_adamw(h, config(32), table, 1, None, None, None)
+            assert e.value.code == aq.AQ_EINVAL and str(TYPES[laid_out]) in str(e.value) and "aq_adamw" not in recorder.calls[n:]
+        aq.aq_grad_norm(h, table, 1, 1.0, 1.0, None, None, None)              # the gradients' type is in the array
+        assert recorder.calls[-1] == "aq_grad_norm"
+
+
+def test_tables_whose_element_type_is_not_known_are_taken(stage):
+    st, recorder = stage
+    table = aq.aq_adam_table(77, **columns(torch.bfloat16, torch.float32))     # a handle that was not made by the wrappers
+    aq.aq_adamw(st, config(32), table, 1, None, None, None)
+    aq.aq_adamw(77, config(32), aq.aq_adam_table(st, **columns(torch.float16, torch.float32)), 1, None, None, None)
+    aq.aq_adamw(st, config(32), (aq.AdamTensor * 1)(), 1, None, None, None)
+    aq.aq_adamw(st, config(32), 1 << 20, 1, None, None, None)
+    aq.aq_adamw(st, config(32), None, 0, None, None, None)
+    grads = aq.aq_adam_table(st, grads=[Flat(torch.float32, 300, 2 << 20)])
+    aq.aq_stage_configure(st, aq.AQ_DTYPE, aq.AQ_BF16)
+    aq.aq_grad_norm(st, grads, 1, 1.0, 1.0, None, None, None)
+    assert recorder.calls.count("aq_adamw") == 5 and recorder.calls[-1] == "aq_grad_norm"
