@@ -554,13 +554,23 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
 
 // ---- 2-norm of the gradients ------------------------------------------------------------------------------------
 
-// Squares of eight elements are added in binary32, then everything in binary64: a stage has up to billions of them.
+// Squares of eight elements are added in binary32, then everything in binary64: a stage has up to billions of them.  Where binary32 cannot hold the
+// sum of eight, they are rounded to it one by one, and the norm is infinite for an element whose own square is too large alone (no binary16 one's is).
 template <typename G> __device__ double eight_squares(const uint32_t* w) {
   float s = 0.0f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 g = Eight<G>::open(w, i);
     s = fmaf(g.x, g.x, fmaf(g.y, g.y, s));
+  }
+  if (!std::is_same<G, __half>::value && !(s < __int_as_float(0x7f800000))) {
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 g = Eight<G>::open(w, i);
+      sum += (double)(g.x * g.x) + (double)(g.y * g.y);
+    }
+    return sum;
   }
   return (double)s;
 }
