@@ -548,8 +548,8 @@ typedef struct {
 /*
  * The 2-norm of all tensors' gradients together, and the factor that unscales and clips them, without a read on the host:
  *   norm = inv_scale * sqrt(sum g^2),  factor = inv_scale * min(1, max_norm / (norm + 1e-6))
- * inv_scale: 1 / the scale of the loss; max_norm 0 or infinity: no clipping.  norm, factor float[1], step int64[1] (out, device; each may
- * be null).  A norm that is not finite (an infinity or NaN in a gradient, or one whose square exceeds binary32, above 1.8e19) makes factor NaN, with which
+ * inv_scale: 1 / the scale of the loss, a positive number of binary32's range; max_norm 0 or infinity: no clipping.  norm, factor float[1], step int64[1] (out, device; each may
+ * be null).  A norm that is not finite (an infinity or NaN in a gradient, one whose square exceeds binary32, above 1.8e19, or a norm above 3.4e38) makes factor NaN, with which
  * aq_adamw leaves everything as it is; otherwise *step, the number of the optimizer's step, is advanced by one.  Squares
  * below 1e-45 count as nothing.  n >= 0; more than 400 tensors take a launch for every 400.
  */

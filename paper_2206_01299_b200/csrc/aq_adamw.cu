@@ -647,7 +647,7 @@ __global__ void __launch_bounds__(kAdamThreads, kNormCtasPerSm) grad_norm_kernel
   if (!a.first) sum += *before;
   if (!a.last) { *before = sum; return; }
   const double norm = sqrt(sum) * a.inv_scale;
-  const bool fine = norm <= 1.7976931348623157e308;
+  const bool fine = (float)norm < __int_as_float(0x7f800000);   // as it is returned; the factor is at most inv_scale then, a binary32 number
   if (a.norm) *a.norm = (float)norm;
   if (a.factor) *a.factor = fine ? (float)(a.inv_scale * fmin(1.0, a.max_norm / (norm + 1e-6))) : __int_as_float(0x7fc00000);
   if (a.step && fine) ++*a.step;

@@ -538,7 +538,7 @@ int aq_grad_norm(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, double 
   if (!st) return AQ_EINVAL;
   const char* who = "aq_grad_norm";
   if (n < 0 || (n && !tensors)) return fail(st, AQ_EINVAL, "%s: tensors is null, or n is negative", who);
-  if (!(inv_scale > 0.0) || !std::isfinite(inv_scale)) return fail(st, AQ_EINVAL, "%s: inv_scale must be positive and finite", who);
+  if (!((float)inv_scale > 0.0f) || !std::isfinite((float)inv_scale)) return fail(st, AQ_EINVAL, "%s: inv_scale must be positive and finite in binary32", who);
   if (!(max_norm >= 0.0)) return fail(st, AQ_EINVAL, "%s: max_norm must not be negative or NaN", who);
   if (misaligned(norm, 4) || misaligned(factor, 4) || misaligned(step, 8)) return fail(st, AQ_EINVAL, "%s: misaligned pointer", who);
   for (int64_t i = 0; i < n; ++i) AQ_TRY(check_adam_tensor(st, who, i, tensors[i]));

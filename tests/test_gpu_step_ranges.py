@@ -35,3 +35,21 @@ def test_norm_of_gradients_whose_squares_are_binary32_numbers(aq, stage, dtype, 
         g[at[1]] = bad
         norm, factor, step = norm_of(aq, stage, [g])
         assert not math.isfinite(norm) and math.isnan(factor) and step == 0, bad
+
+
+def test_a_norm_beyond_binary32_is_not_counted(aq, stage):  # noqa: F811
+    """norm is infinite as it is returned, so the step is one to leave out, clipped or not."""
+    set_type(aq, stage, "fp32")
+    g = torch.full((4,), 1e10, device="cuda")
+    for limit in (0.0, 1.0):
+        norm, factor, step = norm_of(aq, stage, [g], 1e30, limit)
+        assert norm == math.inf and math.isnan(factor) and step == 0
+        norm, factor, step = norm_of(aq, stage, [g], 1e28, limit)
+        assert math.isfinite(norm) and math.isfinite(factor) and factor > 0 and step == 1
+
+
+@pytest.mark.parametrize("inv_scale", [3.4e38, 2e-38])
+def test_scales_at_the_ends_of_binary32(aq, stage, inv_scale):  # noqa: F811
+    set_type(aq, stage, "fp32")
+    norm, factor, step = norm_of(aq, stage, [torch.full((4,), 0.25, device="cuda")], inv_scale, 0.0)
+    assert abs(norm / (0.5 * inv_scale) - 1) < 3 * E and abs(factor / inv_scale - 1) < E and step == 1

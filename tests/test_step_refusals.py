@@ -112,3 +112,14 @@ def test_tables_whose_element_type_is_not_known_are_taken(stage):
     aq.aq_stage_configure(st, aq.AQ_DTYPE, aq.AQ_BF16)
     aq.aq_grad_norm(st, grads, 1, 1.0, 1.0, None, None, None)
     assert recorder.calls.count("aq_adamw") == 5 and recorder.calls[-1] == "aq_grad_norm"
+
+
+@no_device
+@pytest.mark.parametrize("inv_scale", [1e39, 3.5e38, 1e300, 1e-46, 5e-324])
+def test_a_scale_outside_binary32_is_refused(handle, inv_scale):
+    """The factor would be infinite or zero: a step that is counted but leaves the weights, or one without a gradient."""
+    L = aq.lib()
+    assert L.aq_grad_norm(handle, None, 0, inv_scale, 0.0, None, None, None) == aq.AQ_EINVAL
+    assert b"inv_scale" in L.aq_stage_last_error(handle)
+    for fine in (3.4e38, 1.0, 1e-38, 2e-45):
+        assert L.aq_grad_norm(handle, None, 0, fine, 0.0, None, None, None) == aq.AQ_ECUDA
