@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
   uint32_t here = shared_address(rings) + warp * 2 * Rg::kSlot, there = here + Rg::kSlot;
   next_may_launch();
   wait_for_previous();
-  Settings set{a.factor ? __ldg(a.factor) : 1.0f, a.beta1, a.rest1, a.beta2, a.rest2, a.one, a.eps, 0, 0, 0, 0};
+  Settings set{a.factor ? *a.factor : 1.0f, a.beta1, a.rest1, a.beta2, a.rest2, a.one, a.eps, 0, 0, 0, 0};
   if (!(fabsf(set.factor) < __int_as_float(0x7f800000))) return;   // a step that is to be left out
 
   // of a piece's blocks those from `first` to `end` lie on the grid of eight elements, or all as far behind it, with the grid's elements around
@@ -403,11 +403,11 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
   }
 
   if (threadIdx.x == 0) {
-    const float lr = a.d_lr ? __ldg(a.d_lr) : a.lr;
+    const float lr = a.d_lr ? *a.d_lr : a.lr;
     float c1 = a.c1, c2 = a.c2;
     uint32_t step = a.step;
     if (a.d_step) {
-      const int64_t n = max(__ldg(reinterpret_cast<const long long*>(a.d_step)), 1ll);
+      const int64_t n = max((long long)*a.d_step, 1ll);
       step = (uint32_t)n;
       c1 = (float)(1.0 - power(a.beta1_exact, (uint64_t)n));
       c2 = (float)(1.0 - power(a.beta2_exact, (uint64_t)n));

@@ -36,12 +36,13 @@ template <> struct Scalar<float> {
   static __device__ float close(float x) { return x; }
 };
 
-// A lane's piece of a row: 16 bytes, or one element where rows do not begin on 16-byte boundaries.
+// A lane's piece of a row: 16 bytes, or one element where rows do not begin on 16-byte boundaries.  Loads are ordinary ones, not those for data that
+// nothing writes while a kernel runs: outputs may take the inputs' places, and a kernel may start while the one before still writes its operands.
 template <typename T, bool WHOLE> struct Piece;
 template <typename T> struct Piece<T, true> {
   static constexpr int N = 8;
   using Raw = uint4;
-  static __device__ Raw load(const T* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+  static __device__ Raw load(const T* p) { return *reinterpret_cast<const uint4*>(p); }
   static __device__ void store(T* p, Raw v) { *reinterpret_cast<uint4*>(p) = v; }
   static __device__ void open(Raw v, float* f) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -55,7 +56,7 @@ template <typename T> struct Piece<T, true> {
 template <> struct Piece<float, true> {
   static constexpr int N = 4;
   using Raw = float4;
-  static __device__ Raw load(const float* p) { return __ldg(reinterpret_cast<const float4*>(p)); }
+  static __device__ Raw load(const float* p) { return *reinterpret_cast<const float4*>(p); }
   static __device__ void store(float* p, Raw v) { *reinterpret_cast<float4*>(p) = v; }
   static __device__ void open(Raw v, float* f) { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
   static __device__ Raw close(const float* f) { return make_float4(f[0], f[1], f[2], f[3]); }
@@ -98,7 +99,7 @@ template <typename Pc, typename T> __device__ void load_weights(const T* w, int 
   }
   const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(w + at) & 15);   // the same for a whole warp
   const uint4* const from = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(w + at) - off);
-  const uint4 a = __ldg(from), b = off ? __ldg(from + 1) : a;
+  const uint4 a = *from, b = off ? from[1] : a;
   uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
   if (off & 8) {
 #pragma unroll
@@ -584,7 +585,7 @@ __global__ void __launch_bounds__(kColumns * kWalks) layer_norm_columns_kernel(c
     const int n_rows = (int)min((a.rows - row + step - 1) / step, 64ll);
 #pragma unroll 8
     for (int i = 0; i < n_rows; ++i, row += step) {
-      const float n = (Scalar<T>::open(s[row * a.lds]) - __ldg(a.mean + row)) * __ldg(a.rstd + row), dy = Scalar<T>::open(g[row * a.lddy]);
+      const float n = (Scalar<T>::open(s[row * a.lds]) - a.mean[row]) * a.rstd[row], dy = Scalar<T>::open(g[row * a.lddy]);
       dw = fmaf(dy, n, dw);
       db += dy;
     }
@@ -663,7 +664,7 @@ __global__ void __launch_bounds__(32 * kStripWarps) layer_norm_strips_kernel(con
         float2 n[H], y[H];
         load(static_cast<const T*>(a.s) + row * a.lds + column, n);
         load(static_cast<const T*>(a.dy) + row * a.lddy + column, y);
-        const float mean = __ldg(a.mean + row), rstd = __ldg(a.rstd + row);
+        const float mean = a.mean[row], rstd = a.rstd[row];
 #pragma unroll
         for (int j = 0; j < H; ++j) {
           n[j] = mul2(add2(n[j], both(-mean)), both(rstd));
@@ -679,7 +680,7 @@ __global__ void __launch_bounds__(32 * kStripWarps) layer_norm_strips_kernel(con
     }
   };
   if (hi == N) {
-    walk([](const T* p, float2* f) { Ps::open(__ldg(reinterpret_cast<const uint4*>(p)), f); });
+    walk([](const T* p, float2* f) { Ps::open(*reinterpret_cast<const uint4*>(p), f); });
   } else if (hi) {
     walk([hi](const T* p, float2* f) {
 #pragma unroll
@@ -701,10 +702,11 @@ __global__ void __launch_bounds__(32 * kStripWarps) layer_norm_strips_kernel(con
 }
 
 // dx of wide rows that begin alike in all operands: a CTA has a row in registers, P pieces of 16 bytes to a thread.  Without EDGE they are whole
-// pieces on 16-byte boundaries, and so is w.
+// pieces on 16-byte boundaries, and so is w.  Four pieces go into 64 registers and two CTAs on a multiprocessor (one, at 66: 172 instead of 127 us for
+// 4096 x 12000 fp16).
 constexpr int kWideThreads = 512;
 template <typename T, bool EDGE, int P>
-__global__ void __launch_bounds__(kWideThreads) layer_norm_wide_kernel(const LayerNormGradArgs a) {
+__global__ void __launch_bounds__(kWideThreads, P == 4 ? 2 : 1) layer_norm_wide_kernel(const LayerNormGradArgs a) {
   using Pc = Piece<T, true>;
   constexpr int N = Pc::N, kStep = kWideThreads * N;
   __shared__ float shared[2][kWideThreads / 32];
@@ -737,7 +739,7 @@ __global__ void __launch_bounds__(kWideThreads) layer_norm_wide_kernel(const Lay
     vs[i] = load_piece<Pc>(s + at(i), lo(i), hi(i));
     vy[i] = load_piece<Pc>(dy + at(i), lo(i), hi(i));
   }
-  const float mean = __ldg(a.mean + row), rstd = __ldg(a.rstd + row);
+  const float mean = a.mean[row], rstd = a.rstd[row];
   float sum_g = 0.0f, sum_gn = 0.0f;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
