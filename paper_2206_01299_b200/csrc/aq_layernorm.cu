@@ -871,10 +871,13 @@ template <typename T> cudaError_t run_grad(const LayerNormGradArgs& a, cudaStrea
       const bool whole = a.rows_at == kRowsWhole && a.hidden % kPiece == 0 && reinterpret_cast<uintptr_t>(a.w) % 16 == 0;
       const int span = a.hidden + kPiece - 1;
       const dim3 rows((unsigned)a.rows), threads(kWideThreads);
-      if (whole && a.hidden <= 4 * kWideThreads * kPiece) e = launch(layer_norm_wide_kernel<T, false, 4>, rows, threads, 0, s, a);
-      else if (whole && a.hidden <= 8 * kWideThreads * kPiece) e = launch(layer_norm_wide_kernel<T, false, 8>, rows, threads, 0, s, a);
-      else if (a.rows_at != kRowsAny && span <= 4 * kWideThreads * kPiece) e = launch(layer_norm_wide_kernel<T, true, 4>, rows, threads, 0, s, a);
-      else if (a.rows_at != kRowsAny && span <= 8 * kWideThreads * kPiece) e = launch(layer_norm_wide_kernel<T, true, 8>, rows, threads, 0, s, a);
+      // four pieces where they hold a row; binary32 rows that come here are wider
+      constexpr int kFew = sizeof(T) == 2 ? 4 : 8, kFewSpan = kFew * kWideThreads * kPiece, kSpan = 8 * kWideThreads * kPiece;
+      static_assert(sizeof(T) == 2 || 4 * kWideThreads * kPiece <= 16 * kGradWide, "rows of four binary32 pieces go by the other kernel");
+      if (whole && a.hidden <= kFewSpan) e = launch(layer_norm_wide_kernel<T, false, kFew>, rows, threads, 0, s, a);
+      else if (whole && a.hidden <= kSpan) e = launch(layer_norm_wide_kernel<T, false, 8>, rows, threads, 0, s, a);
+      else if (a.rows_at != kRowsAny && span <= kFewSpan) e = launch(layer_norm_wide_kernel<T, true, kFew>, rows, threads, 0, s, a);
+      else if (a.rows_at != kRowsAny && span <= kSpan) e = launch(layer_norm_wide_kernel<T, true, 8>, rows, threads, 0, s, a);
       else e = launch(layer_norm_rows_kernel<T>, dim3((unsigned)a.rows), dim3(kRowThreads), 0, s, a);
     }
   } else {

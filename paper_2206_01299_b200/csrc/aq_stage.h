@@ -95,7 +95,6 @@ struct LayerNormArgs {
   void* y; long long ldy;
   float *mean, *rstd;                     // may be null
   int rows_at;                            // where rows begin
-  int sms;
 };
 
 struct LayerNormGradArgs {
@@ -171,7 +170,7 @@ long long ffn_grad_partial_bytes(const FfnGradArgs& a);
 cudaError_t launch_ffn(int dtype, const FfnArgs& a, cudaStream_t s);
 cudaError_t launch_ffn_grad(int dtype, const FfnGradArgs& a, cudaStream_t s);
 cudaError_t launch_layer_norm(int dtype, const LayerNormArgs& a, cudaStream_t s);
-// bytes of `partials` that a call with dw or db needs; goes by the sizes, dsum, rows_at and sms
+// bytes of `partials` that a call with dw or db needs; goes by the sizes, the row stride of s, rows_at and sms
 long long layer_norm_grad_bytes(const LayerNormGradArgs& a);
 cudaError_t launch_layer_norm_grad(int dtype, const LayerNormGradArgs& a, cudaStream_t s);
 // `parts`: 0..kAdamTable tensors, none of them empty; they travel in the launch's arguments

@@ -498,7 +498,7 @@ int aq_layer_norm(aq_stage* st, const void* x, int64_t ldx, const void* residual
   DeviceGuard guard(st->device);
   const bool whole = r.whole && hidden % (16 / size_of(st->dtype)) == 0 && !misaligned(w, 16) && !misaligned(b, 16);
   const aq::LayerNormArgs a{x, ldx, residual, ldr, w, b, eps, rows, hidden, sum, lds, y, ldy, mean, rstd,
-                            whole ? aq::kRowsWhole : r.alike ? aq::kRowsAlike : aq::kRowsAny, st->sms};
+                            whole ? aq::kRowsWhole : r.alike ? aq::kRowsAlike : aq::kRowsAny};
   return launched(st, aq::launch_layer_norm(st->dtype, a, st->stream), who);
 }
 
