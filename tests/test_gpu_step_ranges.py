@@ -7,7 +7,7 @@ import torch
 from tests import step_forms as forms
 from tests.stage_forms import TYPES
 from tests.test_gpu_stage import E, set_type
-from tests.test_gpu_step import aq, stage  # noqa: F401
+from tests.test_gpu_step import Set, aq, check_norm, norm_inputs, run_norm, stage  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +53,64 @@ def test_scales_at_the_ends_of_binary32(aq, stage, inv_scale):  # noqa: F811
     set_type(aq, stage, "fp32")
     norm, factor, step = norm_of(aq, stage, [torch.full((4,), 0.25, device="cuda")], inv_scale, 0.0)
     assert abs(norm / (0.5 * inv_scale) - 1) < 3 * E and abs(factor / inv_scale - 1) < E and step == 1
+
+
+@pytest.mark.parametrize("rows,d", [(1375000, 1600), (2000000, 64)])
+def test_sums_over_very_many_rows(aq, stage, rows, d):  # noqa: F811
+    """dw and db of 2.2e9 elements: a thread adds rows / 148 or fewer one by one, then come the CTA's warps and up to 148 CTAs' sums one
+    by one: (rows / 148 + 200) e of the sum of magnitudes with the three roundings of n and of its product."""
+    set_type(aq, stage, "bf16")
+    chunks = [slice(r, min(r + 125000, rows)) for r in range(0, rows, 125000)]
+    s, dy = (torch.empty((rows, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(d)
+    want, size = [torch.zeros((2, d), dtype=torch.float64, device="cuda") for _ in range(2)]
+    for c in chunks:
+        s[c] = torch.randn(s[c].shape, generator=g, device="cuda") + 1.0
+        dy[c] = torch.randn(s[c].shape, generator=g, device="cuda") + 0.25     # a sum that grows with the rows
+        mean[c], rstd[c] = s[c].float().mean(1), 1 + 0.1 * torch.rand(s[c].shape[0], generator=g, device="cuda")
+        y = dy[c].double()
+        n = (s[c].double() - mean[c, None].double()) * rstd[c, None].double()
+        for out, f in ((want, lambda x: x), (size, torch.abs)):
+            out += torch.stack([f(y * n).sum(0), f(y).sum(0)])
+        del y, n
+    w, dw, db = torch.ones(d, device="cuda").bfloat16(), torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    dx = torch.empty_like(s) if d == 64 else None
+    aq.aq_layer_norm_grad(stage, dy, d, None, 0, s, d, w, mean, rstd, rows, d, dx, d, dw, db)
+    k = (rows / 148 + 200) * E
+    for have, exact, magnitude in zip((dw, db), want, size):
+        assert bool(((have.double() - exact).abs() <= k * magnitude).all())
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "fp32"])
+@pytest.mark.parametrize("d", [1, 40, 64, 1021, 1600, 1601, 5000, 12001, 33000, 40001])
+@pytest.mark.parametrize("with_w,with_b", [(True, False), (False, True)])
+def test_layer_norm_with_one_of_weight_and_bias(aq, stage, dtype, d, with_w, with_b):  # noqa: F811
+    set_type(aq, stage, dtype)
+    for pad, offset in ((0, 0), (3, 0), (1, 5)):
+        x, r, w, b, _, _ = norm_inputs(5, d, dtype, seed=12)
+        w, b = w if with_w else None, b if with_b else None
+        s, y, mean, rstd = run_norm(aq, stage, dtype, x, r, w, b, 1e-5, pad, offset)
+        check_norm(dtype, s, torch.ones(d) if w is None else w, torch.zeros(d) if b is None else b, 1e-5, y, mean, rstd)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_gradient_whose_square_exceeds_binary32(aq, stage, bits):  # noqa: F811
+    """v is infinite then and the element moves by its decay alone; in 8 bits its block's v is NaN from the next step on, and other blocks
+    are as they would have been."""
+    set_type(aq, stage, "fp32")
+    one, two = (Set([1000], "fp32", "fp32", bits, False, False, seed=41, decay=0.0) for _ in range(2))
+    one.grad[0][300] = 1e20
+    old = one.param[0].clone()
+    for s in (one, two):
+        aq.aq_adamw(stage, aq.AdamwConfig(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=3, state_bits=bits), s.table(aq, stage), 1, None, None, None)
+    assert one.param[0][300] == old[300]
+    keep = torch.arange(1000, device="cuda") != 300
+    assert torch.equal(one.param[0][keep], two.param[0][keep])
+    if bits == 32:
+        assert one.v[0][300] == math.inf and torch.equal(one.v[0][keep], two.v[0][keep]) and torch.equal(one.m[0][keep], two.m[0][keep])
+    else:
+        assert one.v_scale[0].isnan().tolist() == [False, True, False, False] and not one.m_scale[0].isnan().any()
+        others = torch.arange(1000, device="cuda") // 256 != 1
+        for name in ("m", "v"):
+            assert torch.equal(getattr(one, name)[0].view(torch.uint8)[others], getattr(two, name)[0].view(torch.uint8)[others])
