@@ -458,6 +458,7 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
       if (i >= here) break;
       const float2 st = stats[slot][warp][i];
       const float mean = st.x, rstd = rstds[i] = st.y;
+      const bool far = !(fabsf(mean * rstd) < __int_as_float(0x7f800000));   // a zero would have an infinite n, whatever the row's elements have
       float2 sg = make_float2(0.0f, 0.0f), sgn = sg;
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
@@ -469,6 +470,11 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
 #pragma unroll
           for (int j = 0; j < N; ++j)
             if (j < lo[q]) (j & 1 ? n[i][q][j / 2].y : n[i][q][j / 2].x) = (j & 1 ? y[i][q][j / 2].y : y[i][q][j / 2].x) = 0.0f;
+        }
+        if (far && hi[q] < N) {                                // places behind the row's end, which hold zeros
+#pragma unroll
+          for (int j = 0; j < N; ++j)
+            if (j >= hi[q]) (j & 1 ? n[i][q][j / 2].y : n[i][q][j / 2].x) = 0.0f;
         }
 #pragma unroll
         for (int j = 0; j < H; ++j) {
@@ -752,6 +758,7 @@ __global__ void __launch_bounds__(kWideThreads, P == 4 ? 2 : 1) layer_norm_wide_
     for (int j = 0; j < N; ++j) {                              // elements around the row have dy of zero
       g[j] *= w[j];
       sum_g += g[j];
+      if (EDGE && (j < lo(i) || j >= hi(i))) continue;         // but mean rstd may be infinite where no element of the row is
       sum_gn = fmaf(g[j], (f[j] - mean) * rstd, sum_gn);
     }
   }

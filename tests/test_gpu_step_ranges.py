@@ -7,7 +7,7 @@ import torch
 from tests import step_forms as forms
 from tests.stage_forms import TYPES
 from tests.test_gpu_stage import E, set_type
-from tests.test_gpu_step import Set, aq, check_norm, norm_inputs, run_norm, stage  # noqa: F401
+from tests.test_gpu_step import Set, aq, check_norm, check_norm_grad, norm_inputs, run_norm, run_norm_grad, stage, statistics  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -114,3 +114,19 @@ def test_a_gradient_whose_square_exceeds_binary32(aq, stage, bits):  # noqa: F81
         others = torch.arange(1000, device="cuda") // 256 != 1
         for name in ("m", "v"):
             assert torch.equal(getattr(one, name)[0].view(torch.uint8)[others], getattr(two, name)[0].view(torch.uint8)[others])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [3, 64, 250, 1021, 1600, 2045, 5001, 8190, 12000, 12001, 40001])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_gradient_of_rows_very_far_from_zero(aq, stage, dtype, d, pad):  # noqa: F811
+    """Rows of one value, whose mean times rstd is beyond binary32 though every element is at its mean: the places behind a row's end, which
+    threads fill with zeros, count for nothing."""
+    set_type(aq, stage, dtype)
+    rows = 19
+    s, _, w, _, dy, dsum = norm_inputs(rows, d, dtype, seed=13)
+    s[::3] = torch.tensor([2.0 ** 115, -2.0 ** 120, 2.0 ** 127, 2.0 ** 100])[torch.arange(rows)[::3] % 4].to(s.dtype)[:, None]
+    mean, rstd = statistics(s)
+    mean[::3], rstd[::3] = s[::3, 0].float(), 1e5
+    got = run_norm_grad(aq, stage, dtype, dy, dsum, s, w, mean, rstd, pad)
+    check_norm_grad(dtype, dy, dsum, s, w, mean, rstd, got)
