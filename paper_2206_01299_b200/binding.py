@@ -417,8 +417,8 @@ def aq_layer_norm_grad(st, dy, lddy, dsum, ldds, s, lds, w, mean, rstd, rows, hi
 def aq_adam_table(st, grads, params=None, masters=None, m=None, v=None, m_scale=None, v_scale=None, weight_decay=0.0):
     """Array of AdamTensor for aq_adamw, or for aq_grad_norm where nothing but the gradients is given.
 
-    Every argument is a list with one contiguous CUDA tensor (or None, for a tensor without that part) for each of the
-    tensors; weight_decay is a number for all of them or a list.  Moments in 8 bits are torch.float8_e4m3fn (m) and torch.float8_e5m2 (v) or
+    Every argument is a list with one contiguous CUDA tensor (or None, for a tensor without that part; every one has a
+    gradient) for each of the tensors; weight_decay is a number for all of them or a list.  Moments in 8 bits are torch.float8_e4m3fn (m) and torch.float8_e5m2 (v) or
     their bytes as torch.uint8, with m_scale and v_scale.  The array holds addresses: it can be kept for as long as the
     tensors keep their places, and does not keep them alive.  Lay it out anew where gradients are allocated in every step.
     aq_adamw refuses it with a handle of another element type.
@@ -436,6 +436,7 @@ def aq_adam_table(st, grads, params=None, masters=None, m=None, v=None, m_scale=
     table.element_type = t                              # the parameters'; nothing in the structure tells it
     written = []
     for i, row in enumerate(table):
+        assert grads[i] is not None, f"tensor {i} has no gradient: one that is left out of a step is left out of its table"
         row.numel, row.weight_decay, row.grad_dtype = grads[i].numel(), decay[i], codes[grads[i].dtype]
         for name, column in columns.items():
             x = None if column is None else column[i]

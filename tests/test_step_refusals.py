@@ -123,3 +123,11 @@ def test_a_scale_outside_binary32_is_refused(handle, inv_scale):
     assert b"inv_scale" in L.aq_stage_last_error(handle)
     for fine in (3.4e38, 1.0, 1e-38, 2e-45):
         assert L.aq_grad_norm(handle, None, 0, fine, 0.0, None, None, None) == aq.AQ_ECUDA
+
+
+def test_a_tensor_without_a_gradient_is_refused(stage):
+    st, _ = stage
+    c = {n: x * 1 + [Flat(x[0].dtype, 300, x[0].at + (1 << 16))] for n, x in columns(torch.float16, torch.float16).items()}
+    assert len(aq.aq_adam_table(st, **c)) == 2
+    with pytest.raises(AssertionError, match="tensor 1 has no gradient"):
+        aq.aq_adam_table(st, **dict(c, grads=[c["grads"][0], None]))
