@@ -510,8 +510,8 @@ int aq_qk_norm_rope_grad(aq_stage* st, const aq_qk_shape* shape, int64_t rows, c
  * may be null): what aq_layer_norm_grad needs, with s.  s is rounded to T, as it is stored, before the norm.  y may be x
  * or residual, and sum may be the other of the two or residual, where their row strides are equal.  hidden in 1..2^20, rows >= 0, element
  * alignment; rows of whole 16-byte pieces on 16-byte boundaries are the fast ones.  A row with a NaN or an infinity has NaN in mean, rstd and y or
- * parts of them, and touches no other row; with eps 0 so has a row of equal values.  Squares are binary32: a row with elements 1e19 and more
- * from its mean has rstd 0.
+ * parts of them, and touches no other row; with eps 0 so has a row of equal values.  Sums and squares are binary32: a row whose elements add up to
+ * more than 3.4e38 may count as one with an infinity, and one with elements 1e19 and more from its mean has rstd 0.
  */
 int aq_layer_norm(aq_stage* st, const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* w, const void* b, float eps,
                   int64_t rows, int hidden, void* sum, int64_t lds, void* y, int64_t ldy, float* mean, float* rstd);
@@ -522,8 +522,9 @@ int aq_layer_norm(aq_stage* st, const void* x, int64_t ldx, const void* residual
  * dy T[rows][lddy] (in); dsum T[rows][ldds] (in; may be null): the gradient that reaches s past the norm, along the residual
  * stream; s (the stored sum, or x without a residual), mean, rstd as aq_layer_norm left them.  dx T[rows][lddx] (out; may be null) is
  * the gradient of x and of residual alike; it may be dy, dsum or s, where the row strides are equal.  dw, db float[hidden] (out; each may be null).
- * A row with a NaN or an infinity makes dw and db NaN, and its own dx.  Sums of dw and db are kept in the handle's workspace, which grows
- * as aq_gated_ffn_grad says.
+ * A row with a NaN or an infinity makes dw and db NaN, and its own dx.  dw and db are sums of rows / 148 or fewer terms one by one in binary32 and
+ * then of those: an element is off by at most (rows / 148 + 200) * 2^-24 of the sum of its terms' magnitudes.  They are kept in the handle's workspace,
+ * which grows as aq_gated_ffn_grad says.
  */
 int aq_layer_norm_grad(aq_stage* st, const void* dy, int64_t lddy, const void* dsum, int64_t ldds, const void* s, int64_t lds, const void* w,
                        const float* mean, const float* rstd, int64_t rows, int hidden, void* dx, int64_t lddx, float* dw, float* db);
@@ -551,7 +552,8 @@ typedef struct {
  * inv_scale: 1 / the scale of the loss, a positive number of binary32's range; max_norm 0 or infinity: no clipping.  norm, factor float[1], step int64[1] (out, device; each may
  * be null).  A norm that is not finite (an infinity or NaN in a gradient, one whose square exceeds binary32, above 1.8e19, or a norm above 3.4e38) makes factor NaN, with which
  * aq_adamw leaves everything as it is; otherwise *step, the number of the optimizer's step, is advanced by one.  Squares
- * below 1e-45 count as nothing.  n >= 0; more than 400 tensors take a launch for every 400.
+ * below 1e-45 count as nothing.  n >= 0; more than 400 tensors take a launch for every 400, where a gradient that does not begin at a multiple of
+ * eight elements counts twice, and a tensor for every 2^30 elements.
  */
 int aq_grad_norm(aq_stage* st, const aq_adam_tensor* tensors, int64_t n, double inv_scale, double max_norm, float* norm, float* factor, int64_t* step);
 
@@ -578,7 +580,9 @@ typedef struct {
  * A = 0xBB67AE85 and B = 0x9E3779B9:  k = step * B;  k = (k ^ k >> 16) * A;  k = (k ^ k >> 15) * B;  k = k ^ k >> 16;
  * u = (i + k) * A;  u = (u ^ u >> 15) * B;  u = u ^ u >> 16.  A v above zero does not become zero.  m and v are computed with a rounding of
  * every product and sum, so that the codes are reproducible elsewhere.  A gradient that is not finite, where no factor holds the step
- * back, makes its element NaN, and with 8-bit moments its whole block from the next step on.
+ * back, makes its element NaN, and with 8-bit moments its whole block from the next step on.  One whose square exceeds binary32 (above 1.8e19) makes
+ * v infinite: the element moves by its decay alone from then on, and with 8-bit moments the block is NaN from the next step on.  Launches as for
+ * aq_grad_norm; with 32-bit moments a tensor counts twice whose addresses lie off the multiples of eight elements, all by as many.
  */
 int aq_adamw(aq_stage* st, const aq_adamw_config* config, const aq_adam_tensor* tensors, int64_t n, const float* factor, const float* d_lr,
              const int64_t* d_step);

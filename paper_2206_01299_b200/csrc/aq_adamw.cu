@@ -10,8 +10,10 @@
 // 8-bit moments).  Two CTAs on a multiprocessor are enough where every thread has 100 bytes and more on their way.
 //
 // Measured, of a plain copy's 6.5 TB/s: 246M fp16 weights with binary32 copies and moments 1105 us (0.95), 492M bf16 weights with
-// 8-bit moments 935 to 985 us (0.77 to 0.81), where instruction issue (0.6, 44 instructions an element, a sixth of them the hash) and
-// memory share the time: 865 us without the arithmetic, 950 us without the hash.  13M weights in tensors of any length 47 us (0.42).
+// 8-bit moments 934 to 993 us (0.76 to 0.81), where instruction issue (0.6, 44 instructions an element, a sixth of them the hash) and
+// memory share the time: 865 us without the arithmetic, 950 us without the hash.  13M weights in tensors of any length 47 us (0.42).  8-bit moments
+// of 246M weights beside binary32 copies 685 to 696 us (0.87), of binary32 weights 655 to 674 us (0.9), with binary32 gradients of bf16 weights without a
+// copy 623 to 736 us (0.61 to 0.72): their rings hold one block a piece.
 //
 // Moments in 8 bits.  256 elements are a block with one scale per moment: the smallest power of two that keeps the
 // block's largest magnitude in the format (m e4m3, up to 1.75 * 2^8; v e5m2, up to 1.75 * 2^15).  Powers of two, since scaling by them
@@ -574,7 +576,7 @@ template <typename G> __device__ double eight_squares(const uint32_t* w) {
   }
   return (double)s;
 }
-// A warp's blocks of one tensor, from element `at` on.  Four blocks are on their way at a time: 492M fp16 gradients take 144 us, with one 206 us.
+// A warp's blocks of one tensor, from element `at` on.  Four blocks are on their way at a time: 492M fp16 gradients take 140 to 145 us, with one 206 us.
 template <typename G> __device__ double squares(const AdamPart& part, uint32_t at, uint32_t blocks, int lane) {
   const G* const g = static_cast<const G*>(part.grad);
   double sum = 0.0;

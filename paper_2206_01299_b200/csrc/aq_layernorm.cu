@@ -9,15 +9,15 @@
 // last use, so the variance is that of the differences from the mean (no cancellation), and every operand is read once.
 //
 // Forward: rows up to 256 pieces of 16 bytes belong to a warp, which needs no barrier; wider ones to a CTA.  32768 x 1600 fp16 with a
-// residual 68 to 69 us, 0.93 to 0.95 of a plain copy's bandwidth.
+// residual 68 to 70 us, 0.92 to 0.95 of a plain copy's bandwidth.
 // Backward: a CTA of as many threads as a row has eight elements (up to 256 elements: eight warps with a row each; over 2048: sixteen to
-// a thread) walks over the rows, a thread always at the same columns, whose sums of dw and db it keeps in registers; a CTA's sums go to a workspace,
-// which a second kernel adds up in a fixed order.  Rows come ahead through shared memory by asynchronous copies.  32768 x 1600 fp16 with a gradient
-// along the stream 77 to 82 us (0.78 to 0.84): two CTAs of 120 registers a thread, and 24 instructions an element with a barrier for every two rows;
+// a thread) walks over the rows, a thread always at the same columns, whose sums of dw and db it keeps in registers, in binary32 over all of its rows
+// (110 of 32768 x 1600's, rows / 148 at most); a CTA's sums go to a workspace, which a second kernel adds up in a fixed order.  Rows come ahead through shared memory by asynchronous copies.  32768 x 1600 fp16 with a gradient
+// along the stream 77 to 83 us (0.77 to 0.84): two CTAs of 120 registers a thread, and 25 instructions an element with a barrier for every two rows;
 // issue 0.44.  16384 x 1600 binary32 68 us (0.95).  What did not help: three CTAs at 80 registers (spills, 83 to 125 us), forming n and g again after
 // the barrier instead of keeping them (89 us), one row or four at a time (106 us, 87 us), a thread's copies side by side in shared memory (115 us).
 // Rows that begin inside a piece: forward a row's pieces are those of the grid it lies on, the first and last by elements; backward a CTA takes
-// every `period`-th row, which begin alike, so that its columns stay.  16384 x 1601 fp16: 80 us and 52 us (one element at a time: 217 and 152).
+// every `period`-th row, which begin alike, so that its columns stay.  16384 x 1601 fp16: 78 us and 50 us (one element at a time: 217 and 152).
 // Backward, rows over 8192 elements are read once for the columns' sums and once for dx (4096 x 12000 fp16: 126 us, element by element 269). Rows of
 // operands that begin differently, and forward rows over 4096 pieces, go element by element through kernels that read them again.
 
