@@ -17,7 +17,7 @@
 // issue 0.44.  16384 x 1600 binary32 68 us (0.95).  What did not help: three CTAs at 80 registers (spills, 83 to 125 us), forming n and g again after
 // the barrier instead of keeping them (89 us), one row or four at a time (106 us, 87 us), a thread's copies side by side in shared memory (115 us).
 // Rows that begin inside a piece: forward a row's pieces are those of the grid it lies on, the first and last by elements; backward a CTA takes
-// every `period`-th row, which begin alike, so that its columns stay.  16384 x 1601 fp16: 78 us and 50 us (one element at a time: 217 and 152).
+// every `period`-th row, which begin alike, so that its columns stay.  16384 x 1601 fp16: 78 us and 49 us (one element at a time: 217 and 152).
 // Backward, rows over 8192 elements are read once for the columns' sums and once for dx (4096 x 12000 fp16: 126 us, element by element 269). Rows of
 // operands that begin differently, and forward rows over 4096 pieces, go element by element through kernels that read them again.
 
@@ -458,7 +458,7 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
       if (i >= here) break;
       const float2 st = stats[slot][warp][i];
       const float mean = st.x, rstd = rstds[i] = st.y;
-      const bool far = !(fabsf(mean * rstd) < __int_as_float(0x7f800000));   // a zero would have an infinite n, whatever the row's elements have
+      const bool far = fabsf(mean) > 1e15f;                    // a zero's n may be infinite (rstd is 3e22 at most), whatever the row's elements have
       float2 sg = make_float2(0.0f, 0.0f), sgn = sg;
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(MAX, CTAS) layer_norm_grad_kernel(const LayerN
           for (int j = 0; j < N; ++j)
             if (j < lo[q]) (j & 1 ? n[i][q][j / 2].y : n[i][q][j / 2].x) = (j & 1 ? y[i][q][j / 2].y : y[i][q][j / 2].x) = 0.0f;
         }
-        if (far && hi[q] < N) {                                // places behind the row's end, which hold zeros
+        if (far) {                                             // places behind the row's end, which hold zeros
 #pragma unroll
           for (int j = 0; j < N; ++j)
             if (j >= hi[q]) (j & 1 ? n[i][q][j / 2].y : n[i][q][j / 2].x) = 0.0f;

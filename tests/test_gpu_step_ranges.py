@@ -130,3 +130,19 @@ def test_gradient_of_rows_very_far_from_zero(aq, stage, dtype, d, pad):  # noqa:
     mean[::3], rstd[::3] = s[::3, 0].float(), 1e5
     got = run_norm_grad(aq, stage, dtype, dy, dsum, s, w, mean, rstd, pad)
     check_norm_grad(dtype, dy, dsum, s, w, mean, rstd, got)
+
+
+@pytest.mark.parametrize("d", [3, 64, 250, 1600, 2045, 8190, 12000, 12001, 40001])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_gradient_of_rows_very_far_apart(aq, stage, d, pad):  # noqa: F811
+    """Rows with elements of 3e38 on both sides of their mean, which have rstd 0: dx is the gradient along the stream."""
+    set_type(aq, stage, "fp32")
+    rows = 19
+    s, _, w, _, dy, dsum = norm_inputs(rows, d, "fp32", seed=14)
+    s[::3] = 3e38 * torch.sign(s[::3])
+    dy[::3] *= 100
+    mean, rstd = statistics(s)
+    mean[::3], rstd[::3] = 0.0, 0.0
+    got = run_norm_grad(aq, stage, "fp32", dy, dsum, s, w, mean, rstd, pad)
+    check_norm_grad("fp32", dy, dsum, s, w, mean, rstd, got)
+    assert torch.equal(got[0][::3].cpu(), dsum[::3])
